@@ -36,6 +36,9 @@ EXPORTS = (
     "lccrf_strerror", "lccrf_version", "lccrf_marginals_static", "lccrf_static_scratch_bytes",
     "lccrf_set_pair_poll_limit", "lccrf_set_lane_poll_limit", "lccrf_stream_probe", "lccrf_stream_probe_bytes", "lccrf_sample_seeded",
     "lccrf_first_pass_largest_row", "lccrf_marginals_by_edges", "lccrf_first_pass_pieces",
+    "lccrf_embed", "lccrf_embed_grad", "lccrf_embed_grad_workspace_bytes", "lccrf_conv", "lccrf_conv_grad",
+    "lccrf_conv_grad_workspace_bytes", "lccrf_conv_step", "lccrf_state_scan", "lccrf_state_scan_saved_bytes",
+    "lccrf_state_scan_workspace_bytes", "lccrf_state_scan_grad", "lccrf_state_scan_grad_workspace_bytes", "lccrf_state_step",
 )
 
 _lib = None
@@ -113,6 +116,7 @@ def load_library() -> ctypes.CDLL:
     lib.lccrf_set_lane_poll_limit.restype = i
     lib.lccrf_auto_algo.argtypes = [i, i, i, i]
     lib.lccrf_auto_algo.restype = i
+    _encoder.declare(lib)
     _lib = lib
     return lib
 
@@ -454,3 +458,10 @@ def lccrf_stream_probe(src: torch.Tensor, dst: Optional[torch.Tensor], workgroup
     _enqueue("lccrf_stream_probe", src.device, lib.lccrf_stream_probe, src.data_ptr(), None if dst is None else dst.data_ptr(), nbytes, int(workgroups),
              sink.data_ptr(), _stream(src.device))
     return int(lib.lccrf_stream_probe_bytes(nbytes, int(workgroups)))
+
+
+# What stands in front of the chain (include/lccrf_encoder.h).
+from . import encoder as _encoder  # noqa: E402
+from .encoder import (  # noqa: E402,F401
+    lccrf_conv, lccrf_conv_grad, lccrf_conv_step, lccrf_embed, lccrf_embed_grad, lccrf_state_scan, lccrf_state_scan_grad,
+    lccrf_state_step, state_scan_saved)

@@ -1,0 +1,109 @@
+// Shared by the scan's forward and backward kernels: how channels, states and positions are spread, and what goes through LDS.
+//
+// A lane has one channel with all its states in registers; a wave 64 channels of one group, so Bm and Cm of a position are the
+// same for all its lanes: a wave puts those of eight positions into LDS of its own, widened, and reads them back as
+// broadcasts.  The state lives in base 2: exp(step A) = exp2(step (A log2 e)).
+#pragma once
+
+#include "lccrf_encoder.h"
+
+namespace lccrf {
+namespace enc {
+
+constexpr int kP = kScanBlock;
+
+struct ScanPlan {
+    int tiles;      // waves that cover a group's channels
+    int segments;   // a sequence is cut into so many
+    int seg_len;    // positions each, a multiple of kP
+};
+
+// Where a wave's work lies.
+struct Where {
+    int b, seg, group, channel;  // channel of this lane (clamped into the group)
+    bool is;                     // lane has a channel of its own
+};
+
+__device__ __forceinline__ int clamp_length(const int32_t* lengths, int b, int N) {
+    if (!lengths) return N;
+    const int n = lengths[b];
+    return n < 0 ? 0 : n > N ? N : n;
+}
+
+template <typename T> __device__ __forceinline__ const T* at(const AnyRows& r, int64_t b, int64_t l) {
+    return static_cast<const T*>(r.data) + b * r.batch + l * r.row;
+}
+
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// exp2's argument of a state: A log2(e), kept finite so that a step of 0 (positions past the end) leaves the state as it is.
+__device__ __forceinline__ float base2(float A) {
+    const float a = A * kLog2e;
+    return a < -3.0e38f ? -3.0e38f : a;
+}
+
+// Bm and Cm of kP positions for the states s0 .. s0 + SP - 1, on their way from memory to LDS [kP][2 * SP] (Bm, then Cm).
+// Positions outside [0, len) and states past S count as 0.
+template <typename T, int SP> struct GroupVectors {
+    static constexpr int R = kP * 2 * SP / 64 ? kP * 2 * SP / 64 : 1;
+    T raw[R];
+    __device__ __forceinline__ void load(const ScanIn& in, int b, int l0, int len, int group, int s0, int lane) {
+        const T* B = at<T>(in.Bm, b, 0) + group * in.b_group;
+        const T* C = at<T>(in.Cm, b, 0) + group * in.c_group;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int k = i * 64 + lane, s = s0 + k % SP;
+            int l = l0 + k / (2 * SP);
+            l = l < len ? l : len - 1;
+            const bool c = k / SP & 1;
+            raw[i] = (c ? C : B)[l * (c ? in.Cm.row : in.Bm.row) + (s < in.S ? s : 0)];
+        }
+    }
+    __device__ __forceinline__ void put(float* lds, const ScanIn& in, int l0, int len, int s0, int lane) const {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int k = i * 64 + lane;
+            const bool is = s0 + k % SP < in.S && l0 + k / (2 * SP) < len;
+            if (kP * 2 * SP >= 64 || k < kP * 2 * SP) lds[k] = is ? widen(raw[i]) : 0.0f;
+        }
+    }
+};
+
+// Saved states: [B][ceil(N / kP)][ceil(S / 4)][D][4] floats.
+__host__ __device__ inline int quads(int S) { return (S + 3) / 4; }
+__device__ __forceinline__ int64_t quad_at(int64_t block, int S, int D, int q, int d) { return ((block * quads(S) + q) * D + d) * 4; }
+
+inline int scan_blocks(int N) { return (N + kP - 1) / kP; }
+
+// Segments: the recursion over a segment needs the state in front of it, which takes a pass of its own over all segments (six
+// tenths of the work again) and a short one along them.  That pays where the waves that the batch has by itself leave
+// most of the chip empty.
+inline ScanPlan scan_plan(int B, int N, int D, int G, int waves_a_tile) {
+    ScanPlan p;
+    p.tiles = (D / G + 63) / 64;
+    const int64_t waves = static_cast<int64_t>(B) * G * p.tiles * waves_a_tile;
+    int64_t segments = waves >= 1024 ? 1 : (2048 + waves - 1) / waves;
+    const int64_t most = (N + 63) / 64;
+    if (segments > most) segments = most;
+    p.seg_len = static_cast<int>(((N + segments - 1) / segments + kP - 1) / kP * kP);
+    p.segments = (N + p.seg_len - 1) / p.seg_len;
+    return p;
+}
+
+inline bool scan_fits(int B, int N, int D, int S, int G, const ScanPlan& p) {
+    const int64_t most = (int64_t{1} << 32) - 1024, b = B;
+    return b * p.segments * G * p.tiles * 256 < most && b * D * quads(S) < most && b * N * G * S < most;
+}
+
+// Runs the scan for the saved states alone (out and final_state null), or with them.
+hipError_t run_state_scan(int dtype, const ScanIn& in, const float* state, void* out, float* final_state, float* saved, void* ws, hipStream_t st);
+// The pass along the segments: ends [B][segments][quads][D][4] of every segment from 0 become what stands at its beginning
+// (back: at its end).  state: [B][D][S] in front of the first, or null.
+hipError_t launch_join_segments(const ScanIn& in, const ScanPlan& p, const float* state, float* ends, const float* steps, bool back, hipStream_t st);
+
+}  // namespace enc
+}  // namespace lccrf

@@ -1,0 +1,353 @@
+// Selective state space scan: forward pass and single-token form.
+//
+// An update of one state is a product, an exponential (two issue slots), a product, two fused multiply-adds: six slots of a
+// SIMD, which with 16 states bound the pass before its traffic does (per channel and position 96 slots, some 30 for the gates, against
+// 8 bytes).  All of it is vector arithmetic: the decays differ by channel and state, so no matrix instruction has the form.
+// Segments of a sequence run side by side where the batch is small (scan_plan).
+#include "lccrf_state.h"
+
+namespace lccrf {
+namespace enc {
+namespace {
+
+enum { kOut = 1, kSave = 2, kEnds = 4 };
+
+struct ScanRun {
+    ScanIn in;
+    const float* state;  // [B][D][S] or null
+    void* out;
+    float* final_state;
+    float* saved;
+    float* ends;   // segments > 1: the states in front of every segment (kEnds: written, what a segment makes of 0)
+    float* steps;  // kEnds: sum of the steps [B][segments][D]
+    ScanPlan plan;
+    int waves;     // of a workgroup
+};
+
+template <typename T, int SP, int MODE>
+__global__ __launch_bounds__(256, SP <= 16 ? 3 : 2) void scan_kernel(ScanRun r) {
+    extern __shared__ float lds[];  // [waves][kP][2 * SP]
+    const ScanIn& in = r.in;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int groups_of_tiles = (in.G * r.plan.tiles + r.waves - 1) / r.waves;
+    const unsigned which = blockIdx.x / groups_of_tiles;
+    const int tile = (blockIdx.x - which * groups_of_tiles) * r.waves + wave;
+    const int b = which / r.plan.segments, seg = which - b * r.plan.segments;
+    if (tile >= in.G * r.plan.tiles) return;
+    const int width = in.D_ / in.G, group = tile / r.plan.tiles, c0 = (tile - group * r.plan.tiles) * 64 + lane;
+    const bool is = c0 < width;
+    const int d = group * width + (is ? c0 : width - 1);
+    const int len = clamp_length(in.lengths, b, in.N), begin = seg * r.plan.seg_len;
+    const int stop = begin + r.plan.seg_len < in.N ? begin + r.plan.seg_len : in.N, end = stop < len ? stop : len;
+    float* bc = lds + wave * (kP * 2 * SP);
+    T* out = MODE & kOut ? static_cast<T*>(r.out) + static_cast<int64_t>(b) * in.N * in.D_ + d : nullptr;
+    const bool gated = in.z.data != nullptr;
+    const float skip = in.D ? in.D[d] : 0.0f, bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
+
+    float h[SP], A[SP], total = 0.0f;
+#pragma unroll
+    for (int s = 0; s < SP; ++s) {
+        A[s] = s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s]) : 0.0f;
+        h[s] = 0.0f;
+    }
+    if (!(MODE & kEnds)) {
+        if (r.plan.segments > 1) {
+            const int64_t from = static_cast<int64_t>(b) * r.plan.segments + seg;
+#pragma unroll
+            for (int s = 0; s < SP; ++s)
+                if (s < in.S) h[s] = r.ends[quad_at(from, in.S, in.D_, s / 4, d) + s % 4];
+        } else if (r.state) {
+#pragma unroll
+            for (int s = 0; s < SP; ++s)
+                if (s < in.S) h[s] = r.state[(static_cast<int64_t>(b) * in.D_ + d) * in.S + s];
+        }
+    }
+
+    if (begin < end) {
+        T xr[kP], tr[kP], zr[kP];
+        GroupVectors<T, SP> gv;
+        const auto fetch = [&](int l0) {
+            gv.load(in, b, l0, len, group, 0, lane);
+#pragma unroll
+            for (int i = 0; i < kP; ++i) {
+                const int l = l0 + i < len ? l0 + i : len - 1;
+                xr[i] = at<T>(in.x, b, l)[d];
+                tr[i] = at<T>(in.dt, b, l)[d];
+                if (MODE & kOut)
+                    if (gated) zr[i] = at<T>(in.z, b, l)[d];
+            }
+        };
+        fetch(begin);
+        for (int l0 = begin; l0 < end; l0 += kP) {
+            float step[kP], put[kP], y[kP], x[kP], z[kP];
+#pragma unroll
+            for (int i = 0; i < kP; ++i) {
+                const bool on = l0 + i < end;
+                step[i] = on ? softplus(widen(tr[i]) + bias).value : 0.0f;
+                x[i] = on ? widen(xr[i]) : 0.0f;
+                put[i] = step[i] * x[i];
+                if (MODE & kOut) z[i] = gated ? widen(zr[i]) : 0.0f;
+                if (MODE & kEnds) total += step[i];
+            }
+            wave_sync();
+            gv.put(bc, in, l0, len, 0, lane);
+            wave_sync();
+            if (l0 + kP < end) fetch(l0 + kP);
+            if (MODE & kSave) {
+                const int64_t block = static_cast<int64_t>(b) * ((in.N + kP - 1) / kP) + l0 / kP;
+#pragma unroll
+                for (int q = 0; q < SP / 4; ++q)
+                    if (is && 4 * q < in.S)
+                        *reinterpret_cast<f32x4*>(r.saved + quad_at(block, in.S, in.D_, q, d)) = f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]};
+            }
+#pragma unroll
+            for (int i = 0; i < kP; ++i) {
+                const f32x4* B4 = reinterpret_cast<const f32x4*>(bc + i * 2 * SP);
+                const f32x4* C4 = B4 + SP / 4;
+                float y0 = 0.0f, y1 = 0.0f;
+#pragma unroll
+                for (int q = 0; q < SP / 4; ++q) {
+                    const f32x4 Bq = B4[q];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int s = 4 * q + j;
+                        h[s] = fmaf(exp2_fast(step[i] * A[s]), h[s], put[i] * Bq[j]);
+                    }
+                    if (MODE & kOut) {
+                        const f32x4 Cq = C4[q];
+                        y0 = fmaf(h[4 * q], Cq[0], y0);
+                        y1 = fmaf(h[4 * q + 1], Cq[1], y1);
+                        y0 = fmaf(h[4 * q + 2], Cq[2], y0);
+                        y1 = fmaf(h[4 * q + 3], Cq[3], y1);
+                    }
+                }
+                y[i] = y0 + y1;
+                asm volatile("" : "+v"(y[i]));  // computed here: moved behind the store's condition, it would keep the states of all eight positions
+            }
+            if (MODE & kOut) {
+#pragma unroll
+                for (int i = 0; i < kP; ++i) {
+                    const float v = fmaf(skip, x[i], y[i]);
+                    const float o = gated ? v * z[i] * sigmoid(z[i]) : v;
+                    if (is && l0 + i < end) put1(out + static_cast<int64_t>(l0 + i) * in.D_, o);
+                }
+            }
+        }
+    }
+    if (MODE & kOut)
+        for (int l = begin < end ? end : begin; l < stop; ++l)
+            if (is) put1(out + static_cast<int64_t>(l) * in.D_, 0.0f);
+    if (MODE & kEnds) {
+        const int64_t to = static_cast<int64_t>(b) * r.plan.segments + seg;
+        if (is) {
+#pragma unroll
+            for (int s = 0; s < SP; ++s)
+                if (s < in.S) r.ends[quad_at(to, in.S, in.D_, s / 4, d) + s % 4] = h[s];
+            r.steps[to * in.D_ + d] = total;
+        }
+    } else if (r.final_state && is && (end == len && (begin < len || seg == 0))) {
+#pragma unroll
+        for (int s = 0; s < SP; ++s)
+            if (s < in.S) r.final_state[(static_cast<int64_t>(b) * in.D_ + d) * in.S + s] = h[s];
+    }
+}
+
+// A thread has four states of a channel and goes from segment to segment.
+template <bool BACK>
+__global__ __launch_bounds__(256) void join_segments_kernel(ScanIn in, ScanPlan p, const float* __restrict__ state, float* __restrict__ ends,
+                                                            const float* __restrict__ steps) {
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t rest = id / in.D_;
+    const int d = static_cast<int>(id - rest * in.D_), q = static_cast<int>(rest % quads(in.S));
+    const int64_t b = rest / quads(in.S);
+    if (b >= in.B) return;
+    float A[4], h[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int s = 4 * q + j;
+        A[j] = s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s]) : 0.0f;
+        h[j] = state && s < in.S ? state[(b * in.D_ + d) * in.S + s] : 0.0f;
+    }
+    constexpr int U = 8;
+    for (int k0 = 0; k0 < p.segments; k0 += U) {
+        f32x4 e[U];
+        float t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k0 + u < p.segments ? k0 + u : p.segments - 1;
+            const int64_t seg = b * p.segments + (BACK ? p.segments - 1 - k : k);
+            e[u] = *reinterpret_cast<const f32x4*>(ends + quad_at(seg, in.S, in.D_, q, d));
+            t[u] = steps[seg * in.D_ + d];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k0 + u;
+            if (k < p.segments) {
+                const int64_t seg = b * p.segments + (BACK ? p.segments - 1 - k : k);
+                *reinterpret_cast<f32x4*>(ends + quad_at(seg, in.S, in.D_, q, d)) = f32x4{h[0], h[1], h[2], h[3]};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) h[j] = fmaf(exp2_fast(t[u] * A[j]), h[j], 4 * q + j < in.S ? e[u][j] : 0.0f);
+            }
+        }
+    }
+}
+
+// ---- one position ---------------------------------------------------------------------------------------------
+// A thread has four states of a channel and `many` streams one after the other, their states in flight together; LQ threads a
+// channel.  The states read and written are what bounds it.
+template <typename T, int LQ, int MANY, bool WHOLE>
+__global__ __launch_bounds__(256) void step_kernel(ScanIn in, float* __restrict__ state, T* __restrict__ out) {
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t ch = id / LQ, row = ch / in.D_;
+    const int q = threadIdx.x % LQ, d = static_cast<int>(ch - row * in.D_), s0 = 4 * q;
+    const int b0 = static_cast<int>(row) * MANY;
+    if (row * MANY >= in.B) return;  // whole groups of LQ threads leave together
+    const int group = d / (in.D_ / in.G);
+    const float skip = in.D ? in.D[d] : 0.0f, bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
+    float A[4], h[MANY][4];
+    T xr[MANY], tr[MANY], zr[MANY], Br[MANY][4], Cr[MANY][4];
+#pragma unroll
+    for (int m = 0; m < MANY; ++m) {
+        const int b = b0 + m < in.B ? b0 + m : in.B - 1;
+        const float* mine = state + (static_cast<int64_t>(b) * in.D_ + d) * in.S + s0;
+        if (WHOLE) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(mine);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) h[m][j] = v[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) h[m][j] = s0 + j < in.S ? mine[j] : 0.0f;
+        }
+        xr[m] = at<T>(in.x, b, 0)[d];
+        tr[m] = at<T>(in.dt, b, 0)[d];
+        if (in.z.data) zr[m] = at<T>(in.z, b, 0)[d];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int s = WHOLE || s0 + j < in.S ? s0 + j : 0;
+            Br[m][j] = (at<T>(in.Bm, b, 0) + group * in.b_group)[s];
+            Cr[m][j] = (at<T>(in.Cm, b, 0) + group * in.c_group)[s];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) A[j] = WHOLE || s0 + j < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s0 + j]) : 0.0f;
+#pragma unroll
+    for (int m = 0; m < MANY; ++m) {
+        const float step = softplus(widen(tr[m]) + bias).value, x = widen(xr[m]), put = step * x;
+        float y = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            h[m][j] = fmaf(exp2_fast(step * A[j]), h[m][j], put * widen(Br[m][j]));
+            y = WHOLE || s0 + j < in.S ? fmaf(h[m][j], widen(Cr[m][j]), y) : y;
+        }
+#pragma unroll
+        for (int k = 1; k < LQ; k *= 2) y += __shfl_xor(y, k);
+        y = fmaf(skip, x, y);
+        if (in.z.data) {
+            const float z = widen(zr[m]);
+            y = y * z * sigmoid(z);
+        }
+        if (b0 + m < in.B) {
+            float* mine = state + (static_cast<int64_t>(b0 + m) * in.D_ + d) * in.S + s0;
+            if (WHOLE) {
+                *reinterpret_cast<f32x4*>(mine) = f32x4{h[m][0], h[m][1], h[m][2], h[m][3]};
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (s0 + j < in.S) mine[j] = h[m][j];
+            }
+            if (q == 0) put1(out + static_cast<int64_t>(b0 + m) * in.D_ + d, y);
+        }
+    }
+}
+
+template <typename T, int LQ>
+hipError_t step_of(const ScanIn& in, float* state, void* out, hipStream_t st) {
+    // four streams a thread once that leaves 2048 workgroups
+    const bool many = static_cast<int64_t>(in.B) * in.D_ * LQ >= (int64_t{2048} * 256 * 4);
+    const int M = many ? 4 : 1;
+    const int64_t threads = static_cast<int64_t>((in.B + M - 1) / M) * in.D_ * LQ;
+    if (!fits((threads + 255) / 256, 256)) return hipErrorInvalidValue;
+    const bool whole = in.S == 4 * LQ && (reinterpret_cast<uintptr_t>(state) & 15) == 0;
+    const auto kernel = many ? (whole ? step_kernel<T, LQ, 4, true> : step_kernel<T, LQ, 4, false>)
+                             : (whole ? step_kernel<T, LQ, 1, true> : step_kernel<T, LQ, 1, false>);
+    kernel<<<static_cast<unsigned>((threads + 255) / 256), 256, 0, st>>>(in, state, static_cast<T*>(out));
+    return hipGetLastError();
+}
+
+// ---- launches -------------------------------------------------------------------------------------------------
+
+template <typename T, int SP, int MODE>
+void scan_launch(const ScanRun& r, hipStream_t st) {
+    const int64_t wgs = (static_cast<int64_t>(r.in.G) * r.plan.tiles + r.waves - 1) / r.waves;
+    scan_kernel<T, SP, MODE><<<static_cast<unsigned>(wgs * r.in.B * r.plan.segments), 64 * r.waves, sizeof(float) * r.waves * kP * 2 * SP, st>>>(r);
+}
+
+template <typename T, int SP>
+void scan_run(ScanRun& r, hipStream_t st) {
+    if (r.plan.segments > 1) {
+        scan_launch<T, SP, kEnds>(r, st);
+        (void)launch_join_segments(r.in, r.plan, r.state, r.ends, r.steps, false, st);
+    }
+    if (!r.out) scan_launch<T, SP, kSave>(r, st);
+    else if (r.saved) scan_launch<T, SP, kOut | kSave>(r, st);
+    else scan_launch<T, SP, kOut>(r, st);
+}
+
+template <typename T>
+void scan_of(ScanRun& r, hipStream_t st) {
+    if (r.in.S <= 4) scan_run<T, 4>(r, st);
+    else if (r.in.S <= 8) scan_run<T, 8>(r, st);
+    else if (r.in.S <= 16) scan_run<T, 16>(r, st);
+    else if (r.in.S <= 32) scan_run<T, 32>(r, st);
+    else scan_run<T, 64>(r, st);
+}
+
+size_t ends_bytes(const ScanPlan& p, int B, int D, int S) {
+    return up256(static_cast<size_t>(B) * p.segments * quads(S) * D * 16);
+}
+
+}  // namespace
+
+hipError_t launch_join_segments(const ScanIn& in, const ScanPlan& p, const float* state, float* ends, const float* steps, bool back, hipStream_t st) {
+    const int64_t threads = static_cast<int64_t>(in.B) * in.D_ * quads(in.S);
+    const unsigned blocks = static_cast<unsigned>((threads + 255) / 256);
+    if (back) join_segments_kernel<true><<<blocks, 256, 0, st>>>(in, p, state, ends, steps);
+    else join_segments_kernel<false><<<blocks, 256, 0, st>>>(in, p, state, ends, steps);
+    return hipGetLastError();
+}
+
+size_t scan_saved_bytes(int B, int N, int D, int S) { return up256(static_cast<size_t>(B) * scan_blocks(N) * quads(S) * D * 16); }
+
+size_t scan_workspace(int B, int N, int D, int S, int G) {
+    const ScanPlan p = scan_plan(B, N, D, G, 1);
+    if (p.segments == 1) return 256;
+    return ends_bytes(p, B, D, S) + up256(static_cast<size_t>(B) * p.segments * D * 4);
+}
+
+hipError_t run_state_scan(int dtype, const ScanIn& in, const float* state, void* out, float* final_state, float* saved, void* ws, hipStream_t st) {
+    ScanRun r{in, state, out, final_state, saved, nullptr, nullptr, scan_plan(in.B, in.N, in.D_, in.G, 1), 0};
+    if (!scan_fits(in.B, in.N, in.D_, in.S, in.G, r.plan)) return hipErrorInvalidValue;
+    if (r.plan.segments > 1) {
+        r.ends = static_cast<float*>(ws);
+        r.steps = reinterpret_cast<float*>(static_cast<char*>(ws) + ends_bytes(r.plan, in.B, in.D_, in.S));
+    }
+    const int all = in.G * r.plan.tiles;
+    r.waves = all < 4 ? all : 4;
+    if (dtype) scan_of<uint16_t>(r, st);
+    else scan_of<float>(r, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_state_scan(int dtype, const ScanIn& in, const float* state, void* out, float* final_state, void* saved, void* ws, hipStream_t st) {
+    return run_state_scan(dtype, in, state, out, final_state, static_cast<float*>(saved), ws, st);
+}
+
+hipError_t launch_state_step(int dtype, const ScanIn& in, float* state, void* out, hipStream_t st) {
+    const int n = quads(in.S);
+#define LCCRF_STEP(LQ) (dtype ? step_of<uint16_t, LQ>(in, state, out, st) : step_of<float, LQ>(in, state, out, st))
+    return n <= 1 ? LCCRF_STEP(1) : n <= 2 ? LCCRF_STEP(2) : n <= 4 ? LCCRF_STEP(4) : n <= 8 ? LCCRF_STEP(8) : LCCRF_STEP(16);
+#undef LCCRF_STEP
+}
+
+}  // namespace enc
+}  // namespace lccrf

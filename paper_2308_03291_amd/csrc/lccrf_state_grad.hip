@@ -1,0 +1,497 @@
+// Gradient of the selective state space scan.
+//
+// With dh[l] = dy[l] Cm[l] + a[l+1] dh[l+1] running backwards,
+//     dCm = sum_channels dy h,   dBm = sum_channels dh put,   dput = sum_s dh Bm,   back = dh a h[l-1]  (by the decay's logarithm),
+//     dx = dput step + D dy,     dv = (dput x + sum_s back A) sigmoid(v),    dA = sum_positions back step.
+// The states in front of every eighth position are saved by the forward pass; eight positions are run again from there, the products
+// p = a h[l-1] kept in registers (h = p + put Bm follows from them by one multiply-add; p from h would lose what a
+// small decay leaves), and then gone through backwards.  About 22 issue slots an update with 16 states: vector arithmetic bounds it.
+//
+// A wave has 64 channels and up to 16 states; more states are shared by several waves, whose sums over the states meet in LDS.
+// The sums over the channels are taken by halving: two registers and two halves of the wave become one register whose
+// halves hold one sum each (a swap and an addition), and so on, 70 instructions for the 32 sums of a position; the waves of a
+// workgroup meet in LDS, workgroups through memory, always in the same order.
+#include "lccrf_state.h"
+
+namespace lccrf {
+namespace enc {
+namespace {
+
+struct GradPlan {
+    ScanPlan scan;
+    int state_waves;  // waves that share a channel's states
+    int tile_waves;   // tiles of 64 channels a workgroup
+    int parts;        // workgroups a group's channels are spread over
+};
+
+GradPlan grad_plan(int B, int N, int D, int S, int G) {
+    GradPlan p;
+    p.state_waves = (S + 15) / 16;
+    p.scan = scan_plan(B, N, D, G, p.state_waves);
+    p.tile_waves = 4 / p.state_waves;
+    if (p.tile_waves > p.scan.tiles) p.tile_waves = p.scan.tiles;
+    p.parts = (p.scan.tiles + p.tile_waves - 1) / p.tile_waves;
+    return p;
+}
+
+struct GradRun {
+    ScanIn in;
+    AnyRows dout;
+    ScanGrads g;
+    const float* saved;
+    float* ends;     // segments > 1: the gradient by the state behind every segment
+    float* steps;
+    float* part_bc;  // parts > 1: [parts][2][B][N][G][S]
+    float* part_a;   // [B * segments][D][S]
+    float* part_d;   // [B * segments * state_waves][2][D]: dD, ddt_bias
+    GradPlan plan;
+};
+
+template <int CTRL> __device__ __forceinline__ float from_lane(float x) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kRor8 = 0x128;
+
+// Two sums in one register: lanes with the bit clear go on with x, the others with y.
+template <int CTRL> __device__ __forceinline__ float halve(float x, float y, bool bit) {
+    return (bit ? y : x) + from_lane<CTRL>(bit ? x : y);
+}
+// Sums over the 64 lanes of v[0 .. NV); lane k gets sum k / (64 / NV).
+template <int NV> __device__ __forceinline__ float lane_sums(float (&v)[NV], int lane) {
+    static_assert(NV == 8 || NV == 16 || NV == 32, "");
+#pragma unroll
+    for (int i = 0; i < NV / 2; ++i) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + NV / 2]), false, false);
+        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+#pragma unroll
+    for (int i = 0; i < NV / 4; ++i) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + NV / 4]), false, false);
+        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+#pragma unroll
+    for (int i = 0; i < NV / 8; ++i) v[i] = halve<kRor8>(v[i], v[i + NV / 8], lane & 8);
+    if constexpr (NV >= 16) {
+#pragma unroll
+        for (int i = 0; i < NV / 16; ++i) v[i] = halve<kHalfMirror>(v[i], v[i + NV / 16], lane & 4);
+    } else {
+        v[0] += from_lane<kHalfMirror>(v[0]);
+    }
+    if constexpr (NV >= 32) v[0] = halve<kXor2>(v[0], v[1], lane & 2);
+    else v[0] += from_lane<kXor2>(v[0]);
+    return v[0] + from_lane<kXor1>(v[0]);
+}
+
+// dy of a position: the gradient by y.
+__device__ __forceinline__ float through_gate(float dout, float z, bool gated) { return gated ? dout * z * sigmoid(z) : dout; }
+
+// What a segment makes of 0 behind it, and the sum of its steps.
+template <typename T, int SP>
+__global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
+    extern __shared__ float lds[];  // [waves][kP][2 * SP]
+    const ScanIn& in = r.in;
+    const ScanPlan& plan = r.plan.scan;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int tiles = in.G * plan.tiles, groups_of_tiles = (tiles + waves - 1) / waves;
+    const unsigned which = blockIdx.x / groups_of_tiles;
+    const int tile = (blockIdx.x - which * groups_of_tiles) * waves + wave;
+    const int b = which / plan.segments, seg = which - b * plan.segments;
+    if (tile >= tiles) return;
+    const int width = in.D_ / in.G, group = tile / plan.tiles, c0 = (tile - group * plan.tiles) * 64 + lane;
+    const bool is = c0 < width;
+    const int d = group * width + (is ? c0 : width - 1);
+    const int len = clamp_length(in.lengths, b, in.N), begin = seg * plan.seg_len;
+    const int stop = begin + plan.seg_len < in.N ? begin + plan.seg_len : in.N, end = stop < len ? stop : len;
+    float* bc = lds + wave * (kP * 2 * SP);
+    const bool gated = in.z.data != nullptr;
+    const float bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
+    float dh[SP], A[SP], total = 0.0f;
+#pragma unroll
+    for (int s = 0; s < SP; ++s) {
+        A[s] = s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s]) : 0.0f;
+        dh[s] = 0.0f;
+    }
+    if (begin < end) {
+        T tr[kP], zr[kP], dr[kP];
+        GroupVectors<T, SP> gv;
+        const auto fetch = [&](int l0) {
+            gv.load(in, b, l0, len, group, 0, lane);
+#pragma unroll
+            for (int i = 0; i < kP; ++i) {
+                const int l = l0 + i < len ? l0 + i : len - 1;
+                tr[i] = at<T>(in.dt, b, l)[d];
+                dr[i] = at<T>(r.dout, b, l)[d];
+                if (gated) zr[i] = at<T>(in.z, b, l)[d];
+            }
+        };
+        const int last = begin + (end - begin - 1) / kP * kP;
+        fetch(last);
+        for (int l0 = last; l0 >= begin; l0 -= kP) {
+            float step[kP], dy[kP];
+#pragma unroll
+            for (int i = 0; i < kP; ++i) {
+                const bool on = l0 + i < end;
+                step[i] = on ? softplus(widen(tr[i]) + bias).value : 0.0f;
+                dy[i] = on ? through_gate(widen(dr[i]), gated ? widen(zr[i]) : 0.0f, gated) : 0.0f;
+                total += step[i];
+            }
+            wave_sync();
+            gv.put(bc, in, l0, len, 0, lane);
+            wave_sync();
+            if (l0 > begin) fetch(l0 - kP);
+#pragma unroll
+            for (int i = kP - 1; i >= 0; --i) {
+                const f32x4* C4 = reinterpret_cast<const f32x4*>(bc + i * 2 * SP + SP);
+#pragma unroll
+                for (int q = 0; q < SP / 4; ++q) {
+                    const f32x4 Cq = C4[q];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) dh[4 * q + j] = exp2_fast(step[i] * A[4 * q + j]) * fmaf(dy[i], Cq[j], dh[4 * q + j]);
+                }
+            }
+        }
+    }
+    const int64_t to = static_cast<int64_t>(b) * plan.segments + seg;
+    if (is) {
+#pragma unroll
+        for (int s = 0; s < SP; ++s)
+            if (s < in.S) r.ends[quad_at(to, in.S, in.D_, s / 4, d) + s % 4] = dh[s];
+        r.steps[to * in.D_ + d] = total;
+    }
+}
+
+// Values of a channel and position that both directions need, in LDS: [kScal][kP][64] a wave (four waves take 78 KB in all, so
+// that two workgroups fit a compute unit).
+enum { kStep, kDy, kX, kSlope, kDz, kScal };
+
+template <typename T, int SP>
+__global__ __launch_bounds__(256, 2) void scan_grad_kernel(GradRun r) {
+    extern __shared__ float lds[];
+    const ScanIn& in = r.in;
+    const ScanPlan& plan = r.plan.scan;
+    const int SW = r.plan.state_waves, CT = r.plan.tile_waves, waves = SW * CT;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int sw = wave % SW, ct = wave / SW, s0 = sw * SP;
+    unsigned which = blockIdx.x / r.plan.parts;
+    const int part = blockIdx.x - which * r.plan.parts;
+    const unsigned bs = which / in.G;
+    const int group = which - bs * in.G;
+    const int b = bs / plan.segments, seg = bs - b * plan.segments;
+    const int tile = part * CT + ct, width = in.D_ / in.G, c0 = tile * 64 + lane;
+    const bool is = c0 < width;  // (a whole wave may have no channel: it keeps the workgroup company)
+    const int d = group * width + (is ? c0 : width - 1);
+    const int len = clamp_length(in.lengths, b, in.N), begin = seg * plan.seg_len;
+    const int stop = begin + plan.seg_len < in.N ? begin + plan.seg_len : in.N, end = stop < len ? stop : len;
+
+    float* bc = lds + wave * (kP * 2 * SP);                                  // [waves][kP][2 * SP]
+    float* scal = lds + waves * (kP * 2 * SP) + wave * (kScal * kP * 64);    // [waves][kScal][kP][64]
+    float* sums = lds + waves * (kP * 2 * SP + kScal * kP * 64);             // [waves][3][kP][64]: y, dput, sum back A
+    float* red = sums + waves * (3 * kP * 64);                               // [2][waves][kP][2 * SP]
+    float* my_sums = sums + wave * (3 * kP * 64);
+
+    const bool gated = in.z.data != nullptr;
+    const float skip = in.D ? in.D[d] : 0.0f, bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
+    const int64_t row = static_cast<int64_t>(b) * in.N;
+    T* dx = static_cast<T*>(r.g.dx) + row * in.D_ + d;
+    T* ddt = static_cast<T*>(r.g.ddt) + row * in.D_ + d;
+    T* dz = gated ? static_cast<T*>(r.g.dz) + row * in.D_ + d : nullptr;
+
+    float dh[SP], A[SP], dA[SP], sum_dD = 0.0f, sum_dv = 0.0f;
+#pragma unroll
+    for (int s = 0; s < SP; ++s) {
+        A[s] = s0 + s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s0 + s]) : 0.0f;
+        dh[s] = 0.0f;
+        dA[s] = 0.0f;
+    }
+    if (plan.segments > 1 && is) {
+        const int64_t from = static_cast<int64_t>(b) * plan.segments + seg;
+#pragma unroll
+        for (int s = 0; s < SP; ++s)
+            if (s0 + s < in.S) dh[s] = r.ends[quad_at(from, in.S, in.D_, (s0 + s) / 4, d) + s % 4];
+    }
+
+    if (begin < end) {
+        T xr[kP], tr[kP], zr[kP], dr[kP];
+        GroupVectors<T, SP> gv;
+        const auto fetch = [&](int l0) {
+            gv.load(in, b, l0, len, group, s0, lane);
+#pragma unroll
+            for (int i = 0; i < kP; ++i) {
+                const int l = l0 + i < len ? l0 + i : len - 1;
+                xr[i] = at<T>(in.x, b, l)[d];
+                tr[i] = at<T>(in.dt, b, l)[d];
+                dr[i] = at<T>(r.dout, b, l)[d];
+                if (gated) zr[i] = at<T>(in.z, b, l)[d];
+            }
+        };
+        const int last = begin + (end - begin - 1) / kP * kP;
+        int turn = 0;
+        fetch(last);
+        for (int l0 = last; l0 >= begin; l0 -= kP, turn ^= 1) {
+            float h[SP], p[kP][SP];
+            const int64_t block = static_cast<int64_t>(b) * ((in.N + kP - 1) / kP) + l0 / kP;
+#pragma unroll
+            for (int q = 0; q < SP / 4; ++q) {
+                f32x4 v = {};
+                if (is && s0 + 4 * q < in.S) v = *reinterpret_cast<const f32x4*>(r.saved + quad_at(block, in.S, in.D_, s0 / 4 + q, d));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) h[4 * q + j] = v[j];
+            }
+#pragma unroll
+            for (int i = 0; i < kP; ++i) {
+                const bool on = is && l0 + i < end;
+                const Softplus sp = softplus(widen(tr[i]) + bias);
+                const float x = widen(xr[i]), dout = widen(dr[i]), z = gated ? widen(zr[i]) : 0.0f, gate = sigmoid(z);
+                float* to = scal + i * 64 + lane;
+                to[kStep * kP * 64] = on ? sp.value : 0.0f;
+                to[kDy * kP * 64] = on ? (gated ? dout * z * gate : dout) : 0.0f;
+                to[kX * kP * 64] = on ? x : 0.0f;
+                to[kSlope * kP * 64] = sp.slope;
+                to[kDz * kP * 64] = dout * gate * fmaf(z, 1.0f - gate, 1.0f);
+            }
+            gv.put(bc, in, l0, len, s0, lane);
+            wave_sync();
+            // forwards
+#pragma unroll
+            for (int i = 0; i < kP; ++i) {
+                const f32x4* B4 = reinterpret_cast<const f32x4*>(bc + i * 2 * SP);
+                const float step = scal[(kStep * kP + i) * 64 + lane], put = step * scal[(kX * kP + i) * 64 + lane];
+                float y0 = 0.0f, y1 = 0.0f;
+#pragma unroll
+                for (int q = 0; q < SP / 4; ++q) {
+                    const f32x4 Bq = B4[q], Cq = B4[SP / 4 + q];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int s = 4 * q + j;
+                        p[i][s] = exp2_fast(step * A[s]) * h[s];
+                        h[s] = fmaf(put, Bq[j], p[i][s]);
+                        if (j & 1) y1 = fmaf(h[s], Cq[j], y1);
+                        else y0 = fmaf(h[s], Cq[j], y0);
+                    }
+                }
+                my_sums[i * 64 + lane] = y0 + y1;
+            }
+            // backwards
+#pragma unroll
+            for (int i = kP - 1; i >= 0; --i) {
+                const f32x4* B4 = reinterpret_cast<const f32x4*>(bc + i * 2 * SP);
+                const float step = scal[(kStep * kP + i) * 64 + lane], put = step * scal[(kX * kP + i) * 64 + lane], dy = scal[(kDy * kP + i) * 64 + lane];
+                float v[2 * SP], dput0 = 0.0f, dput1 = 0.0f, back0 = 0.0f, back1 = 0.0f;
+#pragma unroll
+                for (int q = 0; q < SP / 4; ++q) {
+                    const f32x4 Bq = B4[q], Cq = B4[SP / 4 + q];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int s = 4 * q + j;
+                        const float e = fmaf(dy, Cq[j], dh[s]);
+                        v[s] = e * put;
+                        v[SP + s] = dy * fmaf(put, Bq[j], p[i][s]);
+                        const float back = e * p[i][s];
+                        if (j & 1) {
+                            dput1 = fmaf(e, Bq[j], dput1);
+                            back1 = fmaf(back, A[s], back1);
+                        } else {
+                            dput0 = fmaf(e, Bq[j], dput0);
+                            back0 = fmaf(back, A[s], back0);
+                        }
+                        dA[s] = fmaf(back, step, dA[s]);
+                        dh[s] = e * exp2_fast(step * A[s]);
+                    }
+                }
+                my_sums[(kP + i) * 64 + lane] = dput0 + dput1;
+                my_sums[(2 * kP + i) * 64 + lane] = (back0 + back1) * kLn2f;
+                const float sum = lane_sums<2 * SP>(v, lane);
+                if (lane % (32 / SP) == 0) red[((turn * waves + wave) * kP + i) * (2 * SP) + lane / (32 / SP)] = sum;
+            }
+            __syncthreads();
+            if (l0 > begin) fetch(l0 - kP);
+            // The waves of a tile share its positions.
+            for (int i = sw; i < kP && l0 + i < end; i += SW) {
+                float y = 0.0f, dput = 0.0f, back = 0.0f;
+                for (int k = 0; k < SW; ++k) {
+                    const float* from = sums + (ct * SW + k) * (3 * kP * 64) + lane;
+                    y += from[i * 64];
+                    dput += from[(kP + i) * 64];
+                    back += from[(2 * kP + i) * 64];
+                }
+                const float* own = scal + i * 64 + lane;
+                const float step = own[kStep * kP * 64], dy = own[kDy * kP * 64], x = own[kX * kP * 64];
+                const float dv = fmaf(dput, x, back) * own[kSlope * kP * 64];
+                sum_dv += dv;
+                sum_dD = fmaf(dy, x, sum_dD);
+                if (is) {
+                    const int64_t to = static_cast<int64_t>(l0 + i) * in.D_;
+                    put1(dx + to, fmaf(dput, step, skip * dy));
+                    put1(ddt + to, dv);
+                    if (gated) put1(dz + to, own[kDz * kP * 64] * fmaf(skip, x, y));
+                }
+            }
+            for (int k = threadIdx.x; k < kP * SW * 2 * SP; k += blockDim.x) {
+                const int i = k / (SW * 2 * SP), c = k / (SW * SP) & 1, s = k % (SW * SP);
+                if (l0 + i < end && s < in.S) {
+                    float sum = 0.0f;
+                    for (int t = 0; t < CT; ++t) sum += red[((turn * waves + t * SW + s / SP) * kP + i) * (2 * SP) + c * SP + s % SP];
+                    const int64_t to = ((row + l0 + i) * in.G + group) * in.S + s;
+                    if (r.plan.parts == 1) put1(static_cast<T*>(c ? r.g.dCm : r.g.dBm) + to, sum);
+                    else r.part_bc[(static_cast<int64_t>(part) * 2 + c) * in.B * in.N * in.G * in.S + to] = sum;
+                }
+            }
+            if (SW > 1) __syncthreads();  // `sums` is used again
+            else wave_sync();
+        }
+    }
+    // Positions past the end.
+    for (int l = begin < end ? end : begin; l < stop; ++l) {
+        const int64_t to = static_cast<int64_t>(l) * in.D_;
+        if (is && sw == 0) {
+            put1(dx + to, 0.0f);
+            put1(ddt + to, 0.0f);
+            if (gated) put1(dz + to, 0.0f);
+        }
+        if (r.plan.parts == 1)
+            for (int s = threadIdx.x; s < in.S; s += blockDim.x) {
+                put1(static_cast<T*>(r.g.dBm) + ((row + l) * in.G + group) * in.S + s, 0.0f);
+                put1(static_cast<T*>(r.g.dCm) + ((row + l) * in.G + group) * in.S + s, 0.0f);
+            }
+    }
+    if (is) {
+#pragma unroll
+        for (int s = 0; s < SP; ++s)
+            if (s0 + s < in.S) r.part_a[(static_cast<int64_t>(bs) * in.D_ + d) * in.S + s0 + s] = dA[s];
+        float* pd = r.part_d + (static_cast<int64_t>(bs) * SW + sw) * 2 * in.D_ + d;
+        pd[0] = sum_dD;
+        pd[in.D_] = sum_dv;
+        if (r.g.dstate && seg == 0) {
+#pragma unroll
+            for (int s = 0; s < SP; ++s)
+                if (s0 + s < in.S) r.g.dstate[(static_cast<int64_t>(b) * in.D_ + d) * in.S + s0 + s] = dh[s];
+        }
+    }
+}
+
+// dBm and dCm from the workgroups that share a group; 0 past the end.
+template <typename T>
+__global__ __launch_bounds__(256) void group_sums_kernel(GradRun r) {
+    const ScanIn& in = r.in;
+    const int64_t all = static_cast<int64_t>(in.B) * in.N * in.G * in.S, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (id >= all) return;
+    const int64_t pos = id / (in.G * in.S);
+    const int b = static_cast<int>(pos / in.N), l = static_cast<int>(pos - static_cast<int64_t>(b) * in.N);
+    float sB = 0.0f, sC = 0.0f;
+    if (l < clamp_length(in.lengths, b, in.N))
+        for (int p = 0; p < r.plan.parts; ++p) {
+            sB += r.part_bc[2 * p * all + id];
+            sC += r.part_bc[(2 * p + 1) * all + id];
+        }
+    put1(static_cast<T*>(r.g.dBm) + id, sB);
+    put1(static_cast<T*>(r.g.dCm) + id, sC);
+}
+
+// dA, dD and ddt_bias: columns summed over their rows, sixteen threads a column.
+__global__ __launch_bounds__(1024) void column_sums_kernel(GradRun r, int a_blocks) {
+    __shared__ float sums[16][64];
+    const ScanIn& in = r.in;
+    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    const bool isA = static_cast<int>(blockIdx.x) < a_blocks;
+    const int64_t columns = isA ? static_cast<int64_t>(in.D_) * in.S : 2 * static_cast<int64_t>(in.D_);
+    const int64_t col = static_cast<int64_t>(isA ? blockIdx.x : blockIdx.x - a_blocks) * 64 + x;
+    const int rows = in.B * r.plan.scan.segments * (isA ? 1 : r.plan.state_waves);
+    const float* from = isA ? r.part_a : r.part_d;
+    float sum = 0.0f;
+    if (col < columns) {
+#pragma unroll 4
+        for (int k = y; k < rows; k += 16) sum += from[k * columns + col];
+    }
+    sums[y][x] = sum;
+    __syncthreads();
+    if (y == 0 && col < columns) {
+        for (int i = 1; i < 16; ++i) sum += sums[i][x];
+        if (isA) r.g.dA[col] = sum;
+        else if (col < in.D_) { if (r.g.dD) r.g.dD[col] = sum; }
+        else if (r.g.ddt_bias) r.g.ddt_bias[col - in.D_] = sum;
+    }
+}
+
+struct Carve {
+    size_t saved, scan, ends, steps, bc, a, d, total;
+};
+Carve carve(int B, int N, int D, int S, int G, bool with_saved) {
+    const GradPlan p = grad_plan(B, N, D, S, G);
+    const size_t rows = static_cast<size_t>(B) * p.scan.segments;
+    Carve c;
+    size_t off = 0;
+    c.saved = off; off += with_saved ? 0 : scan_saved_bytes(B, N, D, S);
+    c.scan = off; off += with_saved ? 0 : scan_workspace(B, N, D, S, G);
+    c.ends = off; off += p.scan.segments > 1 ? up256(rows * quads(S) * D * 16) : 0;
+    c.steps = off; off += p.scan.segments > 1 ? up256(rows * D * 4) : 0;
+    c.bc = off; off += p.parts > 1 ? up256(static_cast<size_t>(p.parts) * 2 * B * N * G * S * 4) : 0;
+    c.a = off; off += up256(rows * D * S * 4);
+    c.d = off; off += up256(rows * p.state_waves * 2 * D * 4);
+    c.total = off;
+    return c;
+}
+
+template <typename T, int SP>
+void back_ends(const GradRun& r, hipStream_t st) {
+    const int64_t tiles = static_cast<int64_t>(r.in.G) * r.plan.scan.tiles, waves = tiles < 4 ? tiles : 4;
+    const int64_t blocks = (tiles + waves - 1) / waves * r.in.B * r.plan.scan.segments;
+    back_ends_kernel<T, SP><<<static_cast<unsigned>(blocks), 64 * waves, sizeof(float) * waves * kP * 2 * SP, st>>>(r);
+}
+
+template <typename T, int SP>
+hipError_t grad_main(const GradRun& r, hipStream_t st) {
+    const int waves = r.plan.state_waves * r.plan.tile_waves;
+    const size_t bytes = sizeof(float) * waves * (kP * 2 * SP + (kScal + 3) * kP * 64 + 2 * kP * 2 * SP);
+    const int64_t blocks = static_cast<int64_t>(r.in.B) * r.plan.scan.segments * r.in.G * r.plan.parts;
+    const auto kernel = scan_grad_kernel<T, SP>;
+    // more than 64 KB of LDS has to be asked for
+    if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)); e != hipSuccess)
+        return e;
+    kernel<<<static_cast<unsigned>(blocks), 64 * waves, bytes, st>>>(r);
+    return hipSuccess;
+}
+
+template <typename T>
+hipError_t grad_of(const GradRun& r, hipStream_t st) {
+    const int S = r.in.S;
+    if (r.plan.scan.segments > 1) {
+        if (S <= 4) back_ends<T, 4>(r, st);
+        else if (S <= 8) back_ends<T, 8>(r, st);
+        else if (S <= 16) back_ends<T, 16>(r, st);
+        else if (S <= 32) back_ends<T, 32>(r, st);
+        else back_ends<T, 64>(r, st);
+        (void)launch_join_segments(r.in, r.plan.scan, nullptr, r.ends, r.steps, true, st);
+    }
+    const hipError_t e = S <= 4 ? grad_main<T, 4>(r, st) : S <= 8 ? grad_main<T, 8>(r, st) : grad_main<T, 16>(r, st);
+    if (e != hipSuccess) return e;
+    if (r.plan.parts > 1) {
+        const int64_t all = static_cast<int64_t>(r.in.B) * r.in.N * r.in.G * S;
+        group_sums_kernel<T><<<static_cast<unsigned>((all + 255) / 256), 256, 0, st>>>(r);
+    }
+    const int a_blocks = static_cast<int>((static_cast<int64_t>(r.in.D_) * S + 63) / 64);
+    column_sums_kernel<<<a_blocks + (2 * r.in.D_ + 63) / 64, 1024, 0, st>>>(r, a_blocks);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t scan_grad_workspace(int B, int N, int D, int S, int G, bool with_saved) { return carve(B, N, D, S, G, with_saved).total; }
+
+hipError_t launch_state_scan_grad(int dtype, AnyRows dout, const ScanIn& in, const float* state, const void* saved, const ScanGrads& g, void* ws,
+                                  hipStream_t st) {
+    const Carve c = carve(in.B, in.N, in.D_, in.S, in.G, saved != nullptr);
+    char* base = static_cast<char*>(ws);
+    const auto floats = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
+    if (!scan_fits(in.B, in.N, in.D_, in.S, in.G, grad_plan(in.B, in.N, in.D_, in.S, in.G).scan)) return hipErrorInvalidValue;
+    if (!saved) {
+        const hipError_t e = run_state_scan(dtype, in, state, nullptr, nullptr, floats(c.saved), base + c.scan, st);
+        if (e != hipSuccess) return e;
+        saved = floats(c.saved);
+    }
+    const GradRun r{in, dout, g, static_cast<const float*>(saved), floats(c.ends), floats(c.steps), floats(c.bc), floats(c.a), floats(c.d),
+                    grad_plan(in.B, in.N, in.D_, in.S, in.G)};
+    return dtype ? grad_of<uint16_t>(r, st) : grad_of<float>(r, st);
+}
+
+}  // namespace enc
+}  // namespace lccrf
