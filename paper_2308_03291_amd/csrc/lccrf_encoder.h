@@ -85,26 +85,19 @@ template <int W, bool SMALL> __device__ __forceinline__ int piece_start(int piec
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// exp(x) with the rounding of x * log2(e) taken back: at |x| = 16 the plain product is off by 2^-20 of the result.
-__device__ __forceinline__ float exp_near(float x) {
-    const float t = x * kLog2e;
-    const float rest = fmaf(x, 1.92596299112661746887e-8f, fmaf(x, kLog2e, -t));  // log2(e) = kLog2e + 1.9e-8
-    const float e = exp2_fast(t);
-    return fmaf(e, rest * kLn2f, e);
-}
-
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exp2_fast(-x * kLog2e)); }
 
 // log(1 + exp(v)) and its derivative.  With e = exp(-|v|): max(v, 0) + log1p(e), and log1p(e) = e (1 + e q(e)) with q of degree 8
 // fitted to it on [0, 1] (off by at most 1.4 units in the last place): a logarithm of 1 + e would lose the steps near 0.001 that
-// such scans live on.  exp(-inf) = 0 gives 0 and inf at the ends; a NaN stays one.
+// such scans live on.  e is exp2(t), t = -|v| log2(e) rounded, times 1 + (-|v| - t ln2): the rounding of t alone would cost 2^-20
+// at |v| = 16.  exp(-126) is 0 in float already, so -|v| may stop there; a NaN stays one.
 struct Softplus { float value, slope; };
 __device__ __forceinline__ Softplus softplus(float v) {
-    const float a = -fabsf(v);
+    const float a = fmaxf(-fabsf(v), -126.0f);
     const float t = a * kLog2e;
+    const float rest = fmaf(t, 1.9046542999577680e-9f, fmaf(t, -0.693147182464599609375f, a));  // ln2 in two parts
     float e = exp2_fast(t);
-    const float rest = a > -126.0f ? fmaf(a, 1.92596299112661746887e-8f, fmaf(a, kLog2e, -t)) : 0.0f;
-    e = fmaf(e, rest * kLn2f, e);
+    e = fmaf(e, rest, e);
     float q = -0.004579766187816858f;
     q = fmaf(q, e, 0.025682786479592323f);
     q = fmaf(q, e, -0.06751181185245514f);
@@ -115,8 +108,8 @@ __device__ __forceinline__ Softplus softplus(float v) {
     q = fmaf(q, e, 0.3333289325237274f);
     q = fmaf(q, e, -0.49999997f);
     q = fmaf(q, e, 1.0f);
-    const float r = __builtin_amdgcn_rcpf(1.0f + e);
-    return {fmaf(q, e, v > 0.0f ? v : (v < 0.0f ? 0.0f : v)), v >= 0.0f ? r : e * r};
+    const float value = fmaf(q, e, fmaxf(v, 0.0f)), r = __builtin_amdgcn_rcpf(1.0f + e);
+    return {v == v ? value : v, v >= 0.0f ? r : e * r};
 }
 
 // Rows of an input: element strides between sequences and positions.

@@ -34,6 +34,40 @@ template <typename T> __device__ __forceinline__ const T* at(const AnyRows& r, i
     return static_cast<const T*>(r.data) + b * r.batch + l * r.row;
 }
 
+// Channel d of P rows from l0 on, `stride` apart; those past the end take the place of one before it.
+template <typename T, int P> __device__ __forceinline__ void load_rows(const AnyRows& r, int b, int l0, int stride, int len, int d, T (&v)[P]) {
+    const T* p = at<T>(r, b, l0 < len ? l0 : len - 1);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        v[i] = p[d];
+        l0 += stride;
+        p += l0 < len ? stride * r.row : 0;
+    }
+}
+
+// The sequence with rank k among the lengths, the longest first (equal ones in their order).  Waves of long sequences that start
+// last are what a launch waits for; where the lengths are given and a wave can look through them quickly, the
+// order of work follows them.
+constexpr int kMaxRanked = 256;
+__device__ __forceinline__ int ranked(const int32_t* lengths, int B, int N, int k, int lane) {
+    if (!lengths || B > kMaxRanked) return k;
+    int len[kMaxRanked / 64], rank[kMaxRanked / 64] = {};
+#pragma unroll
+    for (int c = 0; c < kMaxRanked / 64; ++c) len[c] = c * 64 + lane < B ? clamp_length(lengths, c * 64 + lane, N) : -1;
+    for (int j = 0; j < B; ++j) {
+        const int other = clamp_length(lengths, j, N);
+#pragma unroll
+        for (int c = 0; c < kMaxRanked / 64; ++c) rank[c] += other > len[c] || (other == len[c] && j < c * 64 + lane);
+    }
+    int b = 0;
+#pragma unroll
+    for (int c = 0; c < kMaxRanked / 64; ++c) {
+        const uint64_t hit = __ballot(rank[c] == k && c * 64 + lane < B);
+        if (hit) b = c * 64 + __builtin_ctzll(hit);
+    }
+    return b;
+}
+
 __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();

@@ -68,14 +68,9 @@ __global__ __launch_bounds__(256, SP <= 16 ? 3 : 2) void scan_kernel(ScanRun r) 
         GroupVectors<T, SP> gv;
         const auto fetch = [&](int l0) {
             gv.load(in, b, l0, len, group, 0, lane);
-#pragma unroll
-            for (int i = 0; i < kP; ++i) {
-                const int l = l0 + i < len ? l0 + i : len - 1;
-                xr[i] = at<T>(in.x, b, l)[d];
-                tr[i] = at<T>(in.dt, b, l)[d];
-                if (MODE & kOut)
-                    if (gated) zr[i] = at<T>(in.z, b, l)[d];
-            }
+            load_rows<T, kP>(in.x, b, l0, 1, len, d, xr);
+            load_rows<T, kP>(in.dt, b, l0, 1, len, d, tr);
+            if ((MODE & kOut) && gated) load_rows<T, kP>(in.z, b, l0, 1, len, d, zr);
         };
         fetch(begin);
         for (int l0 = begin; l0 < end; l0 += kP) {

@@ -7,9 +7,11 @@
 // p = a h[l-1] kept in registers (h = p + put Bm follows from them by one multiply-add; p from h would lose what a
 // small decay leaves), and then gone through backwards.  About 22 issue slots an update with 16 states: vector arithmetic bounds it.
 //
-// A wave has 64 channels and up to 16 states; more states are shared by several waves, whose sums over the states meet in LDS.
+// A wave has 64 channels and up to 8 states (64 registers of products; with 16 states a wave the registers that remain hold
+// neither the next positions' inputs nor a second and third wave's work, and it took three times as long); more states are shared by
+// several waves of a workgroup, which also share what is computed once a channel, and whose sums over the states meet in LDS.
 // The sums over the channels are taken by halving: two registers and two halves of the wave become one register whose
-// halves hold one sum each (a swap and an addition), and so on, 70 instructions for the 32 sums of a position; the waves of a
+// halves hold one sum each (a swap and an addition), and so on, 35 instructions for the 16 sums of a position; the waves of a
 // workgroup meet in LDS, workgroups through memory, always in the same order.
 #include "lccrf_state.h"
 
@@ -19,16 +21,16 @@ namespace {
 
 struct GradPlan {
     ScanPlan scan;
-    int state_waves;  // waves that share a channel's states
+    int state_waves;  // waves that share a channel's states: 1, 2, 4 or 8
     int tile_waves;   // tiles of 64 channels a workgroup
     int parts;        // workgroups a group's channels are spread over
 };
 
 GradPlan grad_plan(int B, int N, int D, int S, int G) {
     GradPlan p;
-    p.state_waves = (S + 15) / 16;
+    p.state_waves = S <= 8 ? 1 : S <= 16 ? 2 : S <= 32 ? 4 : 8;
     p.scan = scan_plan(B, N, D, G, p.state_waves);
-    p.tile_waves = 4 / p.state_waves;
+    p.tile_waves = p.state_waves >= 4 ? 1 : 4 / p.state_waves;
     if (p.tile_waves > p.scan.tiles) p.tile_waves = p.scan.tiles;
     p.parts = (p.scan.tiles + p.tile_waves - 1) / p.tile_waves;
     return p;
@@ -56,28 +58,27 @@ constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kRor8 = 0x128;
 template <int CTRL> __device__ __forceinline__ float halve(float x, float y, bool bit) {
     return (bit ? y : x) + from_lane<CTRL>(bit ? x : y);
 }
-// Sums over the 64 lanes of v[0 .. NV); lane k gets sum k / (64 / NV).
-template <int NV> __device__ __forceinline__ float lane_sums(float (&v)[NV], int lane) {
-    static_assert(NV == 8 || NV == 16 || NV == 32, "");
+__device__ __forceinline__ float halve32(float x, float y) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halve16(float x, float y) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// The rest of the way for n = SP / 2 registers, each of which holds two sums of every half of the wave (halve32 of dBm and dCm of a
+// state, halve16 of states s and s + n): lane k ends with sum k / (32 / SP) of (dBm of all states, dCm of all states).
+template <int N> __device__ __forceinline__ float lane_sums(float (&v)[N], int lane) {
+    static_assert(N == 2 || N == 4 || N == 8, "");
 #pragma unroll
-    for (int i = 0; i < NV / 2; ++i) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + NV / 2]), false, false);
-        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    }
+    for (int i = 0; i < N / 2; ++i) v[i] = halve<kRor8>(v[i], v[i + N / 2], lane & 8);
+    if constexpr (N >= 4) {
 #pragma unroll
-    for (int i = 0; i < NV / 4; ++i) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + NV / 4]), false, false);
-        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    }
-#pragma unroll
-    for (int i = 0; i < NV / 8; ++i) v[i] = halve<kRor8>(v[i], v[i + NV / 8], lane & 8);
-    if constexpr (NV >= 16) {
-#pragma unroll
-        for (int i = 0; i < NV / 16; ++i) v[i] = halve<kHalfMirror>(v[i], v[i + NV / 16], lane & 4);
+        for (int i = 0; i < N / 4; ++i) v[i] = halve<kHalfMirror>(v[i], v[i + N / 4], lane & 4);
     } else {
         v[0] += from_lane<kHalfMirror>(v[0]);
     }
-    if constexpr (NV >= 32) v[0] = halve<kXor2>(v[0], v[1], lane & 2);
+    if constexpr (N >= 8) v[0] = halve<kXor2>(v[0], v[1], lane & 2);
     else v[0] += from_lane<kXor2>(v[0]);
     return v[0] + from_lane<kXor1>(v[0]);
 }
@@ -116,13 +117,9 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
         GroupVectors<T, SP> gv;
         const auto fetch = [&](int l0) {
             gv.load(in, b, l0, len, group, 0, lane);
-#pragma unroll
-            for (int i = 0; i < kP; ++i) {
-                const int l = l0 + i < len ? l0 + i : len - 1;
-                tr[i] = at<T>(in.dt, b, l)[d];
-                dr[i] = at<T>(r.dout, b, l)[d];
-                if (gated) zr[i] = at<T>(in.z, b, l)[d];
-            }
+            load_rows<T, kP>(in.dt, b, l0, 1, len, d, tr);
+            load_rows<T, kP>(r.dout, b, l0, 1, len, d, dr);
+            if (gated) load_rows<T, kP>(in.z, b, l0, 1, len, d, zr);
         };
         const int last = begin + (end - begin - 1) / kP * kP;
         fetch(last);
@@ -160,34 +157,42 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
     }
 }
 
-// Values of a channel and position that both directions need, in LDS: [kScal][kP][64] a wave (four waves take 78 KB in all, so
-// that two workgroups fit a compute unit).
+// Values of a channel and position that all waves of a tile need, in LDS: [kScal][kP][64] a tile.
 enum { kStep, kDy, kX, kSlope, kDz, kScal };
 
-template <typename T, int SP>
-__global__ __launch_bounds__(256, 2) void scan_grad_kernel(GradRun r) {
+// Floats of LDS: Bm and Cm a wave, `scal` a tile, the sums over the states (y, dput, sum back A) a wave, the sums over the channels a wave.
+template <int SP, int SW> __host__ __device__ constexpr int grad_lds(int tile_waves) {
+    return tile_waves * (SW * (kP * 2 * SP) + kScal * kP * 64 + SW * (3 * kP * 64) + SW * (kP * 2 * SP));
+}
+
+template <typename T, int SP, int SW>
+__global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 8 ? 2 : 3) void scan_grad_kernel(GradRun r) {
     extern __shared__ float lds[];
+    constexpr int P = kP / SW;  // positions whose values of a channel this wave computes: sw, sw + SW, ...
     const ScanIn& in = r.in;
     const ScanPlan& plan = r.plan.scan;
-    const int SW = r.plan.state_waves, CT = r.plan.tile_waves, waves = SW * CT;
+    const int CT = r.plan.tile_waves, waves = SW * CT;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int sw = wave % SW, ct = wave / SW, s0 = sw * SP;
     unsigned which = blockIdx.x / r.plan.parts;
     const int part = blockIdx.x - which * r.plan.parts;
     const unsigned bs = which / in.G;
     const int group = which - bs * in.G;
-    const int b = bs / plan.segments, seg = bs - b * plan.segments;
+    int b = bs / plan.segments;
+    const int seg = bs - b * plan.segments;
+    if (plan.segments == 1) b = ranked(in.lengths, in.B, in.N, b, lane);
     const int tile = part * CT + ct, width = in.D_ / in.G, c0 = tile * 64 + lane;
     const bool is = c0 < width;  // (a whole wave may have no channel: it keeps the workgroup company)
     const int d = group * width + (is ? c0 : width - 1);
     const int len = clamp_length(in.lengths, b, in.N), begin = seg * plan.seg_len;
     const int stop = begin + plan.seg_len < in.N ? begin + plan.seg_len : in.N, end = stop < len ? stop : len;
+    const int64_t from = static_cast<int64_t>(b) * plan.segments + seg;
 
-    float* bc = lds + wave * (kP * 2 * SP);                                  // [waves][kP][2 * SP]
-    float* scal = lds + waves * (kP * 2 * SP) + wave * (kScal * kP * 64);    // [waves][kScal][kP][64]
-    float* sums = lds + waves * (kP * 2 * SP + kScal * kP * 64);             // [waves][3][kP][64]: y, dput, sum back A
-    float* red = sums + waves * (3 * kP * 64);                               // [2][waves][kP][2 * SP]
-    float* my_sums = sums + wave * (3 * kP * 64);
+    float* bc = lds + wave * (kP * 2 * SP);
+    float* scal = lds + waves * (kP * 2 * SP) + ct * (kScal * kP * 64) + lane;
+    float* sums = lds + waves * (kP * 2 * SP) + CT * (kScal * kP * 64) + ct * SW * (3 * kP * 64) + lane;  // of this tile: [SW][3][kP][64]
+    float* my_sums = sums + sw * (3 * kP * 64);
+    float* red = lds + waves * (kP * 2 * SP) + CT * (kScal * kP * 64) + waves * (3 * kP * 64);            // [waves][kP][2 * SP]
 
     const bool gated = in.z.data != nullptr;
     const float skip = in.D ? in.D[d] : 0.0f, bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
@@ -204,45 +209,41 @@ __global__ __launch_bounds__(256, 2) void scan_grad_kernel(GradRun r) {
         dA[s] = 0.0f;
     }
     if (plan.segments > 1 && is) {
-        const int64_t from = static_cast<int64_t>(b) * plan.segments + seg;
 #pragma unroll
         for (int s = 0; s < SP; ++s)
             if (s0 + s < in.S) dh[s] = r.ends[quad_at(from, in.S, in.D_, (s0 + s) / 4, d) + s % 4];
     }
 
     if (begin < end) {
-        T xr[kP], tr[kP], zr[kP], dr[kP];
+        T xr[P], tr[P], zr[P], dr[P];
+        f32x4 before[SP / 4];
         GroupVectors<T, SP> gv;
         const auto fetch = [&](int l0) {
-            gv.load(in, b, l0, len, group, s0, lane);
-#pragma unroll
-            for (int i = 0; i < kP; ++i) {
-                const int l = l0 + i < len ? l0 + i : len - 1;
-                xr[i] = at<T>(in.x, b, l)[d];
-                tr[i] = at<T>(in.dt, b, l)[d];
-                dr[i] = at<T>(r.dout, b, l)[d];
-                if (gated) zr[i] = at<T>(in.z, b, l)[d];
-            }
-        };
-        const int last = begin + (end - begin - 1) / kP * kP;
-        int turn = 0;
-        fetch(last);
-        for (int l0 = last; l0 >= begin; l0 -= kP, turn ^= 1) {
-            float h[SP], p[kP][SP];
             const int64_t block = static_cast<int64_t>(b) * ((in.N + kP - 1) / kP) + l0 / kP;
 #pragma unroll
             for (int q = 0; q < SP / 4; ++q) {
-                f32x4 v = {};
-                if (is && s0 + 4 * q < in.S) v = *reinterpret_cast<const f32x4*>(r.saved + quad_at(block, in.S, in.D_, s0 / 4 + q, d));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) h[4 * q + j] = v[j];
+                before[q] = f32x4{};
+                if (is && s0 + 4 * q < in.S) before[q] = *reinterpret_cast<const f32x4*>(r.saved + quad_at(block, in.S, in.D_, s0 / 4 + q, d));
             }
+            gv.load(in, b, l0, len, group, s0, lane);
+            load_rows<T, P>(in.x, b, l0 + sw, SW, len, d, xr);
+            load_rows<T, P>(in.dt, b, l0 + sw, SW, len, d, tr);
+            load_rows<T, P>(r.dout, b, l0 + sw, SW, len, d, dr);
+            if (gated) load_rows<T, P>(in.z, b, l0 + sw, SW, len, d, zr);
+        };
+        const int last = begin + (end - begin - 1) / kP * kP;
+        fetch(last);
+        for (int l0 = last; l0 >= begin; l0 -= kP) {
+            float h[SP], p[kP][SP];
 #pragma unroll
-            for (int i = 0; i < kP; ++i) {
+            for (int s = 0; s < SP; ++s) h[s] = before[s / 4][s % 4];
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                const int i = sw + k * SW;
                 const bool on = is && l0 + i < end;
-                const Softplus sp = softplus(widen(tr[i]) + bias);
-                const float x = widen(xr[i]), dout = widen(dr[i]), z = gated ? widen(zr[i]) : 0.0f, gate = sigmoid(z);
-                float* to = scal + i * 64 + lane;
+                const Softplus sp = softplus(widen(tr[k]) + bias);
+                const float x = widen(xr[k]), dout = widen(dr[k]), z = gated ? widen(zr[k]) : 0.0f, gate = sigmoid(z);
+                float* to = scal + i * 64;
                 to[kStep * kP * 64] = on ? sp.value : 0.0f;
                 to[kDy * kP * 64] = on ? (gated ? dout * z * gate : dout) : 0.0f;
                 to[kX * kP * 64] = on ? x : 0.0f;
@@ -250,12 +251,14 @@ __global__ __launch_bounds__(256, 2) void scan_grad_kernel(GradRun r) {
                 to[kDz * kP * 64] = dout * gate * fmaf(z, 1.0f - gate, 1.0f);
             }
             gv.put(bc, in, l0, len, s0, lane);
-            wave_sync();
+            if (l0 > begin) fetch(l0 - kP);
+            if (SW > 1) __syncthreads();
+            else wave_sync();
             // forwards
 #pragma unroll
             for (int i = 0; i < kP; ++i) {
                 const f32x4* B4 = reinterpret_cast<const f32x4*>(bc + i * 2 * SP);
-                const float step = scal[(kStep * kP + i) * 64 + lane], put = step * scal[(kX * kP + i) * 64 + lane];
+                const float step = scal[(kStep * kP + i) * 64], put = step * scal[(kX * kP + i) * 64];
                 float y0 = 0.0f, y1 = 0.0f;
 #pragma unroll
                 for (int q = 0; q < SP / 4; ++q) {
@@ -269,75 +272,74 @@ __global__ __launch_bounds__(256, 2) void scan_grad_kernel(GradRun r) {
                         else y0 = fmaf(h[s], Cq[j], y0);
                     }
                 }
-                my_sums[i * 64 + lane] = y0 + y1;
+                my_sums[i * 64] = y0 + y1;
             }
             // backwards
 #pragma unroll
             for (int i = kP - 1; i >= 0; --i) {
                 const f32x4* B4 = reinterpret_cast<const f32x4*>(bc + i * 2 * SP);
-                const float step = scal[(kStep * kP + i) * 64 + lane], put = step * scal[(kX * kP + i) * 64 + lane], dy = scal[(kDy * kP + i) * 64 + lane];
-                float v[2 * SP], dput0 = 0.0f, dput1 = 0.0f, back0 = 0.0f, back1 = 0.0f;
+                const float step = scal[(kStep * kP + i) * 64], put = step * scal[(kX * kP + i) * 64], dy = scal[(kDy * kP + i) * 64];
+                float v[SP / 2], dput0 = 0.0f, dput1 = 0.0f, back0 = 0.0f, back1 = 0.0f;
+                const auto one = [&](int s, float Bs, float Cs, float& dput, float& sum) {
+                    const float e = fmaf(dy, Cs, dh[s]);
+                    const float back = e * p[i][s];
+                    dput = fmaf(e, Bs, dput);
+                    sum = fmaf(back, A[s], sum);
+                    dA[s] = fmaf(back, step, dA[s]);
+                    asm volatile("" : "+v"(dA[s]));  // here: gathered behind the loop it would keep `back` of all eight positions
+                    dh[s] = e * exp2_fast(step * A[s]);
+                    return halve32(e * put, dy * fmaf(put, Bs, p[i][s]));
+                };
+                // states s and s + SP / 2 together, so that few sums are under way at a time
+                const f32x4 B1 = B4[0], C1 = B4[SP / 4], B2 = B4[SP / 4 - 1], C2 = B4[SP / 2 - 1];
 #pragma unroll
-                for (int q = 0; q < SP / 4; ++q) {
-                    const f32x4 Bq = B4[q], Cq = B4[SP / 4 + q];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int s = 4 * q + j;
-                        const float e = fmaf(dy, Cq[j], dh[s]);
-                        v[s] = e * put;
-                        v[SP + s] = dy * fmaf(put, Bq[j], p[i][s]);
-                        const float back = e * p[i][s];
-                        if (j & 1) {
-                            dput1 = fmaf(e, Bq[j], dput1);
-                            back1 = fmaf(back, A[s], back1);
-                        } else {
-                            dput0 = fmaf(e, Bq[j], dput0);
-                            back0 = fmaf(back, A[s], back0);
-                        }
-                        dA[s] = fmaf(back, step, dA[s]);
-                        dh[s] = e * exp2_fast(step * A[s]);
-                    }
+                for (int s = 0; s < SP / 2; ++s) {
+                    const int k = SP == 4 ? s + 2 : s;
+                    const float first = one(s, B1[s], C1[s], dput0, back0);
+                    v[s] = halve16(first, one(s + SP / 2, B2[k], C2[k], dput1, back1));
                 }
-                my_sums[(kP + i) * 64 + lane] = dput0 + dput1;
-                my_sums[(2 * kP + i) * 64 + lane] = (back0 + back1) * kLn2f;
-                const float sum = lane_sums<2 * SP>(v, lane);
-                if (lane % (32 / SP) == 0) red[((turn * waves + wave) * kP + i) * (2 * SP) + lane / (32 / SP)] = sum;
+                my_sums[(kP + i) * 64] = dput0 + dput1;
+                my_sums[(2 * kP + i) * 64] = (back0 + back1) * kLn2f;
+                const float sum = lane_sums<SP / 2>(v, lane);
+                if (lane % (32 / SP) == 0) red[(wave * kP + i) * (2 * SP) + lane / (32 / SP)] = sum;
             }
             __syncthreads();
-            if (l0 > begin) fetch(l0 - kP);
-            // The waves of a tile share its positions.
-            for (int i = sw; i < kP && l0 + i < end; i += SW) {
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                const int i = sw + k * SW;
                 float y = 0.0f, dput = 0.0f, back = 0.0f;
-                for (int k = 0; k < SW; ++k) {
-                    const float* from = sums + (ct * SW + k) * (3 * kP * 64) + lane;
-                    y += from[i * 64];
-                    dput += from[(kP + i) * 64];
-                    back += from[(2 * kP + i) * 64];
+#pragma unroll
+                for (int w = 0; w < SW; ++w) {
+                    y += sums[(w * 3 * kP + i) * 64];
+                    dput += sums[(w * 3 * kP + kP + i) * 64];
+                    back += sums[(w * 3 * kP + 2 * kP + i) * 64];
                 }
-                const float* own = scal + i * 64 + lane;
+                const float* own = scal + i * 64;
                 const float step = own[kStep * kP * 64], dy = own[kDy * kP * 64], x = own[kX * kP * 64];
                 const float dv = fmaf(dput, x, back) * own[kSlope * kP * 64];
-                sum_dv += dv;
-                sum_dD = fmaf(dy, x, sum_dD);
-                if (is) {
-                    const int64_t to = static_cast<int64_t>(l0 + i) * in.D_;
-                    put1(dx + to, fmaf(dput, step, skip * dy));
-                    put1(ddt + to, dv);
-                    if (gated) put1(dz + to, own[kDz * kP * 64] * fmaf(skip, x, y));
+                if (l0 + i < end) {
+                    sum_dv += dv;
+                    sum_dD = fmaf(dy, x, sum_dD);
+                    if (is) {
+                        const int64_t to = static_cast<int64_t>(l0 + i) * in.D_;
+                        put1(dx + to, fmaf(dput, step, skip * dy));
+                        put1(ddt + to, dv);
+                        if (gated) put1(dz + to, own[kDz * kP * 64] * fmaf(skip, x, y));
+                    }
                 }
             }
             for (int k = threadIdx.x; k < kP * SW * 2 * SP; k += blockDim.x) {
                 const int i = k / (SW * 2 * SP), c = k / (SW * SP) & 1, s = k % (SW * SP);
                 if (l0 + i < end && s < in.S) {
                     float sum = 0.0f;
-                    for (int t = 0; t < CT; ++t) sum += red[((turn * waves + t * SW + s / SP) * kP + i) * (2 * SP) + c * SP + s % SP];
+                    for (int t = 0; t < CT; ++t) sum += red[((t * SW + s / SP) * kP + i) * (2 * SP) + c * SP + s % SP];
                     const int64_t to = ((row + l0 + i) * in.G + group) * in.S + s;
                     if (r.plan.parts == 1) put1(static_cast<T*>(c ? r.g.dCm : r.g.dBm) + to, sum);
                     else r.part_bc[(static_cast<int64_t>(part) * 2 + c) * in.B * in.N * in.G * in.S + to] = sum;
                 }
             }
-            if (SW > 1) __syncthreads();  // `sums` is used again
-            else wave_sync();
+            // `sums` and `red` are next written behind the next barrier, of the next eight positions (SW = 1 has none there)
+            if (SW == 1) __syncthreads();
         }
     }
     // Positions past the end.
@@ -357,8 +359,8 @@ __global__ __launch_bounds__(256, 2) void scan_grad_kernel(GradRun r) {
     if (is) {
 #pragma unroll
         for (int s = 0; s < SP; ++s)
-            if (s0 + s < in.S) r.part_a[(static_cast<int64_t>(bs) * in.D_ + d) * in.S + s0 + s] = dA[s];
-        float* pd = r.part_d + (static_cast<int64_t>(bs) * SW + sw) * 2 * in.D_ + d;
+            if (s0 + s < in.S) r.part_a[(from * in.D_ + d) * in.S + s0 + s] = dA[s];
+        float* pd = r.part_d + (from * SW + sw) * 2 * in.D_ + d;
         pd[0] = sum_dD;
         pd[in.D_] = sum_dv;
         if (r.g.dstate && seg == 0) {
@@ -438,16 +440,17 @@ void back_ends(const GradRun& r, hipStream_t st) {
     back_ends_kernel<T, SP><<<static_cast<unsigned>(blocks), 64 * waves, sizeof(float) * waves * kP * 2 * SP, st>>>(r);
 }
 
-template <typename T, int SP>
+template <typename T, int SP, int SW>
 hipError_t grad_main(const GradRun& r, hipStream_t st) {
-    const int waves = r.plan.state_waves * r.plan.tile_waves;
-    const size_t bytes = sizeof(float) * waves * (kP * 2 * SP + (kScal + 3) * kP * 64 + 2 * kP * 2 * SP);
+    const int bytes = static_cast<int>(sizeof(float)) * grad_lds<SP, SW>(r.plan.tile_waves);
     const int64_t blocks = static_cast<int64_t>(r.in.B) * r.plan.scan.segments * r.in.G * r.plan.parts;
-    const auto kernel = scan_grad_kernel<T, SP>;
+    const auto kernel = scan_grad_kernel<T, SP, SW>;
     // more than 64 KB of LDS has to be asked for
-    if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)); e != hipSuccess)
-        return e;
-    kernel<<<static_cast<unsigned>(blocks), 64 * waves, bytes, st>>>(r);
+    if (bytes > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<static_cast<unsigned>(blocks), 64 * SW * r.plan.tile_waves, bytes, st>>>(r);
     return hipSuccess;
 }
 
@@ -462,7 +465,8 @@ hipError_t grad_of(const GradRun& r, hipStream_t st) {
         else back_ends<T, 64>(r, st);
         (void)launch_join_segments(r.in, r.plan.scan, nullptr, r.ends, r.steps, true, st);
     }
-    const hipError_t e = S <= 4 ? grad_main<T, 4>(r, st) : S <= 8 ? grad_main<T, 8>(r, st) : grad_main<T, 16>(r, st);
+    const hipError_t e = S <= 4 ? grad_main<T, 4, 1>(r, st) : S <= 8 ? grad_main<T, 8, 1>(r, st) : S <= 16 ? grad_main<T, 8, 2>(r, st)
+                         : S <= 32 ? grad_main<T, 8, 4>(r, st) : grad_main<T, 8, 8>(r, st);
     if (e != hipSuccess) return e;
     if (r.plan.parts > 1) {
         const int64_t all = static_cast<int64_t>(r.in.B) * r.in.N * r.in.G * S;
