@@ -14,7 +14,7 @@ inline AnyRows rows(const lccrf_rows& r) { return {r.data, r.batch, r.row}; }
 inline bool positions_ok(int B, int N, int D) { return B >= 1 && N >= 1 && D >= 1 && static_cast<int64_t>(B) * N < (int64_t{1} << 31); }
 inline bool conv_ok(int B, int N, int D, int K) { return positions_ok(B, N, D) && K >= LCCRF_MIN_TAPS && K <= LCCRF_MAX_TAPS; }
 inline bool scan_ok(int B, int N, int D, int S, int G) {
-    return positions_ok(B, N, D) && S >= 1 && S <= LCCRF_MAX_STATES && G >= 1 && G <= D && D % G == 0;
+    return positions_ok(B, N, D) && D <= 1 << 22 && S >= 1 && S <= LCCRF_MAX_STATES && G >= 1 && G <= D && D % G == 0 && static_cast<int64_t>(G) * S < (1 << 27);
 }
 inline bool embed_grad_ok(int64_t n, int V, int D) { return n >= 0 && n <= (int64_t{1} << 30) && V >= 1 && V <= 1 << 30 && D >= 1; }
 

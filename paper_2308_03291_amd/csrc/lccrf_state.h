@@ -3,14 +3,22 @@
 // A lane has one channel with all its states in registers; a wave 64 channels of one group, so Bm and Cm of a position are the
 // same for all its lanes: a wave puts those of eight positions into LDS of its own, widened, and reads them back as
 // broadcasts.  The state lives in base 2: exp(step A) = exp2(step (A log2 e)).
+//
+// Blocks of eight positions are worked on while the next one's inputs are on their way.  Loads and stores come back in order, and
+// a wait can only leave in flight what is known to have been issued behind what it waits for: so a whole block has no
+// condition around a store (lanes past a group's end repeat its last channel and write the same value there again), and only the block that ends
+// a sequence is taken with conditions.
 #pragma once
 
 #include "lccrf_encoder.h"
+
+#include <type_traits>
 
 namespace lccrf {
 namespace enc {
 
 constexpr int kP = kScanBlock;
+
 
 struct ScanPlan {
     int tiles;      // waves that cover a group's channels
@@ -34,15 +42,29 @@ template <typename T> __device__ __forceinline__ const T* at(const AnyRows& r, i
     return static_cast<const T*>(r.data) + b * r.batch + l * r.row;
 }
 
-// Channel d of P rows from l0 on, `stride` apart; those past the end take the place of one before it.
-template <typename T, int P> __device__ __forceinline__ void load_rows(const AnyRows& r, int b, int l0, int stride, int len, int d, T (&v)[P]) {
+// The element `bytes` behind a place that is the same for the whole wave: the address stays a scalar pair and a 32-bit offset.
+template <typename T> __device__ __forceinline__ T take(const T* place, unsigned bytes) {
+    return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(place) + bytes);
+}
+template <typename T> __device__ __forceinline__ void give(T* place, unsigned bytes, float v) {
+    put1(reinterpret_cast<T*>(reinterpret_cast<char*>(place) + bytes), v);
+}
+
+// A channel (its byte offset) of P rows from l0 on, `stride` apart; those past the end take the place of one before it.
+template <typename T, int P> __device__ __forceinline__ void load_rows(const AnyRows& r, int b, int l0, int stride, int len, unsigned bytes, T (&v)[P]) {
     const T* p = at<T>(r, b, l0 < len ? l0 : len - 1);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        v[i] = p[d];
+        v[i] = take(p, bytes);
         l0 += stride;
         p += l0 < len ? stride * r.row : 0;
     }
+}
+// The same where all rows lie in front of the end, p the first of them.
+template <typename T, int P> __device__ __forceinline__ void load_whole(const T* p, int64_t row, unsigned bytes, T (&v)[P]) {
+    asm volatile("" : "+v"(bytes));  // widened here, where the loads can use it as their offset, and not in front of the loop
+#pragma unroll
+    for (int i = 0; i < P; ++i, p += row) v[i] = take(p, bytes);
 }
 
 // The sequence with rank k among the lengths, the longest first (equal ones in their order).  Waves of long sequences that start
@@ -81,35 +103,53 @@ __device__ __forceinline__ float base2(float A) {
 }
 
 // Bm and Cm of kP positions for the states s0 .. s0 + SP - 1, on their way from memory to LDS [kP][2 * SP] (Bm, then Cm).
-// Positions outside [0, len) and states past S count as 0.
+// Positions past the end and states past S count as 0.  A lane has state lane % SP of the positions lane / SP + i * kStep.
 template <typename T, int SP> struct GroupVectors {
-    static constexpr int R = kP * 2 * SP / 64 ? kP * 2 * SP / 64 : 1;
-    T raw[R];
+    static constexpr int R = kP * SP / 64 ? kP * SP / 64 : 1, kStep = 64 / SP;
+    T vb[R], vc[R];
+    const T *pb, *pc;  // of this lane's first position
+    int first;
+    bool state;
+    // A first time; past the end the last position stands in.  `next` then moves on by a whole block, all of it in front of the end.
     __device__ __forceinline__ void load(const ScanIn& in, int b, int l0, int len, int group, int s0, int lane) {
-        const T* B = at<T>(in.Bm, b, 0) + group * in.b_group;
-        const T* C = at<T>(in.Cm, b, 0) + group * in.c_group;
+        const int s = s0 + lane % SP;
+        first = lane / SP % kP;
+        state = s < in.S;
+        pb = at<T>(in.Bm, b, l0 + first) + group * in.b_group + (state ? s : 0);
+        pc = at<T>(in.Cm, b, l0 + first) + group * in.c_group + (state ? s : 0);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int k = i * 64 + lane, s = s0 + k % SP;
-            int l = l0 + k / (2 * SP);
-            l = l < len ? l : len - 1;
-            const bool c = k / SP & 1;
-            raw[i] = (c ? C : B)[l * (c ? in.Cm.row : in.Bm.row) + (s < in.S ? s : 0)];
+            const int l = l0 + first + i * kStep, back = l < len ? 0 : l - (len - 1);
+            vb[i] = pb[(i * kStep - back) * in.Bm.row];
+            vc[i] = pc[(i * kStep - back) * in.Cm.row];
         }
     }
-    __device__ __forceinline__ void put(float* lds, const ScanIn& in, int l0, int len, int s0, int lane) const {
+    __device__ __forceinline__ void next(const ScanIn& in, int blocks) {
+        pb += blocks * kP * in.Bm.row;
+        pc += blocks * kP * in.Cm.row;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int k = i * 64 + lane;
-            const bool is = s0 + k % SP < in.S && l0 + k / (2 * SP) < len;
-            if (kP * 2 * SP >= 64 || k < kP * 2 * SP) lds[k] = is ? widen(raw[i]) : 0.0f;
+            vb[i] = pb[i * kStep * in.Bm.row];
+            vc[i] = pc[i * kStep * in.Cm.row];
+        }
+    }
+    template <bool WHOLE> __device__ __forceinline__ void put(float* lds, int l0, int len, int lane) const {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int pos = first + i * kStep;
+            const bool is = state && (WHOLE || l0 + pos < len);
+            lds[pos * 2 * SP + lane % SP] = is ? widen(vb[i]) : 0.0f;
+            lds[pos * 2 * SP + SP + lane % SP] = is ? widen(vc[i]) : 0.0f;
         }
     }
 };
 
-// Saved states: [B][ceil(N / kP)][ceil(S / 4)][D][4] floats.
-__host__ __device__ inline int quads(int S) { return (S + 3) / 4; }
+// Saved states: [B][ceil(N / kP)][quads][D][4] floats, the states rounded up to what a kernel holds.
+__host__ __device__ inline int quads(int S) { return S <= 4 ? 1 : S <= 8 ? 2 : S <= 16 ? 4 : S <= 32 ? 8 : 16; }
 __device__ __forceinline__ int64_t quad_at(int64_t block, int S, int D, int q, int d) { return ((block * quads(S) + q) * D + d) * 4; }
+
+// The same as a place for the whole wave and a byte offset (a channel's 16 bytes; D <= 2^22).
+__device__ __forceinline__ unsigned quad_bytes(int D, int q, int d) { return (static_cast<unsigned>(q) * D + d) * 16; }
 
 inline int scan_blocks(int N) { return (N + kP - 1) / kP; }
 

@@ -24,7 +24,7 @@ struct ScanRun {
     int waves;     // of a workgroup
 };
 
-template <typename T, int SP, int MODE>
+template <typename T, int SP, int MODE, bool GATED>
 __global__ __launch_bounds__(256, SP <= 16 ? 3 : 2) void scan_kernel(ScanRun r) {
     extern __shared__ float lds[];  // [waves][kP][2 * SP]
     const ScanIn& in = r.in;
@@ -32,16 +32,20 @@ __global__ __launch_bounds__(256, SP <= 16 ? 3 : 2) void scan_kernel(ScanRun r) 
     const int groups_of_tiles = (in.G * r.plan.tiles + r.waves - 1) / r.waves;
     const unsigned which = blockIdx.x / groups_of_tiles;
     const int tile = (blockIdx.x - which * groups_of_tiles) * r.waves + wave;
-    const int b = which / r.plan.segments, seg = which - b * r.plan.segments;
+    int b = which / r.plan.segments;
+    const int seg = which - b * r.plan.segments;
     if (tile >= in.G * r.plan.tiles) return;
+    // Whole sequences, as many waves as there is room for at once: long ones first, then the short ones from the shortest on, so that a
+    // SIMD's waves are about as long together everywhere.
+    if (r.plan.segments == 1) b = ranked(in.lengths, in.B, in.N, b < (in.B + 1) / 2 ? b : in.B - 1 - (b - (in.B + 1) / 2), lane);
     const int width = in.D_ / in.G, group = tile / r.plan.tiles, c0 = (tile - group * r.plan.tiles) * 64 + lane;
     const bool is = c0 < width;
     const int d = group * width + (is ? c0 : width - 1);
     const int len = clamp_length(in.lengths, b, in.N), begin = seg * r.plan.seg_len;
     const int stop = begin + r.plan.seg_len < in.N ? begin + r.plan.seg_len : in.N, end = stop < len ? stop : len;
     float* bc = lds + wave * (kP * 2 * SP);
-    T* out = MODE & kOut ? static_cast<T*>(r.out) + static_cast<int64_t>(b) * in.N * in.D_ + d : nullptr;
-    const bool gated = in.z.data != nullptr;
+    const unsigned bytes = static_cast<unsigned>(d) * sizeof(T);
+    T* out = MODE & kOut ? static_cast<T*>(r.out) + static_cast<int64_t>(b) * in.N * in.D_ : nullptr;
     const float skip = in.D ? in.D[d] : 0.0f, bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
 
     float h[SP], A[SP], total = 0.0f;
@@ -66,34 +70,46 @@ __global__ __launch_bounds__(256, SP <= 16 ? 3 : 2) void scan_kernel(ScanRun r) 
     if (begin < end) {
         T xr[kP], tr[kP], zr[kP];
         GroupVectors<T, SP> gv;
+        const T *px = at<T>(in.x, b, begin), *pt = at<T>(in.dt, b, begin), *pz = at<T>(in.z, b, begin);
         const auto fetch = [&](int l0) {
             gv.load(in, b, l0, len, group, 0, lane);
-            load_rows<T, kP>(in.x, b, l0, 1, len, d, xr);
-            load_rows<T, kP>(in.dt, b, l0, 1, len, d, tr);
-            if ((MODE & kOut) && gated) load_rows<T, kP>(in.z, b, l0, 1, len, d, zr);
+            load_rows<T, kP>(in.x, b, l0, 1, len, bytes, xr);
+            load_rows<T, kP>(in.dt, b, l0, 1, len, bytes, tr);
+            if (GATED) load_rows<T, kP>(in.z, b, l0, 1, len, bytes, zr);
         };
-        fetch(begin);
-        for (int l0 = begin; l0 < end; l0 += kP) {
+        const auto block = [&](auto whole, int l0) {
+            constexpr bool WHOLE = decltype(whole)::value;
             float step[kP], put[kP], y[kP], x[kP], z[kP];
 #pragma unroll
             for (int i = 0; i < kP; ++i) {
-                const bool on = l0 + i < end;
+                const bool on = WHOLE || l0 + i < end;
                 step[i] = on ? softplus(widen(tr[i]) + bias).value : 0.0f;
                 x[i] = on ? widen(xr[i]) : 0.0f;
                 put[i] = step[i] * x[i];
-                if (MODE & kOut) z[i] = gated ? widen(zr[i]) : 0.0f;
+                if (GATED) z[i] = widen(zr[i]);
                 if (MODE & kEnds) total += step[i];
             }
             wave_sync();
-            gv.put(bc, in, l0, len, 0, lane);
+            gv.template put<WHOLE>(bc, l0, len, lane);
             wave_sync();
-            if (l0 + kP < end) fetch(l0 + kP);
+            if (WHOLE) {
+                if (l0 + 2 * kP <= end) {
+                    px += kP * in.x.row;
+                    pt += kP * in.dt.row;
+                    pz += kP * in.z.row;
+                    gv.next(in, 1);
+                    load_whole<T, kP>(px, in.x.row, bytes, xr);
+                    load_whole<T, kP>(pt, in.dt.row, bytes, tr);
+                    if (GATED) load_whole<T, kP>(pz, in.z.row, bytes, zr);
+                } else if (l0 + kP < end) {
+                    fetch(l0 + kP);
+                }
+            }
             if (MODE & kSave) {
-                const int64_t block = static_cast<int64_t>(b) * ((in.N + kP - 1) / kP) + l0 / kP;
+                float* place = r.saved + quad_at(static_cast<int64_t>(b) * ((in.N + kP - 1) / kP) + l0 / kP, in.S, in.D_, 0, 0);
 #pragma unroll
                 for (int q = 0; q < SP / 4; ++q)
-                    if (is && 4 * q < in.S)
-                        *reinterpret_cast<f32x4*>(r.saved + quad_at(block, in.S, in.D_, q, d)) = f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]};
+                    *reinterpret_cast<f32x4*>(reinterpret_cast<char*>(place) + quad_bytes(in.D_, q, d)) = f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]};
             }
 #pragma unroll
             for (int i = 0; i < kP; ++i) {
@@ -117,21 +133,27 @@ __global__ __launch_bounds__(256, SP <= 16 ? 3 : 2) void scan_kernel(ScanRun r) 
                     }
                 }
                 y[i] = y0 + y1;
-                asm volatile("" : "+v"(y[i]));  // computed here: moved behind the store's condition, it would keep the states of all eight positions
+                asm volatile("" : "+v"(y[i]));  // computed here: moved behind a store's condition, it would keep the states of all eight positions
             }
             if (MODE & kOut) {
+                T* to = out + static_cast<int64_t>(l0) * in.D_;
+                unsigned o = bytes;
+                asm volatile("" : "+v"(o));
 #pragma unroll
-                for (int i = 0; i < kP; ++i) {
+                for (int i = 0; i < kP; ++i, to += in.D_) {
                     const float v = fmaf(skip, x[i], y[i]);
-                    const float o = gated ? v * z[i] * sigmoid(z[i]) : v;
-                    if (is && l0 + i < end) put1(out + static_cast<int64_t>(l0 + i) * in.D_, o);
+                    if (WHOLE || l0 + i < end) give(to, o, GATED ? v * z[i] * sigmoid(z[i]) : v);
                 }
             }
-        }
+        };
+        fetch(begin);
+        int l0 = begin;
+        for (; l0 + kP <= end; l0 += kP) block(std::true_type{}, l0);
+        if (l0 < end) block(std::false_type{}, l0);
     }
     if (MODE & kOut)
         for (int l = begin < end ? end : begin; l < stop; ++l)
-            if (is) put1(out + static_cast<int64_t>(l) * in.D_, 0.0f);
+            if (is) give(out + static_cast<int64_t>(l) * in.D_, bytes, 0.0f);
     if (MODE & kEnds) {
         const int64_t to = static_cast<int64_t>(b) * r.plan.segments + seg;
         if (is) {
@@ -274,7 +296,8 @@ hipError_t step_of(const ScanIn& in, float* state, void* out, hipStream_t st) {
 template <typename T, int SP, int MODE>
 void scan_launch(const ScanRun& r, hipStream_t st) {
     const int64_t wgs = (static_cast<int64_t>(r.in.G) * r.plan.tiles + r.waves - 1) / r.waves;
-    scan_kernel<T, SP, MODE><<<static_cast<unsigned>(wgs * r.in.B * r.plan.segments), 64 * r.waves, sizeof(float) * r.waves * kP * 2 * SP, st>>>(r);
+    const auto kernel = (MODE & kOut) && r.in.z.data ? scan_kernel<T, SP, MODE, (MODE & kOut) != 0> : scan_kernel<T, SP, MODE, false>;
+    kernel<<<static_cast<unsigned>(wgs * r.in.B * r.plan.segments), 64 * r.waves, sizeof(float) * r.waves * kP * 2 * SP, st>>>(r);
 }
 
 template <typename T, int SP>

@@ -3,11 +3,10 @@
 // With dh[l] = dy[l] Cm[l] + a[l+1] dh[l+1] running backwards,
 //     dCm = sum_channels dy h,   dBm = sum_channels dh put,   dput = sum_s dh Bm,   back = dh a h[l-1]  (by the decay's logarithm),
 //     dx = dput step + D dy,     dv = (dput x + sum_s back A) sigmoid(v),    dA = sum_positions back step.
-// The states in front of every eighth position are saved by the forward pass; eight positions are run again from there, the products
-// p = a h[l-1] kept in registers (h = p + put Bm follows from them by one multiply-add; p from h would lose what a
-// small decay leaves), and then gone through backwards.  About 22 issue slots an update with 16 states: vector arithmetic bounds it.
+// The states in front of every eighth position are saved by the forward pass; eight positions are run again from there, states
+// and decays kept in registers, and then gone through backwards.  About 22 issue slots an update with 16 states: vector arithmetic bounds it.
 //
-// A wave has 64 channels and up to 8 states (64 registers of products; with 16 states a wave the registers that remain hold
+// A wave has 64 channels and up to 8 states (128 registers of states and decays of eight positions; with 16 states a wave the registers that remain hold
 // neither the next positions' inputs nor a second and third wave's work, and it took three times as long); more states are shared by
 // several waves of a workgroup, which also share what is computed once a channel, and whose sums over the states meet in LDS.
 // The sums over the channels are taken by halving: two registers and two halves of the wave become one register whose
@@ -31,8 +30,8 @@ GradPlan grad_plan(int B, int N, int D, int S, int G) {
     p.state_waves = S <= 8 ? 1 : S <= 16 ? 2 : S <= 32 ? 4 : 8;
     p.scan = scan_plan(B, N, D, G, p.state_waves);
     p.tile_waves = p.state_waves >= 4 ? 1 : 4 / p.state_waves;
-    if (p.tile_waves > p.scan.tiles) p.tile_waves = p.scan.tiles;
-    p.parts = (p.scan.tiles + p.tile_waves - 1) / p.tile_waves;
+    while (p.scan.tiles % p.tile_waves) p.tile_waves /= 2;  // no wave without a channel
+    p.parts = p.scan.tiles / p.tile_waves;
     return p;
 }
 
@@ -105,6 +104,7 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
     const int stop = begin + plan.seg_len < in.N ? begin + plan.seg_len : in.N, end = stop < len ? stop : len;
     float* bc = lds + wave * (kP * 2 * SP);
     const bool gated = in.z.data != nullptr;
+    const unsigned bytes = static_cast<unsigned>(d) * sizeof(T);
     const float bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
     float dh[SP], A[SP], total = 0.0f;
 #pragma unroll
@@ -115,14 +115,12 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
     if (begin < end) {
         T tr[kP], zr[kP], dr[kP];
         GroupVectors<T, SP> gv;
-        const auto fetch = [&](int l0) {
-            gv.load(in, b, l0, len, group, 0, lane);
-            load_rows<T, kP>(in.dt, b, l0, 1, len, d, tr);
-            load_rows<T, kP>(r.dout, b, l0, 1, len, d, dr);
-            if (gated) load_rows<T, kP>(in.z, b, l0, 1, len, d, zr);
-        };
         const int last = begin + (end - begin - 1) / kP * kP;
-        fetch(last);
+        gv.load(in, b, last, len, group, 0, lane);
+        load_rows<T, kP>(in.dt, b, last, 1, len, bytes, tr);
+        load_rows<T, kP>(r.dout, b, last, 1, len, bytes, dr);
+        if (gated) load_rows<T, kP>(in.z, b, last, 1, len, bytes, zr);
+        const T *pt = at<T>(in.dt, b, last), *pd = at<T>(r.dout, b, last), *pz = at<T>(in.z, b, last);
         for (int l0 = last; l0 >= begin; l0 -= kP) {
             float step[kP], dy[kP];
 #pragma unroll
@@ -133,9 +131,17 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
                 total += step[i];
             }
             wave_sync();
-            gv.put(bc, in, l0, len, 0, lane);
+            gv.template put<false>(bc, l0, len, lane);
             wave_sync();
-            if (l0 > begin) fetch(l0 - kP);
+            if (l0 > begin) {
+                pt -= kP * in.dt.row;
+                pd -= kP * r.dout.row;
+                pz -= kP * in.z.row;
+                gv.next(in, -1);
+                load_whole<T, kP>(pt, in.dt.row, bytes, tr);
+                load_whole<T, kP>(pd, r.dout.row, bytes, dr);
+                if (gated) load_whole<T, kP>(pz, in.z.row, bytes, zr);
+            }
 #pragma unroll
             for (int i = kP - 1; i >= 0; --i) {
                 const f32x4* C4 = reinterpret_cast<const f32x4*>(bc + i * 2 * SP + SP);
@@ -165,8 +171,8 @@ template <int SP, int SW> __host__ __device__ constexpr int grad_lds(int tile_wa
     return tile_waves * (SW * (kP * 2 * SP) + kScal * kP * 64 + SW * (3 * kP * 64) + SW * (kP * 2 * SP));
 }
 
-template <typename T, int SP, int SW>
-__global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 8 ? 2 : 3) void scan_grad_kernel(GradRun r) {
+template <typename T, int SP, int SW, bool GATED>
+__global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 4 ? 4 : SW == 1 ? 2 : 3) void scan_grad_kernel(GradRun r) {
     extern __shared__ float lds[];
     constexpr int P = kP / SW;  // positions whose values of a channel this wave computes: sw, sw + SW, ...
     const ScanIn& in = r.in;
@@ -182,7 +188,7 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 8 ? 2 : 3) void scan_gra
     const int seg = bs - b * plan.segments;
     if (plan.segments == 1) b = ranked(in.lengths, in.B, in.N, b, lane);
     const int tile = part * CT + ct, width = in.D_ / in.G, c0 = tile * 64 + lane;
-    const bool is = c0 < width;  // (a whole wave may have no channel: it keeps the workgroup company)
+    const bool is = c0 < width, full_tile = tile * 64 + 64 <= width;
     const int d = group * width + (is ? c0 : width - 1);
     const int len = clamp_length(in.lengths, b, in.N), begin = seg * plan.seg_len;
     const int stop = begin + plan.seg_len < in.N ? begin + plan.seg_len : in.N, end = stop < len ? stop : len;
@@ -194,13 +200,12 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 8 ? 2 : 3) void scan_gra
     float* my_sums = sums + sw * (3 * kP * 64);
     float* red = lds + waves * (kP * 2 * SP) + CT * (kScal * kP * 64) + waves * (3 * kP * 64);            // [waves][kP][2 * SP]
 
-    const bool gated = in.z.data != nullptr;
     const float skip = in.D ? in.D[d] : 0.0f, bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
     const int64_t row = static_cast<int64_t>(b) * in.N;
-    T* dx = static_cast<T*>(r.g.dx) + row * in.D_ + d;
-    T* ddt = static_cast<T*>(r.g.ddt) + row * in.D_ + d;
-    T* dz = gated ? static_cast<T*>(r.g.dz) + row * in.D_ + d : nullptr;
-
+    const unsigned bytes = static_cast<unsigned>(d) * sizeof(T);
+    T* dx = static_cast<T*>(r.g.dx) + row * in.D_;
+    T* ddt = static_cast<T*>(r.g.ddt) + row * in.D_;
+    T* dz = static_cast<T*>(r.g.dz) + row * in.D_;
     float dh[SP], A[SP], dA[SP], sum_dD = 0.0f, sum_dv = 0.0f;
 #pragma unroll
     for (int s = 0; s < SP; ++s) {
@@ -208,7 +213,7 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 8 ? 2 : 3) void scan_gra
         dh[s] = 0.0f;
         dA[s] = 0.0f;
     }
-    if (plan.segments > 1 && is) {
+    if (plan.segments > 1) {
 #pragma unroll
         for (int s = 0; s < SP; ++s)
             if (s0 + s < in.S) dh[s] = r.ends[quad_at(from, in.S, in.D_, (s0 + s) / 4, d) + s % 4];
@@ -218,40 +223,54 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 8 ? 2 : 3) void scan_gra
         T xr[P], tr[P], zr[P], dr[P];
         f32x4 before[SP / 4];
         GroupVectors<T, SP> gv;
-        const auto fetch = [&](int l0) {
-            const int64_t block = static_cast<int64_t>(b) * ((in.N + kP - 1) / kP) + l0 / kP;
-#pragma unroll
-            for (int q = 0; q < SP / 4; ++q) {
-                before[q] = f32x4{};
-                if (is && s0 + 4 * q < in.S) before[q] = *reinterpret_cast<const f32x4*>(r.saved + quad_at(block, in.S, in.D_, s0 / 4 + q, d));
-            }
-            gv.load(in, b, l0, len, group, s0, lane);
-            load_rows<T, P>(in.x, b, l0 + sw, SW, len, d, xr);
-            load_rows<T, P>(in.dt, b, l0 + sw, SW, len, d, tr);
-            load_rows<T, P>(r.dout, b, l0 + sw, SW, len, d, dr);
-            if (gated) load_rows<T, P>(in.z, b, l0 + sw, SW, len, d, zr);
-        };
         const int last = begin + (end - begin - 1) / kP * kP;
-        fetch(last);
-        for (int l0 = last; l0 >= begin; l0 -= kP) {
-            float h[SP], p[kP][SP];
+        const int64_t block = static_cast<int64_t>(in.D_) * quads(in.S) * 4;
+        const float* ps = r.saved + (static_cast<int64_t>(b) * ((in.N + kP - 1) / kP) + last / kP) * block;
+        const unsigned quad = quad_bytes(in.D_, s0 / 4, d);
+        const auto load_before = [&] {
 #pragma unroll
-            for (int s = 0; s < SP; ++s) h[s] = before[s / 4][s % 4];
+            for (int q = 0; q < SP / 4; ++q)
+                before[q] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(ps) + (quad + static_cast<unsigned>(q * in.D_) * 16));
+        };
+        load_before();
+        gv.load(in, b, last, len, group, s0, lane);
+        load_rows<T, P>(in.x, b, last + sw, SW, len, bytes, xr);
+        load_rows<T, P>(in.dt, b, last + sw, SW, len, bytes, tr);
+        load_rows<T, P>(r.dout, b, last + sw, SW, len, bytes, dr);
+        if (GATED) load_rows<T, P>(in.z, b, last + sw, SW, len, bytes, zr);
+        const T *px = at<T>(in.x, b, last + sw), *pt = at<T>(in.dt, b, last + sw), *pd = at<T>(r.dout, b, last + sw), *pz = at<T>(in.z, b, last + sw);
+        const auto fetch = [&] {  // the block in front
+            ps -= block;
+            px -= kP * in.x.row;
+            pt -= kP * in.dt.row;
+            pd -= kP * r.dout.row;
+            pz -= kP * in.z.row;
+            load_before();
+            gv.next(in, -1);
+            load_whole<T, P>(px, SW * in.x.row, bytes, xr);
+            load_whole<T, P>(pt, SW * in.dt.row, bytes, tr);
+            load_whole<T, P>(pd, SW * r.dout.row, bytes, dr);
+            if (GATED) load_whole<T, P>(pz, SW * in.z.row, bytes, zr);
+        };
+        const auto eight = [&](auto whole, int l0) {
+            constexpr bool WHOLE = decltype(whole)::value;
+            float h[kP + 1][SP];  // h[i]: in front of position i
+#pragma unroll
+            for (int s = 0; s < SP; ++s) h[0][s] = before[s / 4][s % 4];
 #pragma unroll
             for (int k = 0; k < P; ++k) {
                 const int i = sw + k * SW;
-                const bool on = is && l0 + i < end;
+                const bool on = WHOLE || l0 + i < end;
                 const Softplus sp = softplus(widen(tr[k]) + bias);
-                const float x = widen(xr[k]), dout = widen(dr[k]), z = gated ? widen(zr[k]) : 0.0f, gate = sigmoid(z);
+                const float x = widen(xr[k]), dout = widen(dr[k]), z = GATED ? widen(zr[k]) : 0.0f, gate = sigmoid(z);
                 float* to = scal + i * 64;
                 to[kStep * kP * 64] = on ? sp.value : 0.0f;
-                to[kDy * kP * 64] = on ? (gated ? dout * z * gate : dout) : 0.0f;
+                to[kDy * kP * 64] = on ? (GATED ? dout * z * gate : dout) : 0.0f;
                 to[kX * kP * 64] = on ? x : 0.0f;
                 to[kSlope * kP * 64] = sp.slope;
-                to[kDz * kP * 64] = dout * gate * fmaf(z, 1.0f - gate, 1.0f);
+                if (GATED) to[kDz * kP * 64] = dout * gate * fmaf(z, 1.0f - gate, 1.0f);
             }
-            gv.put(bc, in, l0, len, s0, lane);
-            if (l0 > begin) fetch(l0 - kP);
+            gv.template put<WHOLE>(bc, l0, len, lane);
             if (SW > 1) __syncthreads();
             else wave_sync();
             // forwards
@@ -262,33 +281,41 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 8 ? 2 : 3) void scan_gra
                 float y0 = 0.0f, y1 = 0.0f;
 #pragma unroll
                 for (int q = 0; q < SP / 4; ++q) {
-                    const f32x4 Bq = B4[q], Cq = B4[SP / 4 + q];
+                    const f32x4 Bq = B4[q];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int s = 4 * q + j;
-                        p[i][s] = exp2_fast(step * A[s]) * h[s];
-                        h[s] = fmaf(put, Bq[j], p[i][s]);
-                        if (j & 1) y1 = fmaf(h[s], Cq[j], y1);
-                        else y0 = fmaf(h[s], Cq[j], y0);
+                        h[i + 1][s] = fmaf(exp2_fast(step * A[s]), h[i][s], put * Bq[j]);
+                    }
+                    if (GATED) {  // y itself is what dz needs
+                        const f32x4 Cq = B4[SP / 4 + q];
+                        y0 = fmaf(h[i + 1][4 * q], Cq[0], y0);
+                        y1 = fmaf(h[i + 1][4 * q + 1], Cq[1], y1);
+                        y0 = fmaf(h[i + 1][4 * q + 2], Cq[2], y0);
+                        y1 = fmaf(h[i + 1][4 * q + 3], Cq[3], y1);
                     }
                 }
-                my_sums[i * 64] = y0 + y1;
+                if (GATED) my_sums[i * 64] = y0 + y1;
             }
             // backwards
 #pragma unroll
             for (int i = kP - 1; i >= 0; --i) {
                 const f32x4* B4 = reinterpret_cast<const f32x4*>(bc + i * 2 * SP);
                 const float step = scal[(kStep * kP + i) * 64], put = step * scal[(kX * kP + i) * 64], dy = scal[(kDy * kP + i) * 64];
-                float v[SP / 2], dput0 = 0.0f, dput1 = 0.0f, back0 = 0.0f, back1 = 0.0f;
+                float v[SP / 2], dput0 = 0.0f, dput1 = 0.0f, back0 = 0.0f, back1 = 0.0f, own_put = put, own_dy = dy;
+                if (!full_tile) {  // a channel that a lane only repeats is not to be counted twice
+                    own_put = is ? put : 0.0f;
+                    own_dy = is ? dy : 0.0f;
+                }
                 const auto one = [&](int s, float Bs, float Cs, float& dput, float& sum) {
                     const float e = fmaf(dy, Cs, dh[s]);
-                    const float back = e * p[i][s];
+                    dh[s] = e * exp2_fast(step * A[s]);
+                    const float back = dh[s] * h[i][s];
                     dput = fmaf(e, Bs, dput);
                     sum = fmaf(back, A[s], sum);
                     dA[s] = fmaf(back, step, dA[s]);
                     asm volatile("" : "+v"(dA[s]));  // here: gathered behind the loop it would keep `back` of all eight positions
-                    dh[s] = e * exp2_fast(step * A[s]);
-                    return halve32(e * put, dy * fmaf(put, Bs, p[i][s]));
+                    return halve32(e * own_put, own_dy * h[i + 1][s]);
                 };
                 // states s and s + SP / 2 together, so that few sums are under way at a time
                 const f32x4 B1 = B4[0], C1 = B4[SP / 4], B2 = B4[SP / 4 - 1], C2 = B4[SP / 2 - 1];
@@ -302,53 +329,70 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 8 ? 2 : 3) void scan_gra
                 my_sums[(2 * kP + i) * 64] = (back0 + back1) * kLn2f;
                 const float sum = lane_sums<SP / 2>(v, lane);
                 if (lane % (32 / SP) == 0) red[(wave * kP + i) * (2 * SP) + lane / (32 / SP)] = sum;
+                if (i == kP / 2 && l0 > begin) fetch();  // into the registers of the positions that are done
             }
             __syncthreads();
+            const int64_t first = static_cast<int64_t>(l0 + sw) * in.D_;
+            T *tx = dx + first, *tt = ddt + first, *tz = dz + first;
+            unsigned o = bytes;
+            asm volatile("" : "+v"(o));
 #pragma unroll
             for (int k = 0; k < P; ++k) {
                 const int i = sw + k * SW;
                 float y = 0.0f, dput = 0.0f, back = 0.0f;
 #pragma unroll
                 for (int w = 0; w < SW; ++w) {
-                    y += sums[(w * 3 * kP + i) * 64];
+                    if (GATED) y += sums[(w * 3 * kP + i) * 64];
                     dput += sums[(w * 3 * kP + kP + i) * 64];
                     back += sums[(w * 3 * kP + 2 * kP + i) * 64];
                 }
                 const float* own = scal + i * 64;
                 const float step = own[kStep * kP * 64], dy = own[kDy * kP * 64], x = own[kX * kP * 64];
                 const float dv = fmaf(dput, x, back) * own[kSlope * kP * 64];
-                if (l0 + i < end) {
+                if (WHOLE || l0 + i < end) {
                     sum_dv += dv;
                     sum_dD = fmaf(dy, x, sum_dD);
-                    if (is) {
-                        const int64_t to = static_cast<int64_t>(l0 + i) * in.D_;
-                        put1(dx + to, fmaf(dput, step, skip * dy));
-                        put1(ddt + to, dv);
-                        if (gated) put1(dz + to, own[kDz * kP * 64] * fmaf(skip, x, y));
-                    }
+                    give(tx, o, fmaf(dput, step, skip * dy));
+                    give(tt, o, dv);
+                    if (GATED) give(tz, o, own[kDz * kP * 64] * fmaf(skip, x, y));
                 }
+                tx += SW * in.D_;
+                tt += SW * in.D_;
+                tz += SW * in.D_;
             }
-            for (int k = threadIdx.x; k < kP * SW * 2 * SP; k += blockDim.x) {
-                const int i = k / (SW * 2 * SP), c = k / (SW * SP) & 1, s = k % (SW * SP);
-                if (l0 + i < end && s < in.S) {
-                    float sum = 0.0f;
-                    for (int t = 0; t < CT; ++t) sum += red[((t * SW + s / SP) * kP + i) * (2 * SP) + c * SP + s % SP];
-                    const int64_t to = ((row + l0 + i) * in.G + group) * in.S + s;
-                    if (r.plan.parts == 1) put1(static_cast<T*>(c ? r.g.dCm : r.g.dBm) + to, sum);
-                    else r.part_bc[(static_cast<int64_t>(part) * 2 + c) * in.B * in.N * in.G * in.S + to] = sum;
+            // The sums over the channels: position i, Bm or Cm, state s, from the waves of all tiles.
+            const int64_t group_row = (row + l0) * in.G * in.S;
+            unsigned k = threadIdx.x;
+            asm volatile("" : "+v"(k));  // what follows from it is a few shifts: not worth registers through the loop
+            for (; k < kP * SW * 2 * SP; k += 64 * waves) {
+                const int i = k / (SW * 2 * SP), s = k % (SW * SP);
+                const bool c = k / (SW * SP) & 1;
+                if ((WHOLE || l0 + i < end) && s < in.S) {
+                    const float* from = red + (s / SP * kP + i) * (2 * SP) + c * SP + s % SP;
+                    float sum = from[0];
+                    for (int t = 1; t < CT; ++t) sum += from[t * (SW * kP * 2 * SP)];
+                    const int to = (i * in.G + group) * in.S + s;
+                    if (r.plan.parts == 1) put1((c ? static_cast<T*>(r.g.dCm) : static_cast<T*>(r.g.dBm)) + group_row + to, sum);
+                    else (r.part_bc + (static_cast<int64_t>(part) * 2 + c) * in.B * in.N * in.G * in.S + group_row)[to] = sum;
                 }
             }
             // `sums` and `red` are next written behind the next barrier, of the next eight positions (SW = 1 has none there)
             if (SW == 1) __syncthreads();
+        };
+        int l0 = last;
+        if (l0 + kP > end) {
+            eight(std::false_type{}, l0);
+            l0 -= kP;
         }
+        for (; l0 >= begin; l0 -= kP) eight(std::true_type{}, l0);
     }
     // Positions past the end.
     for (int l = begin < end ? end : begin; l < stop; ++l) {
         const int64_t to = static_cast<int64_t>(l) * in.D_;
         if (is && sw == 0) {
-            put1(dx + to, 0.0f);
-            put1(ddt + to, 0.0f);
-            if (gated) put1(dz + to, 0.0f);
+            give(dx + to, bytes, 0.0f);
+            give(ddt + to, bytes, 0.0f);
+            if (GATED) give(dz + to, bytes, 0.0f);
         }
         if (r.plan.parts == 1)
             for (int s = threadIdx.x; s < in.S; s += blockDim.x) {
@@ -444,7 +488,7 @@ template <typename T, int SP, int SW>
 hipError_t grad_main(const GradRun& r, hipStream_t st) {
     const int bytes = static_cast<int>(sizeof(float)) * grad_lds<SP, SW>(r.plan.tile_waves);
     const int64_t blocks = static_cast<int64_t>(r.in.B) * r.plan.scan.segments * r.in.G * r.plan.parts;
-    const auto kernel = scan_grad_kernel<T, SP, SW>;
+    const auto kernel = r.in.z.data ? scan_grad_kernel<T, SP, SW, true> : scan_grad_kernel<T, SP, SW, false>;
     // more than 64 KB of LDS has to be asked for
     if (bytes > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
