@@ -5,9 +5,9 @@
 // broadcasts.  The state lives in base 2: exp(step A) = exp2(step (A log2 e)).
 //
 // Blocks of eight positions are worked on while the next one's inputs are on their way.  Loads and stores come back in order, and
-// a wait can only leave in flight what is known to have been issued behind what it waits for: so a whole block has no
-// condition around a store (lanes past a group's end repeat its last channel and write the same value there again), and only the block that ends
-// a sequence is taken with conditions.
+// a wait can only leave in flight what is known to have been issued behind what it waits for.  So the next block's inputs are taken up in
+// front of this block's stores, and a whole block has no condition around a store (lanes past a group's end repeat its last
+// channel and write the same value there again); only the block that ends a sequence is taken with conditions.
 #pragma once
 
 #include "lccrf_encoder.h"
@@ -110,13 +110,15 @@ template <typename T, int SP> struct GroupVectors {
     const T *pb, *pc;  // of this lane's first position
     int first;
     bool state;
-    // A first time; past the end the last position stands in.  `next` then moves on by a whole block, all of it in front of the end.
-    __device__ __forceinline__ void load(const ScanIn& in, int b, int l0, int len, int group, int s0, int lane) {
+    __device__ __forceinline__ void place(const ScanIn& in, int b, int l0, int group, int s0, int lane) {
         const int s = s0 + lane % SP;
         first = lane / SP % kP;
         state = s < in.S;
         pb = at<T>(in.Bm, b, l0 + first) + group * in.b_group + (state ? s : 0);
         pc = at<T>(in.Cm, b, l0 + first) + group * in.c_group + (state ? s : 0);
+    }
+    // A block that the end may lie in: past it the last position stands in.
+    __device__ __forceinline__ void load(const ScanIn& in, int l0, int len) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int l = l0 + first + i * kStep, back = l < len ? 0 : l - (len - 1);
@@ -124,6 +126,7 @@ template <typename T, int SP> struct GroupVectors {
             vc[i] = pc[(i * kStep - back) * in.Cm.row];
         }
     }
+    // The whole block that lies `blocks` further.
     __device__ __forceinline__ void next(const ScanIn& in, int blocks) {
         pb += blocks * kP * in.Bm.row;
         pc += blocks * kP * in.Cm.row;

@@ -25,7 +25,7 @@ struct ScanRun {
 };
 
 template <typename T, int SP, int MODE, bool GATED>
-__global__ __launch_bounds__(256, SP <= 16 ? 3 : 2) void scan_kernel(ScanRun r) {
+__global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
     extern __shared__ float lds[];  // [waves][kP][2 * SP]
     const ScanIn& in = r.in;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -71,15 +71,18 @@ __global__ __launch_bounds__(256, SP <= 16 ? 3 : 2) void scan_kernel(ScanRun r) 
         T xr[kP], tr[kP], zr[kP];
         GroupVectors<T, SP> gv;
         const T *px = at<T>(in.x, b, begin), *pt = at<T>(in.dt, b, begin), *pz = at<T>(in.z, b, begin);
-        const auto fetch = [&](int l0) {
-            gv.load(in, b, l0, len, group, 0, lane);
-            load_rows<T, kP>(in.x, b, l0, 1, len, bytes, xr);
-            load_rows<T, kP>(in.dt, b, l0, 1, len, bytes, tr);
-            if (GATED) load_rows<T, kP>(in.z, b, l0, 1, len, bytes, zr);
+        const auto fetch_whole = [&](int ahead) {
+            px += ahead * kP * in.x.row;
+            pt += ahead * kP * in.dt.row;
+            pz += ahead * kP * in.z.row;
+            gv.next(in, ahead);
+            load_whole<T, kP>(px, in.x.row, bytes, xr);
+            load_whole<T, kP>(pt, in.dt.row, bytes, tr);
+            if (GATED) load_whole<T, kP>(pz, in.z.row, bytes, zr);
         };
-        const auto block = [&](auto whole, int l0) {
+        float step[kP], put[kP], x[kP], z[kP];
+        const auto settle = [&](auto whole, int l0) {  // what fetch has brought
             constexpr bool WHOLE = decltype(whole)::value;
-            float step[kP], put[kP], y[kP], x[kP], z[kP];
 #pragma unroll
             for (int i = 0; i < kP; ++i) {
                 const bool on = WHOLE || l0 + i < end;
@@ -87,69 +90,97 @@ __global__ __launch_bounds__(256, SP <= 16 ? 3 : 2) void scan_kernel(ScanRun r) 
                 x[i] = on ? widen(xr[i]) : 0.0f;
                 put[i] = step[i] * x[i];
                 if (GATED) z[i] = widen(zr[i]);
-                if (MODE & kEnds) total += step[i];
             }
             wave_sync();
             gv.template put<WHOLE>(bc, l0, len, lane);
             wave_sync();
-            if (WHOLE) {
-                if (l0 + 2 * kP <= end) {
-                    px += kP * in.x.row;
-                    pt += kP * in.dt.row;
-                    pz += kP * in.z.row;
-                    gv.next(in, 1);
-                    load_whole<T, kP>(px, in.x.row, bytes, xr);
-                    load_whole<T, kP>(pt, in.dt.row, bytes, tr);
-                    if (GATED) load_whole<T, kP>(pz, in.z.row, bytes, zr);
-                } else if (l0 + kP < end) {
-                    fetch(l0 + kP);
-                }
-            }
+        };
+        const auto block = [&](auto whole, int l0) {
+            constexpr bool WHOLE = decltype(whole)::value;
             if (MODE & kSave) {
                 float* place = r.saved + quad_at(static_cast<int64_t>(b) * ((in.N + kP - 1) / kP) + l0 / kP, in.S, in.D_, 0, 0);
 #pragma unroll
                 for (int q = 0; q < SP / 4; ++q)
                     *reinterpret_cast<f32x4*>(reinterpret_cast<char*>(place) + quad_bytes(in.D_, q, d)) = f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]};
             }
+            // The next block, or behind the last whole one that one again: without a branch nothing has to wait for it here.
+            if (WHOLE) fetch_whole(l0 + 2 * kP <= end);
+            const f32x4* bc4 = reinterpret_cast<const f32x4*>(bc);
+            constexpr int Q = SP / 4, R = MODE & kOut ? 2 * Q : Q;
+            // Bm and Cm of a position; the next one's are read while this one's are used (up to 16 states: more registers there are not)
+            constexpr bool AHEAD = SP <= 16;
+            f32x4 v[AHEAD ? 2 : 1][AHEAD ? R : 1];
+            if constexpr (AHEAD) {
+#pragma unroll
+                for (int q = 0; q < R; ++q) v[0][q] = bc4[q];
+            }
+            float o[kP];
 #pragma unroll
             for (int i = 0; i < kP; ++i) {
-                const f32x4* B4 = reinterpret_cast<const f32x4*>(bc + i * 2 * SP);
-                const f32x4* C4 = B4 + SP / 4;
+                if constexpr (AHEAD) {
+                    if (i + 1 < kP) {
+#pragma unroll
+                        for (int q = 0; q < R; ++q) v[(i + 1) & 1][q] = bc4[(i + 1) * 2 * Q + q];
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                const auto now = [&](int q) {
+                    if constexpr (AHEAD) return v[i & 1][q];
+                    else return bc4[i * 2 * Q + q];
+                };
                 float y0 = 0.0f, y1 = 0.0f;
 #pragma unroll
-                for (int q = 0; q < SP / 4; ++q) {
-                    const f32x4 Bq = B4[q];
+                for (int q = 0; q < Q; ++q) {
+                    const f32x4 Bq = now(q);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int s = 4 * q + j;
                         h[s] = fmaf(exp2_fast(step[i] * A[s]), h[s], put[i] * Bq[j]);
                     }
-                    if (MODE & kOut) {
-                        const f32x4 Cq = C4[q];
+                    if constexpr ((MODE & kOut) != 0) {
+                        const f32x4 Cq = now(Q + q);
                         y0 = fmaf(h[4 * q], Cq[0], y0);
                         y1 = fmaf(h[4 * q + 1], Cq[1], y1);
                         y0 = fmaf(h[4 * q + 2], Cq[2], y0);
                         y1 = fmaf(h[4 * q + 3], Cq[3], y1);
                     }
                 }
-                y[i] = y0 + y1;
-                asm volatile("" : "+v"(y[i]));  // computed here: moved behind a store's condition, it would keep the states of all eight positions
-            }
-            if (MODE & kOut) {
-                T* to = out + static_cast<int64_t>(l0) * in.D_;
-                unsigned o = bytes;
-                asm volatile("" : "+v"(o));
-#pragma unroll
-                for (int i = 0; i < kP; ++i, to += in.D_) {
-                    const float v = fmaf(skip, x[i], y[i]);
-                    if (WHOLE || l0 + i < end) give(to, o, GATED ? v * z[i] * sigmoid(z[i]) : v);
+                if (MODE & kOut) {
+                    const float y = fmaf(skip, x[i], y0 + y1);
+                    o[i] = GATED ? y * z[i] * sigmoid(z[i]) : y;
+                    asm volatile("" : "+v"(o[i]));  // computed here: moved behind a store's condition, it would keep the states of all eight positions
                 }
             }
+            if (MODE & kEnds) {
+#pragma unroll
+                for (int i = 0; i < kP; ++i) total += step[i];
+            }
+            if (WHOLE) settle(std::true_type{}, l0 + kP);
+            if (MODE & kOut) {
+                T* to = out + static_cast<int64_t>(l0) * in.D_;
+                unsigned at = bytes;
+                asm volatile("" : "+v"(at));
+#pragma unroll
+                for (int i = 0; i < kP; ++i, to += in.D_)
+                    if (WHOLE || l0 + i < end) give(to, at, o[i]);
+            }
         };
-        fetch(begin);
+        gv.place(in, b, begin, group, 0, lane);
         int l0 = begin;
-        for (; l0 + kP <= end; l0 += kP) block(std::true_type{}, l0);
-        if (l0 < end) block(std::false_type{}, l0);
+        if (begin + kP <= end) {
+            fetch_whole(0);
+            settle(std::true_type{}, begin);
+            for (; l0 + kP <= end; l0 += kP) block(std::true_type{}, l0);
+        }
+        if (l0 < end) {
+            gv.place(in, b, l0, group, 0, lane);
+            gv.load(in, l0, len);
+            load_rows<T, kP>(in.x, b, l0, 1, len, bytes, xr);
+            load_rows<T, kP>(in.dt, b, l0, 1, len, bytes, tr);
+            if (GATED) load_rows<T, kP>(in.z, b, l0, 1, len, bytes, zr);
+            settle(std::false_type{}, l0);
+            block(std::false_type{}, l0);
+        }
     }
     if (MODE & kOut)
         for (int l = begin < end ? end : begin; l < stop; ++l)

@@ -116,7 +116,8 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
         T tr[kP], zr[kP], dr[kP];
         GroupVectors<T, SP> gv;
         const int last = begin + (end - begin - 1) / kP * kP;
-        gv.load(in, b, last, len, group, 0, lane);
+        gv.place(in, b, last, group, 0, lane);
+        gv.load(in, last, len);
         load_rows<T, kP>(in.dt, b, last, 1, len, bytes, tr);
         load_rows<T, kP>(r.dout, b, last, 1, len, bytes, dr);
         if (gated) load_rows<T, kP>(in.z, b, last, 1, len, bytes, zr);
@@ -233,7 +234,8 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 4 ? 4 : SW == 1 ? 2 : 3)
                 before[q] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(ps) + (quad + static_cast<unsigned>(q * in.D_) * 16));
         };
         load_before();
-        gv.load(in, b, last, len, group, s0, lane);
+        gv.place(in, b, last, group, s0, lane);
+        gv.load(in, last, len);
         load_rows<T, P>(in.x, b, last + sw, SW, len, bytes, xr);
         load_rows<T, P>(in.dt, b, last + sw, SW, len, bytes, tr);
         load_rows<T, P>(r.dout, b, last + sw, SW, len, bytes, dr);
