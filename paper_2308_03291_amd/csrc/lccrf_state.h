@@ -156,20 +156,23 @@ __device__ __forceinline__ unsigned quad_bytes(int D, int q, int d) { return (st
 
 inline int scan_blocks(int N) { return (N + kP - 1) / kP; }
 
-// Segments: the recursion over a segment needs the state in front of it, which takes a pass of its own over all segments (six
-// tenths of the work again) and a short one along them.  That pays where the waves that the batch has by itself leave
-// most of the chip empty.
-inline ScanPlan scan_plan(int B, int N, int D, int G, int waves_a_tile) {
+// Segments: the recursion over a segment needs the state in front of it, which takes a pass of its own over all segments (seven
+// tenths of the forward work again, two of the gradient's) and a short one along them.  That pays where the waves that the batch has by
+// itself leave most of the chip empty: a lone wave issues an instruction where two issue three, so one segment costs 1.5 a position where
+// the segments of 2048 waves (two a SIMD, `room`; never a few more than that, which would take a third as long again) cost 1.8 over their number.
+inline ScanPlan scan_plan(int B, int N, int D, int G, int waves_a_tile, int room, int least) {
     ScanPlan p;
     p.tiles = (D / G + 63) / 64;
     const int64_t waves = static_cast<int64_t>(B) * G * p.tiles * waves_a_tile;
-    int64_t segments = waves >= 1024 ? 1 : (2048 + waves - 1) / waves;
+    int64_t segments = room / waves;
+    if (segments < least) segments = 1;
     const int64_t most = (N + 63) / 64;
     if (segments > most) segments = most;
     p.seg_len = static_cast<int>(((N + segments - 1) / segments + kP - 1) / kP * kP);
     p.segments = (N + p.seg_len - 1) / p.seg_len;
     return p;
 }
+inline ScanPlan forward_plan(int B, int N, int D, int G) { return scan_plan(B, N, D, G, 1, 2048, 3); }
 
 inline bool scan_fits(int B, int N, int D, int S, int G, const ScanPlan& p) {
     const int64_t most = (int64_t{1} << 32) - 1024, b = B;

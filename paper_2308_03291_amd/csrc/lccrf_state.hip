@@ -21,20 +21,17 @@ struct ScanRun {
     float* ends;   // segments > 1: the states in front of every segment (kEnds: written, what a segment makes of 0)
     float* steps;  // kEnds: sum of the steps [B][segments][D]
     ScanPlan plan;
-    int waves;     // of a workgroup
 };
 
 template <typename T, int SP, int MODE, bool GATED>
-__global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
-    extern __shared__ float lds[];  // [waves][kP][2 * SP]
+__global__ __launch_bounds__(64, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
+    __shared__ float bc[kP * 2 * SP];
     const ScanIn& in = r.in;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int groups_of_tiles = (in.G * r.plan.tiles + r.waves - 1) / r.waves;
-    const unsigned which = blockIdx.x / groups_of_tiles;
-    const int tile = (blockIdx.x - which * groups_of_tiles) * r.waves + wave;
+    const int lane = threadIdx.x, tiles = in.G * r.plan.tiles;
+    const unsigned which = blockIdx.x / tiles;
+    const int tile = blockIdx.x - which * tiles;
     int b = which / r.plan.segments;
     const int seg = which - b * r.plan.segments;
-    if (tile >= in.G * r.plan.tiles) return;
     // Whole sequences, as many waves as there is room for at once: long ones first, then the short ones from the shortest on, so that a
     // SIMD's waves are about as long together everywhere.
     if (r.plan.segments == 1) b = ranked(in.lengths, in.B, in.N, b < (in.B + 1) / 2 ? b : in.B - 1 - (b - (in.B + 1) / 2), lane);
@@ -43,7 +40,6 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
     const int d = group * width + (is ? c0 : width - 1);
     const int len = clamp_length(in.lengths, b, in.N), begin = seg * r.plan.seg_len;
     const int stop = begin + r.plan.seg_len < in.N ? begin + r.plan.seg_len : in.N, end = stop < len ? stop : len;
-    float* bc = lds + wave * (kP * 2 * SP);
     const unsigned bytes = static_cast<unsigned>(d) * sizeof(T);
     T* out = MODE & kOut ? static_cast<T*>(r.out) + static_cast<int64_t>(b) * in.N * in.D_ : nullptr;
     const float skip = in.D ? in.D[d] : 0.0f, bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
@@ -326,9 +322,9 @@ hipError_t step_of(const ScanIn& in, float* state, void* out, hipStream_t st) {
 
 template <typename T, int SP, int MODE>
 void scan_launch(const ScanRun& r, hipStream_t st) {
-    const int64_t wgs = (static_cast<int64_t>(r.in.G) * r.plan.tiles + r.waves - 1) / r.waves;
+    const int64_t waves = static_cast<int64_t>(r.in.G) * r.plan.tiles * r.in.B * r.plan.segments;
     const auto kernel = (MODE & kOut) && r.in.z.data ? scan_kernel<T, SP, MODE, (MODE & kOut) != 0> : scan_kernel<T, SP, MODE, false>;
-    kernel<<<static_cast<unsigned>(wgs * r.in.B * r.plan.segments), 64 * r.waves, sizeof(float) * r.waves * kP * 2 * SP, st>>>(r);
+    kernel<<<static_cast<unsigned>(waves), 64, 0, st>>>(r);  // of one wave each: they go to the SIMDs one by one
 }
 
 template <typename T, int SP>
@@ -368,20 +364,18 @@ hipError_t launch_join_segments(const ScanIn& in, const ScanPlan& p, const float
 size_t scan_saved_bytes(int B, int N, int D, int S) { return up256(static_cast<size_t>(B) * scan_blocks(N) * quads(S) * D * 16); }
 
 size_t scan_workspace(int B, int N, int D, int S, int G) {
-    const ScanPlan p = scan_plan(B, N, D, G, 1);
+    const ScanPlan p = forward_plan(B, N, D, G);
     if (p.segments == 1) return 256;
     return ends_bytes(p, B, D, S) + up256(static_cast<size_t>(B) * p.segments * D * 4);
 }
 
 hipError_t run_state_scan(int dtype, const ScanIn& in, const float* state, void* out, float* final_state, float* saved, void* ws, hipStream_t st) {
-    ScanRun r{in, state, out, final_state, saved, nullptr, nullptr, scan_plan(in.B, in.N, in.D_, in.G, 1), 0};
+    ScanRun r{in, state, out, final_state, saved, nullptr, nullptr, forward_plan(in.B, in.N, in.D_, in.G)};
     if (!scan_fits(in.B, in.N, in.D_, in.S, in.G, r.plan)) return hipErrorInvalidValue;
     if (r.plan.segments > 1) {
         r.ends = static_cast<float*>(ws);
         r.steps = reinterpret_cast<float*>(static_cast<char*>(ws) + ends_bytes(r.plan, in.B, in.D_, in.S));
     }
-    const int all = in.G * r.plan.tiles;
-    r.waves = all < 4 ? all : 4;
     if (dtype) scan_of<uint16_t>(r, st);
     else scan_of<float>(r, st);
     return hipGetLastError();

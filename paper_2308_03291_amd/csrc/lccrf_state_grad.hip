@@ -28,7 +28,7 @@ struct GradPlan {
 GradPlan grad_plan(int B, int N, int D, int S, int G) {
     GradPlan p;
     p.state_waves = S <= 8 ? 1 : S <= 16 ? 2 : S <= 32 ? 4 : 8;
-    p.scan = scan_plan(B, N, D, G, p.state_waves);
+    p.scan = scan_plan(B, N, D, G, p.state_waves, 3072, 2);
     p.tile_waves = p.state_waves >= 4 ? 1 : 4 / p.state_waves;
     while (p.scan.tiles % p.tile_waves) p.tile_waves /= 2;  // no wave without a channel
     p.parts = p.scan.tiles / p.tile_waves;
@@ -87,22 +87,19 @@ __device__ __forceinline__ float through_gate(float dout, float z, bool gated) {
 
 // What a segment makes of 0 behind it, and the sum of its steps.
 template <typename T, int SP>
-__global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
-    extern __shared__ float lds[];  // [waves][kP][2 * SP]
+__global__ __launch_bounds__(64, 2) void back_ends_kernel(GradRun r) {
+    __shared__ float bc[kP * 2 * SP];
     const ScanIn& in = r.in;
     const ScanPlan& plan = r.plan.scan;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int tiles = in.G * plan.tiles, groups_of_tiles = (tiles + waves - 1) / waves;
-    const unsigned which = blockIdx.x / groups_of_tiles;
-    const int tile = (blockIdx.x - which * groups_of_tiles) * waves + wave;
+    const int lane = threadIdx.x, tiles = in.G * plan.tiles;
+    const unsigned which = blockIdx.x / tiles;
+    const int tile = blockIdx.x - which * tiles;
     const int b = which / plan.segments, seg = which - b * plan.segments;
-    if (tile >= tiles) return;
     const int width = in.D_ / in.G, group = tile / plan.tiles, c0 = (tile - group * plan.tiles) * 64 + lane;
     const bool is = c0 < width;
     const int d = group * width + (is ? c0 : width - 1);
     const int len = clamp_length(in.lengths, b, in.N), begin = seg * plan.seg_len;
     const int stop = begin + plan.seg_len < in.N ? begin + plan.seg_len : in.N, end = stop < len ? stop : len;
-    float* bc = lds + wave * (kP * 2 * SP);
     const bool gated = in.z.data != nullptr;
     const unsigned bytes = static_cast<unsigned>(d) * sizeof(T);
     const float bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
@@ -481,9 +478,8 @@ Carve carve(int B, int N, int D, int S, int G, bool with_saved) {
 
 template <typename T, int SP>
 void back_ends(const GradRun& r, hipStream_t st) {
-    const int64_t tiles = static_cast<int64_t>(r.in.G) * r.plan.scan.tiles, waves = tiles < 4 ? tiles : 4;
-    const int64_t blocks = (tiles + waves - 1) / waves * r.in.B * r.plan.scan.segments;
-    back_ends_kernel<T, SP><<<static_cast<unsigned>(blocks), 64 * waves, sizeof(float) * waves * kP * 2 * SP, st>>>(r);
+    const int64_t waves = static_cast<int64_t>(r.in.G) * r.plan.scan.tiles * r.in.B * r.plan.scan.segments;
+    back_ends_kernel<T, SP><<<static_cast<unsigned>(waves), 64, 0, st>>>(r);
 }
 
 template <typename T, int SP, int SW>
