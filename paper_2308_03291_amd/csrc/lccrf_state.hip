@@ -24,12 +24,14 @@ struct ScanRun {
 };
 
 template <typename T, int SP, int MODE, bool GATED>
-__global__ __launch_bounds__(64, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
-    __shared__ float bc[kP * 2 * SP];
+__global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
+    extern __shared__ float lds[];  // [waves][kP][2 * SP]
     const ScanIn& in = r.in;
-    const int lane = threadIdx.x, tiles = in.G * r.plan.tiles;
-    const unsigned which = blockIdx.x / tiles;
-    const int tile = blockIdx.x - which * tiles;
+    const int lane = threadIdx.x & 63, tiles = in.G * r.plan.tiles;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned at_work = blockIdx.x * (blockDim.x >> 6) + wave, which = at_work / tiles;
+    const int tile = at_work - which * tiles;
+    float* bc = lds + wave * (kP * 2 * SP);
     int b = which / r.plan.segments;
     const int seg = which - b * r.plan.segments;
     // Whole sequences, as many waves as there is room for at once: long ones first, then the short ones from the shortest on, so that a
@@ -324,7 +326,8 @@ template <typename T, int SP, int MODE>
 void scan_launch(const ScanRun& r, hipStream_t st) {
     const int64_t waves = static_cast<int64_t>(r.in.G) * r.plan.tiles * r.in.B * r.plan.segments;
     const auto kernel = (MODE & kOut) && r.in.z.data ? scan_kernel<T, SP, MODE, (MODE & kOut) != 0> : scan_kernel<T, SP, MODE, false>;
-    kernel<<<static_cast<unsigned>(waves), 64, 0, st>>>(r);  // of one wave each: they go to the SIMDs one by one
+    const int w = waves_together(r.in.G * r.plan.tiles);
+    kernel<<<static_cast<unsigned>(waves / w), 64 * w, sizeof(float) * w * kP * 2 * SP, st>>>(r);
 }
 
 template <typename T, int SP>

@@ -87,13 +87,15 @@ __device__ __forceinline__ float through_gate(float dout, float z, bool gated) {
 
 // What a segment makes of 0 behind it, and the sum of its steps.
 template <typename T, int SP>
-__global__ __launch_bounds__(64, 2) void back_ends_kernel(GradRun r) {
-    __shared__ float bc[kP * 2 * SP];
+__global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
+    extern __shared__ float lds[];  // [waves][kP][2 * SP]
     const ScanIn& in = r.in;
     const ScanPlan& plan = r.plan.scan;
-    const int lane = threadIdx.x, tiles = in.G * plan.tiles;
-    const unsigned which = blockIdx.x / tiles;
-    const int tile = blockIdx.x - which * tiles;
+    const int lane = threadIdx.x & 63, tiles = in.G * plan.tiles;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned at_work = blockIdx.x * (blockDim.x >> 6) + wave, which = at_work / tiles;
+    const int tile = at_work - which * tiles;
+    float* bc = lds + wave * (kP * 2 * SP);
     const int b = which / plan.segments, seg = which - b * plan.segments;
     const int width = in.D_ / in.G, group = tile / plan.tiles, c0 = (tile - group * plan.tiles) * 64 + lane;
     const bool is = c0 < width;
@@ -479,7 +481,8 @@ Carve carve(int B, int N, int D, int S, int G, bool with_saved) {
 template <typename T, int SP>
 void back_ends(const GradRun& r, hipStream_t st) {
     const int64_t waves = static_cast<int64_t>(r.in.G) * r.plan.scan.tiles * r.in.B * r.plan.scan.segments;
-    back_ends_kernel<T, SP><<<static_cast<unsigned>(waves), 64, 0, st>>>(r);
+    const int w = waves_together(r.in.G * r.plan.scan.tiles);
+    back_ends_kernel<T, SP><<<static_cast<unsigned>(waves / w), 64 * w, sizeof(float) * w * kP * 2 * SP, st>>>(r);
 }
 
 template <typename T, int SP, int SW>
