@@ -50,7 +50,7 @@ template <typename T, int W, bool SMALL = false> struct Piece {
             }
         }
     }
-    static __device__ __forceinline__ void put(T* p, int, const float (&o)[W]) {
+    template <bool STREAM = false> static __device__ __forceinline__ void put(T* p, int, const float (&o)[W]) {
         Vec v;
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -59,7 +59,8 @@ template <typename T, int W, bool SMALL = false> struct Piece {
 #pragma unroll
             for (int i = 0; i < W / 2; ++i) v[i] = to_bf16(o[2 * i]) | static_cast<uint32_t>(to_bf16(o[2 * i + 1])) << 16;
         }
-        *reinterpret_cast<Any*>(p) = v;
+        if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<Any*>(p));
+        else *reinterpret_cast<Any*>(p) = v;
     }
 };
 template <typename T, int W> struct Piece<T, W, true> {
@@ -72,7 +73,7 @@ template <typename T, int W> struct Piece<T, W, true> {
 #pragma unroll
         for (int i = 0; i < W; ++i) o[i] = widen(raw[i]);
     }
-    static __device__ __forceinline__ void put(T* p, int D, const float (&o)[W]) {
+    template <bool STREAM = false> static __device__ __forceinline__ void put(T* p, int D, const float (&o)[W]) {
 #pragma unroll
         for (int i = 0; i < W; ++i)
             if (i < D) put1(p + i, o[i]);
