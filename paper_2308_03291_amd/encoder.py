@@ -12,6 +12,7 @@ contiguous, and so are results.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -23,17 +24,12 @@ MIN_TAPS, MAX_TAPS, MAX_STATES = 2, 8, 64
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-class _Rows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("row", ctypes.c_int64)]
-
-
-class _ScanInputs(ctypes.Structure):
-    _fields_ = [("x", _Rows), ("dt", _Rows), ("Bm", _Rows), ("Cm", _Rows), ("z", _Rows), ("b_group", ctypes.c_int64),
-                ("c_group", ctypes.c_int64), ("A", ctypes.c_void_p), ("D", ctypes.c_void_p), ("dt_bias", ctypes.c_void_p)]
-
-
-class _ScanGrads(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_void_p) for n in ("dx", "ddt", "dBm", "dCm", "dz", "dA", "dD", "ddt_bias", "dstate")]
+# A call for one token takes the GPU a few microseconds, so the host's part of it counts: the argument blocks of the C ABI (lccrf_rows,
+# lccrf_scan_inputs, lccrf_scan_grads: nothing but 8-byte fields) are filled as arrays in one go, devices are compared by their numbers, sizes
+# of workspaces are asked for once (lccrf_state_step, B=4 D=1024 S=16: 15.2 us of host work -> 11).
+_Rows = ctypes.c_int64 * 3         # address, elements between sequences, elements between positions
+_ScanInputs = ctypes.c_int64 * 20  # x, dt, Bm, Cm, z as _Rows, elements between groups of Bm and Cm, A, D, dt_bias
+_ScanGrads = ctypes.c_int64 * 9    # dx, ddt, dBm, dCm, dz, dA, dD, ddt_bias, dstate
 
 
 def declare(lib) -> None:
@@ -62,39 +58,64 @@ def declare(lib) -> None:
         getattr(lib, name).restype = sz
 
 
-def _type(t: torch.Tensor, name: str) -> int:
+def _lib():
+    return _b._lib or _b.load_library()
+
+
+@functools.lru_cache(maxsize=4096)
+def _bytes(name: str, *sizes: int) -> int:
+    return getattr(_b.load_library(), name)(*sizes)
+
+
+def _first(t: torch.Tensor, name: str):
+    """(dtype's code, dtype, device number) of the tensor that the others have to go with."""
     dt = _DTYPES.get(t.dtype)
     if dt is None:
         raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    if not t.is_cuda:
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError(f"{name} must live on the GPU")
-    return dt
+    return dt, t.dtype, dev
 
 
-def _activation(t: torch.Tensor, name: str, shape, like: torch.Tensor) -> None:
-    """An input whose last dimension is dense."""
-    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{name} must be {like.dtype} {list(shape)} on {like.device}, got {t.dtype} {list(t.shape)} on {t.device}")
-    if t.stride(-1) != 1 and shape[-1] > 1:
+def _activation(t: torch.Tensor, name: str, shape, dtype, dev: int):
+    """The strides of an input whose last dimension is dense."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be {dtype} {list(shape)} on GPU {dev}, got {t.dtype} {list(t.shape)} on {t.device}")
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}'s last dimension must be dense")
+    return strides
 
 
-def _dense(t: Optional[torch.Tensor], name: str, shape, dtype, device, optional: bool = False) -> Optional[int]:
-    """A contiguous tensor's address; None for one that is not there."""
+def _dense(t: Optional[torch.Tensor], name: str, shape, dtype, dev: int, optional: bool = False) -> int:
+    """A contiguous tensor's address; 0 for one that is not there."""
     if t is None:
         if optional:
-            return None
+            return 0
         raise ValueError(f"{name} is missing")
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on {device}")
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on GPU {dev}")
     return t.data_ptr()
 
 
-def _result(t: Optional[torch.Tensor], name: str, shape, dtype, device) -> torch.Tensor:
+def _result(t: Optional[torch.Tensor], name: str, shape, dtype, device, dev: int) -> torch.Tensor:
     if t is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    _dense(t, name, shape, dtype, device)
+    _dense(t, name, shape, dtype, dev)
     return t
+
+
+def _result_like(t: Optional[torch.Tensor], name: str, x: torch.Tensor, dev: int) -> torch.Tensor:
+    """A result of x's shape and type (empty_like takes half of empty's two microseconds; other strides than x's it must not take over)."""
+    if t is None:
+        return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _dense(t, name, x.shape, x.dtype, dev)
+    return t
+
+
+def _lengths(lengths: Optional[torch.Tensor], B: int, dev: int) -> int:
+    return _dense(lengths, "lengths", (B,), torch.int32, dev, True)
 
 
 def _scratch(need: int, what: str, device, workspace: Optional[torch.Tensor]) -> torch.Tensor:
@@ -107,23 +128,29 @@ def _scratch(need: int, what: str, device, workspace: Optional[torch.Tensor]) ->
     return workspace
 
 
-def _rows(t: torch.Tensor) -> _Rows:
-    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+def _call(name: str, dev: int, call, *args) -> None:
+    """call(*args, the current stream) with GPU `dev` current; raises if it reports an error."""
+    if _b._current_device() == dev:
+        rc = call(*args, _b._raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = call(*args, _b._raw_stream(dev))
+    if rc != 0:
+        _b._check(rc, name)
 
 
 def lccrf_embed(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """scale * table[ids]: table [V, D] (rows dense), ids int32 of any shape, contiguous; the result has one dimension, D, more.
     Ids outside [0, V) (padding) give rows of 0."""
-    dt = _type(table, "table")
+    dt, dtype, dev = _first(table, "table")
     if table.dim() != 2 or 0 in table.shape:
         raise ValueError(f"table must be [V, D], got {list(table.shape)}")
     V, D = table.shape
-    _activation(table, "table", table.shape, table)
-    dev = table.device
-    pids = _dense(ids, "ids", ids.shape, torch.int32, dev)
-    out = _result(out, "out", (*ids.shape, D), table.dtype, dev)
-    _b._enqueue("lccrf_embed", dev, _b.load_library().lccrf_embed, table.data_ptr(), dt, V, D, table.stride(0), pids, ids.numel(), scale, out.data_ptr(),
-                _b._stream(dev))
+    row = _activation(table, "table", table.shape, dtype, dev)[0]
+    shape = ids.shape
+    pids = _dense(ids, "ids", shape, torch.int32, dev)
+    out = _result(out, "out", (*shape, D), dtype, table.device, dev)
+    _call("lccrf_embed", dev, _lib().lccrf_embed, table.data_ptr(), dt, V, D, row, pids, ids.numel(), scale, out.data_ptr())
     return out
 
 
@@ -131,33 +158,35 @@ def lccrf_embed_grad(dout: torch.Tensor, ids: torch.Tensor, V: int, *, scale: fl
                      workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of ``lccrf_embed`` by its table, [V, D] in dout's dtype: every row is scale times the sum, in a fixed order, of the
     rows of dout [B, N, D] (or [n, D]) whose id (int32 [B, N] or [n]) it is; ids outside [0, V) have none."""
-    dt = _type(dout, "dout")
+    dt, dtype, dev = _first(dout, "dout")
     if dout.dim() == 2:
         dout, ids = dout[None], ids[None]
-    if dout.dim() != 3 or dout.shape[2] == 0 or V < 1:
-        raise ValueError(f"dout must be [B, N, D] and V positive, got {list(dout.shape)} and {V}")
-    B, N, D = dout.shape
-    _activation(dout, "dout", dout.shape, dout)
-    dev, lib = dout.device, _b.load_library()
+    shape = dout.shape
+    if len(shape) != 3 or shape[2] == 0 or V < 1:
+        raise ValueError(f"dout must be [B, N, D] and V positive, got {list(shape)} and {V}")
+    B, N, D = shape
+    strides = _activation(dout, "dout", shape, dtype, dev)
     pids = _dense(ids, "ids", (B, N), torch.int32, dev)
-    out = _result(out, "out", (V, D), dout.dtype, dev)
-    ws = _scratch(lib.lccrf_embed_grad_workspace_bytes(B * N, V, D), "lccrf_embed_grad", dev, workspace)
-    _b._enqueue("lccrf_embed_grad", dev, lib.lccrf_embed_grad, ctypes.byref(_rows(dout)), dt, pids, B, N, V, D, scale, out.data_ptr(), ws.data_ptr(), ws.numel(),
-                _b._stream(dev))
+    device = dout.device
+    out = _result(out, "out", (V, D), dtype, device, dev)
+    ws = _scratch(_bytes("lccrf_embed_grad_workspace_bytes", B * N, V, D), "lccrf_embed_grad", device, workspace)
+    _call("lccrf_embed_grad", dev, _lib().lccrf_embed_grad, _Rows(dout.data_ptr(), strides[0], strides[1]), dt, pids, B, N, V, D, scale, out.data_ptr(),
+          ws.data_ptr(), ws.numel())
     return out
 
 
 def _conv_args(x: torch.Tensor, weight: torch.Tensor, bias, state):
-    dt = _type(x, "x")
-    D = x.shape[-1]
-    if weight.dim() != 2 or 0 in x.shape:
-        raise ValueError(f"x must be [B, N, D] (one position: [B, D]) and weight [D, K], got {list(x.shape)} and {list(weight.shape)}")
-    K = weight.shape[1]
+    """Checks what all calls of the convolution share; (dtype's code, device number, D, K, strides of x, the others' addresses)."""
+    dt, dtype, dev = _first(x, "x")
+    shape = x.shape
+    if weight.dim() != 2 or 0 in shape:
+        raise ValueError(f"x must be [B, N, D] (one position: [B, D]) and weight [D, K], got {list(shape)} and {list(weight.shape)}")
+    D, K = shape[-1], weight.shape[1]
     if not MIN_TAPS <= K <= MAX_TAPS:
         raise ValueError(f"{MIN_TAPS} to {MAX_TAPS} taps are served, got {K}")
-    _activation(x, "x", x.shape, x)
-    return (dt, D, K, _dense(weight, "weight", (D, K), torch.float32, x.device), _dense(bias, "bias", (D,), torch.float32, x.device, True),
-            _dense(state, "state", (x.shape[0], K - 1, D), x.dtype, x.device, True))
+    strides = _activation(x, "x", shape, dtype, dev)
+    return (dt, dev, D, K, strides, _dense(weight, "weight", (D, K), torch.float32, dev), _dense(bias, "bias", (D,), torch.float32, dev, True),
+            _dense(state, "state", (shape[0], K - 1, D), dtype, dev, True))
 
 
 def lccrf_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None, *,
@@ -167,13 +196,12 @@ def lccrf_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
     on.  Positions past the lengths give 0.  ``final`` must be another tensor than ``state``."""
     if x.dim() != 3:
         raise ValueError(f"x must be [B, N, D], got {list(x.shape)}")
-    dt, D, K, pw, pb, ps = _conv_args(x, weight, bias, state)
-    B, N, dev = x.shape[0], x.shape[1], x.device
-    plen = _b._len_ptr(lengths, B, dev)
-    out = _result(out, "out", (B, N, D), x.dtype, dev)
-    final = _result(final, "final", (B, K - 1, D), x.dtype, dev)
-    _b._enqueue("lccrf_conv", dev, _b.load_library().lccrf_conv, ctypes.byref(_rows(x)), dt, pw, pb, ps, plen, B, N, D, K, out.data_ptr(), final.data_ptr(),
-                _b._stream(dev))
+    dt, dev, D, K, strides, pw, pb, ps = _conv_args(x, weight, bias, state)
+    (B, N, _), device = x.shape, x.device
+    plen = _lengths(lengths, B, dev)
+    out = _result_like(out, "out", x, dev)
+    final = _result(final, "final", (B, K - 1, D), x.dtype, device, dev)
+    _call("lccrf_conv", dev, _lib().lccrf_conv, _Rows(x.data_ptr(), strides[0], strides[1]), dt, pw, pb, ps, plen, B, N, D, K, out.data_ptr(), final.data_ptr())
     return out, final
 
 
@@ -191,15 +219,17 @@ def lccrf_conv_grad(dout: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, b
     not part of it); ``dbias`` and ``dstate`` are None where there is no bias or state."""
     if x.dim() != 3:
         raise ValueError(f"x must be [B, N, D], got {list(x.shape)}")
-    dt, D, K, pw, pb, ps = _conv_args(x, weight, bias, state)
-    _activation(dout, "dout", x.shape, x)
-    B, N, dev, lib = x.shape[0], x.shape[1], x.device, _b.load_library()
-    plen = _b._len_ptr(lengths, B, dev)
-    g = ConvGrad(torch.empty((B, N, D), dtype=x.dtype, device=dev), torch.empty((D, K), device=dev),
-                 None if bias is None else torch.empty((D,), device=dev), None if state is None else torch.empty((B, K - 1, D), dtype=x.dtype, device=dev))
-    ws = _scratch(lib.lccrf_conv_grad_workspace_bytes(B, N, D, K), "lccrf_conv_grad", dev, workspace)
-    _b._enqueue("lccrf_conv_grad", dev, lib.lccrf_conv_grad, ctypes.byref(_rows(dout)), ctypes.byref(_rows(x)), dt, pw, pb, ps, plen, B, N, D, K,
-                *(None if t is None else t.data_ptr() for t in g), ws.data_ptr(), ws.numel(), _b._stream(dev))
+    dt, dev, D, K, strides, pw, pb, ps = _conv_args(x, weight, bias, state)
+    shape, dtype, device, f32 = x.shape, x.dtype, x.device, torch.float32
+    dstrides = _activation(dout, "dout", shape, dtype, dev)
+    B, N, _ = shape
+    plen = _lengths(lengths, B, dev)
+    g = ConvGrad(torch.empty(shape, dtype=dtype, device=device), torch.empty((D, K), dtype=f32, device=device),
+                 None if bias is None else torch.empty((D,), dtype=f32, device=device),
+                 None if state is None else torch.empty((B, K - 1, D), dtype=dtype, device=device))
+    ws = _scratch(_bytes("lccrf_conv_grad_workspace_bytes", B, N, D, K), "lccrf_conv_grad", device, workspace)
+    _call("lccrf_conv_grad", dev, _lib().lccrf_conv_grad, _Rows(dout.data_ptr(), dstrides[0], dstrides[1]), _Rows(x.data_ptr(), strides[0], strides[1]), dt, pw, pb,
+          ps, plen, B, N, D, K, *[0 if t is None else t.data_ptr() for t in g], ws.data_ptr(), ws.numel())
     return g
 
 
@@ -210,40 +240,37 @@ def lccrf_conv_step(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.
         raise ValueError(f"x must be [B, D], got {list(x.shape)}")
     if state is None:
         raise ValueError("state is missing")
-    dt, D, K, pw, pb, ps = _conv_args(x, weight, bias, state)
-    out = _result(out, "out", x.shape, x.dtype, x.device)
-    _b._enqueue("lccrf_conv_step", x.device, _b.load_library().lccrf_conv_step, x.data_ptr(), x.stride(0), dt, pw, pb, ps, x.shape[0], D, K, out.data_ptr(),
-                _b._stream(x.device))
+    dt, dev, D, K, strides, pw, pb, ps = _conv_args(x, weight, bias, state)
+    shape = x.shape
+    out = _result_like(out, "out", x, dev)
+    _call("lccrf_conv_step", dev, _lib().lccrf_conv_step, x.data_ptr(), strides[0], dt, pw, pb, ps, shape[0], D, K, out.data_ptr())
     return out
 
 
 def _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias):
-    """Checks what all calls of the scan share; (dtype, D, S, G, the inputs' block)."""
-    code = _type(x, "x")
-    if 0 in x.shape or A.dim() != 2 or Bm.dim() != x.dim() + 1:
-        raise ValueError(f"x must be [B, N, D], A [D, S] and Bm [B, N, G, S] (one position: [B, D] and [B, G, S]), got {list(x.shape)}, {list(A.shape)} "
+    """Checks what all calls of the scan share; (dtype's code, device number, channels, S, G, shape of x, dtype, the inputs' block)."""
+    code, dtype, dev = _first(x, "x")
+    shape = x.shape
+    if 0 in shape or A.dim() != 2 or Bm.dim() != len(shape) + 1:
+        raise ValueError(f"x must be [B, N, D], A [D, S] and Bm [B, N, G, S] (one position: [B, D] and [B, G, S]), got {list(shape)}, {list(A.shape)} "
                          f"and {list(Bm.shape)}")
-    width, S, G, dev, one = x.shape[-1], A.shape[1], Bm.shape[-2], x.device, x.dim() == 2
+    width, S, G = shape[-1], A.shape[1], Bm.shape[-2]
     if not 1 <= S <= MAX_STATES:
         raise ValueError(f"1 to {MAX_STATES} states a channel are served, got {S}")
     if G < 1 or width % G:
         raise ValueError(f"{width} channels cannot be shared by {G} groups")
-    _activation(x, "x", x.shape, x)
-    _activation(dt, "dt", x.shape, x)
-    vectors = (*x.shape[:-1], G, S)
-    _activation(Bm, "Bm", vectors, x)
-    _activation(Cm, "Cm", vectors, x)
-    if z is not None:
-        _activation(z, "z", x.shape, x)
+    xs, ts = _activation(x, "x", shape, dtype, dev), _activation(dt, "dt", shape, dtype, dev)
+    vectors = (*shape[:-1], G, S)
+    bs, cs = _activation(Bm, "Bm", vectors, dtype, dev), _activation(Cm, "Cm", vectors, dtype, dev)
+    if z is None:
+        pz, zs = 0, (0, 0)
+    else:
+        pz, zs = z.data_ptr(), _activation(z, "z", shape, dtype, dev)
     f32 = torch.float32
-    pA, pD, pb = _dense(A, "A", (width, S), f32, dev), _dense(D, "D", (width,), f32, dev, True), _dense(dt_bias, "dt_bias", (width,), f32, dev, True)
-
-    def rows(t):
-        if t is None:
-            return _Rows(None, 0, 0)
-        return _Rows(t.data_ptr(), t.stride(0), 0 if one else t.stride(1))
-
-    return code, width, S, G, _ScanInputs(rows(x), rows(dt), rows(Bm), rows(Cm), rows(z), Bm.stride(-2), Cm.stride(-2), pA, pD, pb)
+    # (one position: the second stride is that of the channels, which nothing looks at)
+    return code, dev, width, S, G, shape, dtype, _ScanInputs(
+        x.data_ptr(), xs[0], xs[1], dt.data_ptr(), ts[0], ts[1], Bm.data_ptr(), bs[0], bs[1], Cm.data_ptr(), cs[0], cs[1], pz, zs[0], zs[1],
+        bs[-2], cs[-2], _dense(A, "A", (width, S), f32, dev), _dense(D, "D", (width,), f32, dev, True), _dense(dt_bias, "dt_bias", (width,), f32, dev, True))
 
 
 def state_scan_saved(x: torch.Tensor, A: torch.Tensor) -> torch.Tensor:
@@ -251,15 +278,14 @@ def state_scan_saved(x: torch.Tensor, A: torch.Tensor) -> torch.Tensor:
     again.  To be kept until ``lccrf_state_scan_grad`` has it; its layout is the library's."""
     if x.dim() != 3 or A.dim() != 2 or A.shape[0] != x.shape[2]:
         raise ValueError(f"x must be [B, N, D] and A [D, S], got {list(x.shape)} and {list(A.shape)}")
-    need = _b.load_library().lccrf_state_scan_saved_bytes(*x.shape, A.shape[1])
-    return _scratch(need, "state_scan_saved", x.device, None)
+    return _scratch(_bytes("lccrf_state_scan_saved_bytes", *x.shape, A.shape[1]), "state_scan_saved", x.device, None)
 
 
-def _saved_ptr(saved, x, S) -> Optional[int]:
+def _saved_ptr(saved, shape, S, dev: int) -> int:
     if saved is None:
-        return None
-    if saved.dtype != torch.uint8 or saved.device != x.device or not saved.is_contiguous() or \
-            saved.numel() < _b.load_library().lccrf_state_scan_saved_bytes(*x.shape, S):
+        return 0
+    if saved.dtype != torch.uint8 or saved.get_device() != dev or not saved.is_contiguous() or \
+            saved.numel() < _bytes("lccrf_state_scan_saved_bytes", *shape, S):
         raise ValueError("saved must come from state_scan_saved for tensors of these shapes")
     return saved.data_ptr()
 
@@ -276,16 +302,16 @@ def lccrf_state_scan(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, Bm: tor
     the first position (0 without it); ``final`` after the last one within the length, and may be ``state`` itself."""
     if x.dim() != 3:
         raise ValueError(f"x must be [B, N, D], got {list(x.shape)}")
-    code, width, S, G, block = _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias)
-    B, N, dev, lib = x.shape[0], x.shape[1], x.device, _b.load_library()
-    plen = _b._len_ptr(lengths, B, dev)
-    pstate = _dense(state, "state", (B, width, S), torch.float32, dev, True)
-    psaved = _saved_ptr(saved, x, S)
-    out = _result(out, "out", (B, N, width), x.dtype, dev)
-    final = _result(final, "final", (B, width, S), torch.float32, dev)
-    ws = _scratch(lib.lccrf_state_scan_workspace_bytes(B, N, width, S, G), "lccrf_state_scan", dev, workspace)
-    _b._enqueue("lccrf_state_scan", dev, lib.lccrf_state_scan, ctypes.byref(block), code, plen, B, N, width, S, G, pstate, out.data_ptr(), final.data_ptr(), psaved,
-                ws.data_ptr(), ws.numel(), _b._stream(dev))
+    code, dev, width, S, G, shape, dtype, block = _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias)
+    (B, N, _), device, f32 = shape, x.device, torch.float32
+    plen = _lengths(lengths, B, dev)
+    pstate = _dense(state, "state", (B, width, S), f32, dev, True)
+    psaved = _saved_ptr(saved, shape, S, dev)
+    out = _result_like(out, "out", x, dev)
+    final = _result(final, "final", (B, width, S), f32, device, dev)
+    ws = _scratch(_bytes("lccrf_state_scan_workspace_bytes", B, N, width, S, G), "lccrf_state_scan", device, workspace)
+    _call("lccrf_state_scan", dev, _lib().lccrf_state_scan, block, code, plen, B, N, width, S, G, pstate, out.data_ptr(), final.data_ptr(), psaved, ws.data_ptr(),
+          ws.numel())
     return out, final
 
 
@@ -310,24 +336,23 @@ def lccrf_state_scan_grad(dout: torch.Tensor, x: torch.Tensor, dt: torch.Tensor,
     again.  dBm and dCm are sums over the channels of their group."""
     if x.dim() != 3:
         raise ValueError(f"x must be [B, N, D], got {list(x.shape)}")
-    code, width, S, G, block = _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias)
-    _activation(dout, "dout", x.shape, x)
-    B, N, dev, lib = x.shape[0], x.shape[1], x.device, _b.load_library()
-    plen = _b._len_ptr(lengths, B, dev)
-    pstate = _dense(state, "state", (B, width, S), torch.float32, dev, True)
-    psaved = _saved_ptr(saved, x, S)
+    code, dev, width, S, G, shape, dtype, block = _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias)
+    strides = _activation(dout, "dout", shape, dtype, dev)
+    (B, N, _), device, f32 = shape, x.device, torch.float32
+    plen = _lengths(lengths, B, dev)
+    pstate = _dense(state, "state", (B, width, S), f32, dev, True)
+    psaved = _saved_ptr(saved, shape, S, dev)
 
     def like(shape, dtype, wanted=True):
-        return torch.empty(shape, dtype=dtype, device=dev) if wanted else None
+        return torch.empty(shape, dtype=dtype, device=device) if wanted else None
 
-    f32, rows, vectors = torch.float32, (B, N, width), (B, N, G, S)
-    g = ScanGrad(like(rows, x.dtype), like(rows, x.dtype), like(vectors, x.dtype), like(vectors, x.dtype), like(rows, x.dtype, z is not None),
+    vectors = (B, N, G, S)
+    g = ScanGrad(like(shape, dtype), like(shape, dtype), like(vectors, dtype), like(vectors, dtype), like(shape, dtype, z is not None),
                  like((width, S), f32), like((width,), f32, D is not None), like((width,), f32, dt_bias is not None),
                  like((B, width, S), f32, state is not None))
-    ws = _scratch(lib.lccrf_state_scan_grad_workspace_bytes(B, N, width, S, G, saved is not None), "lccrf_state_scan_grad", dev, workspace)
-    grads = _ScanGrads(*(None if t is None else t.data_ptr() for t in g))
-    _b._enqueue("lccrf_state_scan_grad", dev, lib.lccrf_state_scan_grad, ctypes.byref(_rows(dout)), ctypes.byref(block), code, plen, B, N, width, S, G, pstate, psaved,
-                ctypes.byref(grads), ws.data_ptr(), ws.numel(), _b._stream(dev))
+    ws = _scratch(_bytes("lccrf_state_scan_grad_workspace_bytes", B, N, width, S, G, int(saved is not None)), "lccrf_state_scan_grad", device, workspace)
+    _call("lccrf_state_scan_grad", dev, _lib().lccrf_state_scan_grad, _Rows(dout.data_ptr(), strides[0], strides[1]), block, code, plen, B, N, width, S, G, pstate,
+          psaved, _ScanGrads(*[0 if t is None else t.data_ptr() for t in g]), ws.data_ptr(), ws.numel())
     return g
 
 
@@ -337,9 +362,9 @@ def lccrf_state_step(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, Bm: tor
     """One position of every stream: x, dt, z [B, D], Bm, Cm [B, G, S]; state float32 [B, D, S] moves on in place; the result is [B, D]."""
     if x.dim() != 2:
         raise ValueError(f"x must be [B, D], got {list(x.shape)}")
-    code, width, S, G, block = _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias)
-    B, dev = x.shape[0], x.device
+    code, dev, width, S, G, shape, dtype, block = _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias)
+    B = shape[0]
     pstate = _dense(state, "state", (B, width, S), torch.float32, dev)
-    out = _result(out, "out", x.shape, x.dtype, dev)
-    _b._enqueue("lccrf_state_step", dev, _b.load_library().lccrf_state_step, ctypes.byref(block), code, B, width, S, G, pstate, out.data_ptr(), _b._stream(dev))
+    out = _result_like(out, "out", x, dev)
+    _call("lccrf_state_step", dev, _lib().lccrf_state_step, block, code, B, width, S, G, pstate, out.data_ptr())
     return out

@@ -22,12 +22,12 @@ def lib():
 
 
 def rows(data=FAKE):
-    return ctypes.byref(encoder._Rows(data, 8, 8))
+    return encoder._Rows(data or 0, 8, 8)
 
 
 def inputs(x=FAKE, dt=FAKE, Bm=FAKE, Cm=FAKE, z=None, A=FAKE, D=FAKE, dt_bias=FAKE):
-    R = encoder._Rows
-    return encoder._ScanInputs(R(x, 8, 8), R(dt, 8, 8), R(Bm, 8, 8), R(Cm, 8, 8), R(z, 8, 8), 8, 8, A, D, dt_bias)
+    rows = [v for p in (x, dt, Bm, Cm, z) for v in (p or 0, 8, 8)]
+    return encoder._ScanInputs(*rows, 8, 8, A or 0, D or 0, dt_bias or 0)
 
 
 def test_embed_refuses(lib):
@@ -117,7 +117,7 @@ def test_scan_refuses(lib):
     def grad(block=None, dout=rows(), state=FAKE, saved=FAKE, n=small, S=16, **other):
         names = ("dx", "ddt", "dBm", "dCm", "dz", "dA", "dD", "ddt_bias", "dstate")
         values = {k: FAKE for k in names} | {"dz": None} | other
-        return g(dout, ctypes.byref(block or inputs()), 0, None, 2, 4, 8, S, 2, state, saved, ctypes.byref(encoder._ScanGrads(*values.values())), FAKE, n, None)
+        return g(dout, ctypes.byref(block or inputs()), 0, None, 2, 4, 8, S, 2, state, saved, encoder._ScanGrads(*[v or 0 for v in values.values()]), FAKE, n, None)
 
     assert [grad(S=65), grad(dz=FAKE), grad(inputs(z=FAKE)), grad(state=None)] == [EINVAL] * 4
     assert [grad(dout=None), grad(dx=None), grad(ddt=None), grad(dBm=None), grad(dCm=None), grad(dA=None)] == [ENULL] * 6

@@ -28,7 +28,7 @@ def crf():
 def _dirty_memory(monkeypatch):
     """What the binding allocates starts as all-ones bytes (NaN, -1): nothing may rely on what memory held, or leave it."""
     from paper_2308_03291_amd import encoder
-    empty = torch.empty
+    empty, empty_like = torch.empty, torch.empty_like
 
     class Dirty:
         def __getattr__(self, name):
@@ -38,6 +38,12 @@ def _dirty_memory(monkeypatch):
         def empty(*a, **k):
             t = empty(*a, **k)
             t.view(torch.uint8).fill_(0xFF) if t.numel() else None
+            return t
+
+        @staticmethod
+        def empty_like(x):
+            t = empty_like(x)
+            t.view(torch.uint8).fill_(0xFF)
             return t
 
     monkeypatch.setattr(encoder, "torch", Dirty())
