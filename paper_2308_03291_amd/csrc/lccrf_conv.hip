@@ -56,7 +56,7 @@ __device__ __forceinline__ void taps_of(const ConvArgs& a, int c, float (&w)[K][
 
 template <int K> struct Group { static constexpr int U = K >= 4 ? K : K == 3 ? 6 : 4; };  // positions in flight: a multiple of K
 
-template <typename T, int K, bool SMALL>
+template <typename T, int K, bool SMALL, bool STREAM>
 __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a, T* __restrict__ out, T* __restrict__ final_state) {
     constexpr int W = Wide<T>::V, U = Group<K>::U;
     using P = Piece<T, W, SMALL>;
@@ -89,12 +89,12 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a, T* __restrict__ o
                     for (int k = 0; k < K; ++k) pre = fmaf(w[k][j], ring[(u + 1 + k) % K][j], pre);
                     res[j] = l + u < len ? pre * sigmoid(pre) : 0.0f;
                 }
-                if (l + u < l1) P::put(o + static_cast<int64_t>(l + u) * a.D, a.D, res);
+                if (l + u < l1) P::template put<STREAM>(o + static_cast<int64_t>(l + u) * a.D, a.D, res);
             }
         }
     } else {
         const float zero[W] = {};
-        for (int l = l0; l < l1; ++l) P::put(o + static_cast<int64_t>(l) * a.D, a.D, zero);
+        for (int l = l0; l < l1; ++l) P::template put<STREAM>(o + static_cast<int64_t>(l) * a.D, a.D, zero);
     }
     if (r == 0 && final_state) {
 #pragma unroll
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvArgs a, T* __restrict__ o
 // Gradient.  A thread passes over a run of positions and the K - 1 behind it: dpre[l] of the whole window gives dx, those of
 // its own run the sums for weight and bias.  Workgroups are lx pieces wide and 256 / lx runs high; the sums of those runs are
 // joined in shared memory, the workgroups' by conv_sums_kernel, both in a fixed order.
-template <typename T, int K, bool SMALL>
+template <typename T, int K, bool SMALL, bool STREAM>
 __global__ __launch_bounds__(256) void conv_grad_kernel(ConvArgs a, T* __restrict__ dx, T* __restrict__ dstate, float* __restrict__ partial, int lx) {
     constexpr int W = 4, U = Group<K>::U;
     using P = Piece<T, W, SMALL>;
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(256) void conv_grad_kernel(ConvArgs a, T* __restric
                     if (to >= l0 && to < l1) {
 #pragma unroll
                         for (int j = 0; j < W; ++j) res[j] = to < len ? res[j] : 0.0f;
-                        P::put(o + static_cast<int64_t>(to) * a.D, a.D, res);
+                        P::template put<STREAM>(o + static_cast<int64_t>(to) * a.D, a.D, res);
                     } else if (r == 0 && to < 0 && dstate) {
                         P::put(dstate + (static_cast<int64_t>(b) * (K - 1) + (to + K - 1)) * a.D + c, a.D, res);
                     }
@@ -247,14 +247,17 @@ __global__ __launch_bounds__(256) void conv_step_kernel(const T* __restrict__ x,
     P::put(out + b * a.D + c, a.D, pre);
 }
 
-// Positions of a run: 64 unless the chip would stay empty (below 1024 threads a compute unit), then 32 or 16 (8, 24 with the
-// taps that do not divide those).  Always a multiple of the positions in flight.
-int run_length(int K, int64_t threads_a_position, int N) {
+// Positions of a run: 64, or half and half again of that while there would be fewer than `least` threads; always a multiple of the
+// positions in flight, two of them at least.  Measured: forward B=64 N=512 D=2048 bfloat16 62 us with runs of 64 (131072 threads), 69 of 32,
+// 92 of 16 (what a run reads in front of it, and its taps, come to more); forward and gradient of B=128 N=128 D=1001 float 68 us
+// with 64K threads at least in the gradient (runs of 32), 80 with 128K (of 16), 73 with 32K (of 64).
+int run_length(int K, int64_t threads_a_position, int N, int64_t least) {
     const int unit = K == 3 ? 6 : K == 2 ? 4 : K;
     int run = 64 / unit * unit;
-    while (run > 2 * unit && threads_a_position * ((N + run - 1) / run) < (256 << 10)) run = run / 2 / unit * unit;
+    while (run > 2 * unit && threads_a_position * ((N + run - 1) / run) < least) run = run / 2 / unit * unit;
     return run;
 }
+constexpr int64_t kForwardThreads = 128 << 10, kGradThreads = 64 << 10;
 
 struct GradPlan { int run, runs, lx, high; };
 GradPlan grad_plan(int B, int N, int D, int K) {
@@ -262,7 +265,7 @@ GradPlan grad_plan(int B, int N, int D, int K) {
     const int cpr = (D + 3) / 4;
     p.lx = 1;
     while (p.lx < 64 && p.lx < cpr) p.lx *= 2;
-    p.run = run_length(K, static_cast<int64_t>(B) * cpr * 4, N);
+    p.run = run_length(K, static_cast<int64_t>(B) * cpr, N, kGradThreads);
     p.runs = (N + p.run - 1) / p.run;
     const int64_t total = static_cast<int64_t>(B) * p.runs, ly = 256 / p.lx, wide = (cpr + p.lx - 1) / p.lx;
     // at most 2048 workgroups, then they take several runs one after the other
@@ -276,11 +279,12 @@ GradPlan grad_plan(int B, int N, int D, int K) {
 template <typename T, int K>
 hipError_t conv_of(ConvArgs a, void* out, void* final_state, hipStream_t st) {
     a.cpr = (a.D + Wide<T>::V - 1) / Wide<T>::V;
-    a.run = run_length(K, static_cast<int64_t>(a.B) * a.cpr, a.N);
+    a.run = run_length(K, static_cast<int64_t>(a.B) * a.cpr, a.N, kForwardThreads);
     a.runs = (a.N + a.run - 1) / a.run;
     const int64_t threads = static_cast<int64_t>(a.B) * a.runs * a.cpr;
     if (!fits((threads + 255) / 256, 256)) return hipErrorInvalidValue;
-    const auto kernel = a.D < Wide<T>::V ? conv_kernel<T, K, true> : conv_kernel<T, K, false>;
+    const bool stream = past_caches(static_cast<int64_t>(a.B) * a.N * a.D * static_cast<int64_t>(sizeof(T)));
+    const auto kernel = a.D < Wide<T>::V ? conv_kernel<T, K, true, false> : stream ? conv_kernel<T, K, false, true> : conv_kernel<T, K, false, false>;
     kernel<<<static_cast<unsigned>((threads + 255) / 256), 256, 0, st>>>(a, static_cast<T*>(out), static_cast<T*>(final_state));
     return hipGetLastError();
 }
@@ -293,7 +297,8 @@ hipError_t conv_grad_of(ConvArgs a, void* dx, float* dweight, float* dbias, void
     a.runs = p.runs;
     float* partial = static_cast<float*>(ws);
     const dim3 grid((a.cpr + p.lx - 1) / p.lx, p.high);
-    const auto kernel = a.D < 4 ? conv_grad_kernel<T, K, true> : conv_grad_kernel<T, K, false>;
+    const bool stream = past_caches(static_cast<int64_t>(a.B) * a.N * a.D * static_cast<int64_t>(sizeof(T)));
+    const auto kernel = a.D < 4 ? conv_grad_kernel<T, K, true, false> : stream ? conv_grad_kernel<T, K, false, true> : conv_grad_kernel<T, K, false, false>;
     kernel<<<grid, 256, sizeof(float) * 256 * (K + 1) * 4, st>>>(a, static_cast<T*>(dx), static_cast<T*>(dstate), partial, p.lx);
     conv_sums_kernel<K><<<dim3((a.D + 63) / 64, K + 1), 1024, 0, st>>>(partial, p.high, a.D, dweight, dbias);
     return hipGetLastError();

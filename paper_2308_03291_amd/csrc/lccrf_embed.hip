@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kItems = 4;  // pieces a thread of the lookup
 
-template <typename T, bool SMALL>
+template <typename T, bool SMALL, bool STREAM>
 __global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ table, int V, int D, int64_t table_row, const int32_t* __restrict__ ids,
                                                     int64_t n, float scale, T* __restrict__ out, int cpr, int per_block) {
     constexpr int W = Wide<T>::V;
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ table,
             v[i].get(o);
 #pragma unroll
             for (int j = 0; j < W; ++j) o[j] = static_cast<unsigned>(id[i]) < static_cast<unsigned>(V) ? o[j] * scale : 0.0f;
-            if (k0 + 256 * i < here) P::put(out + pos[i] * D + c[i], D, o);
+            if (k0 + 256 * i < here) P::template put<STREAM>(out + pos[i] * D + c[i], D, o);
         }
     }
 }
@@ -329,7 +329,8 @@ hipError_t embed_of(const void* table, int V, int D, int64_t table_row, const in
     // positions a workgroup: its threads' kItems pieces, one position at least
     const int per_block = cpr >= 256 * kItems ? 1 : 256 * kItems / cpr;
     if (!fits((n + per_block - 1) / per_block, 256)) return hipErrorInvalidValue;
-    embed_kernel<T, SMALL><<<static_cast<unsigned>((n + per_block - 1) / per_block), 256, 0, st>>>(static_cast<const T*>(table), V, D, table_row, ids, n, scale,
+    const auto kernel = past_caches(n * D * static_cast<int64_t>(sizeof(T))) ? embed_kernel<T, SMALL, true> : embed_kernel<T, SMALL, false>;
+    kernel<<<static_cast<unsigned>((n + per_block - 1) / per_block), 256, 0, st>>>(static_cast<const T*>(table), V, D, table_row, ids, n, scale,
                                                                                            static_cast<T*>(out), cpr, per_block);
     return hipGetLastError();
 }
@@ -349,9 +350,7 @@ hipError_t embed_grad_of(AnyRows dout, const int32_t* ids, int B, int N, int V, 
     const int64_t row_blocks = (static_cast<int64_t>((V + kRows - 1) / kRows) * cpr + 255) / 256;
     if (!fits(piece_blocks + row_blocks, 256)) return hipErrorInvalidValue;
     index_kernel<<<plan.workgroups, kIndexThreads, sizeof(int32_t) * kIndexWaves * (plan.range + 2 * kKept), st>>>(ids, n, V, plan.range, order, start);
-    // A gradient that the L2 caches could not hold (eight of 4 MB) is written past them: 205 MB 76 us, through them 102.
-    const bool stream = static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T)) > (int64_t{32} << 20);
-    const auto rows = stream ? rows_kernel<T, SMALL, true> : rows_kernel<T, SMALL, false>;
+    const auto rows = past_caches(static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T))) ? rows_kernel<T, SMALL, true> : rows_kernel<T, SMALL, false>;
     rows<<<static_cast<unsigned>(piece_blocks + row_blocks), 256, 0, st>>>(a, dout.as<T>(), static_cast<T*>(grad), static_cast<int>(piece_blocks));
     if (pieces) join_kernel<T, SMALL><<<static_cast<unsigned>((pieces * cpr + 255) / 256), 256, 0, st>>>(a, static_cast<T*>(grad));
     return hipGetLastError();
