@@ -60,8 +60,9 @@ __global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ table,
 constexpr int kIndexWaves = 16, kIndexThreads = 64 * kIndexWaves;
 constexpr int kMaxRange = kIndexThreads;  // tokens of a workgroup of `index`: one a thread
 constexpr int kFlight = 8;                // loads of four ids in flight a thread: all of its share up to 32768 positions
-constexpr int kKept = 256;                // positions a wave of `index` keeps from its first pass; with more it passes over the ids again
-constexpr int kRows = 4;                  // rows of the gradient a thread
+constexpr int kKept = 1024;               // positions a wave of `index` keeps from its first pass; with more it passes over the ids again
+constexpr int kRangeBits = 10;            // a kept word: position within the share and, in the lowest bits, token within the range
+static_assert(kMaxRange == 1 << kRangeBits, "");
 
 struct IndexPlan { int range, workgroups; };
 // 256 workgroups, one a compute unit, as long as their ranges hold 64 tokens at least and kMaxRange at most.
@@ -87,14 +88,13 @@ __device__ __forceinline__ void four_ids(const int32_t* __restrict__ ids, int p,
 
 __global__ __launch_bounds__(kIndexThreads) void index_kernel(const int32_t* __restrict__ ids, int n, int V, int range, int32_t* __restrict__ order,
                                                               int32_t* __restrict__ start) {
-    extern __shared__ int32_t lds[];  // counters [kIndexWaves][range], then kept positions and tokens [kIndexWaves][2][kKept]
+    extern __shared__ int32_t lds[];  // counters [kIndexWaves][range], then kept positions with their tokens [kIndexWaves][kKept]
     __shared__ int32_t wave_sum[kIndexWaves], below_sum[kIndexWaves];
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
     const int lo = blockIdx.x * range, hi = lo + range < V ? lo + range : V;
     const unsigned here = hi - lo;
     int32_t* const count = lds;
-    int32_t* const kept_p = lds + kIndexWaves * range + w * 2 * kKept;
-    int32_t* const kept_id = kept_p + kKept;
+    uint32_t* const keep = reinterpret_cast<uint32_t*>(lds + kIndexWaves * range) + w * kKept;
     for (int k = t; k < kIndexWaves * range; k += kIndexThreads) count[k] = 0;
     __syncthreads();
     int32_t* mine = count + w * range;
@@ -115,10 +115,7 @@ __global__ __launch_bounds__(kIndexThreads) void index_kernel(const int32_t* __r
                 const int to = kept + __popcll(all & before);
                 if (in) {
                     atomicAdd(&mine[local], 1);
-                    if (to < kKept) {
-                        kept_p[to] = p + i;
-                        kept_id[to] = local;
-                    }
+                    if (to < kKept) keep[to] = static_cast<uint32_t>(p + i - begin) << kRangeBits | local;
                 }
                 kept += __popcll(all);
             }
@@ -170,25 +167,30 @@ __global__ __launch_bounds__(kIndexThreads) void index_kernel(const int32_t* __r
         }
     }
     __syncthreads();
-    // Places: the lanes that have the same token take theirs together, a token at a time.
+    // Places: which lanes have the same token follows from one ballot a bit of it; they take theirs together.
+    int bits = 0;
+    while (range > 1 << bits) ++bits;
     const auto place = [&](bool in, int local, int p) {
-        uint64_t left = __ballot(in);
-        while (left) {
-            const int leader = __builtin_ctzll(left);
-            const int which = __builtin_amdgcn_readlane(local, leader);
-            const bool same = in && local == which;
-            const uint64_t all = __ballot(same);
-            int at = 0;
-            if (lane == leader) at = atomicAdd(&mine[which], __popcll(all));
-            at = __builtin_amdgcn_readlane(at, leader);
-            if (same) order[at + __popcll(all & before)] = p;
-            left &= ~all;
+        uint64_t same = __ballot(in);
+        if (!same) return;
+        for (int k = 0; k < bits; ++k) {
+            const uint64_t set = __ballot(local >> k & 1);
+            same &= local >> k & 1 ? set : ~set;
         }
+        int at = 0;
+        if (in) {
+            at = mine[local];
+            order[at + __popcll(same & before)] = p;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (in && !(same & before)) mine[local] = at + __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
-    if (kept <= kKept) {
+    if (kept <= kKept && share <= 1 << (32 - kRangeBits)) {
         for (int k = 0; k < kept; k += 64) {
             const bool in = k + lane < kept;
-            place(in, in ? kept_id[k + lane] : 0, in ? kept_p[k + lane] : 0);
+            const uint32_t v = in ? keep[k + lane] : 0;
+            place(in, v & (kMaxRange - 1), begin + static_cast<int>(v >> kRangeBits));
         }
     } else {  // many of one token: all ids once more, in the same order
         for (int p0 = begin; p0 < end; p0 += 256) {
@@ -237,7 +239,7 @@ __device__ __forceinline__ void sum_rows(const GradArgs& a, Rows<T> dout, int fr
 // The first `piece_blocks` workgroups: partial sums of long rows.  Slot 0 of piece j is for the row that its first
 // position belongs to, slot 1 for the one of its last position, if that is another: a row of more than `piece` positions
 // reaches over an end of every piece it has a part in.
-template <typename T, bool SMALL, bool STREAM>
+template <typename T, bool SMALL, int ROWS, bool STREAM>
 __global__ __launch_bounds__(256) void rows_kernel(GradArgs a, Rows<T> dout, T* __restrict__ grad, int piece_blocks) {
     constexpr int W = Wide<T>::V;
     float sum[W];
@@ -259,14 +261,14 @@ __global__ __launch_bounds__(256) void rows_kernel(GradArgs a, Rows<T> dout, T* 
         return;
     }
     const int64_t k = static_cast<int64_t>(blockIdx.x - piece_blocks) * 256 + threadIdx.x;
-    const int64_t row0 = k / a.cpr * kRows;
+    const int64_t row0 = k / a.cpr * ROWS;
     if (row0 >= a.V) return;
     const int c = piece_start<W, SMALL>(static_cast<int>(k % a.cpr), a.D);
-    int s[kRows + 1];
+    int s[ROWS + 1];
 #pragma unroll
-    for (int i = 0; i <= kRows; ++i) s[i] = a.start[row0 + i < a.V ? row0 + i : a.V];
+    for (int i = 0; i <= ROWS; ++i) s[i] = a.start[row0 + i < a.V ? row0 + i : a.V];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
         const int n = s[i + 1] - s[i];
         if (row0 + i >= a.V || n > a.piece) continue;
         if (n) {
@@ -347,10 +349,16 @@ hipError_t embed_grad_of(AnyRows dout, const int32_t* ids, int B, int N, int V, 
     const GradArgs a{ids, order, start, n, N < 1 ? 1 : N, V, D, cpr, piece_of(n), scale, partial};
     const int64_t pieces = pieces_of(n);  // without a row that can be long there is nothing to cut
     const int64_t piece_blocks = (2 * pieces * cpr + 255) / 256;
-    const int64_t row_blocks = (static_cast<int64_t>((V + kRows - 1) / kRows) * cpr + 255) / 256;
+    // Four rows a thread once that leaves a quarter of a million threads: their starts are loaded together, and rows of zeros cost little else.
+    const bool four = static_cast<int64_t>(V) * cpr >= (int64_t{1} << 20);
+    const int64_t row_blocks = ((four ? (V + 3) / 4 : V) * static_cast<int64_t>(cpr) + 255) / 256;
     if (!fits(piece_blocks + row_blocks, 256)) return hipErrorInvalidValue;
-    index_kernel<<<plan.workgroups, kIndexThreads, sizeof(int32_t) * kIndexWaves * (plan.range + 2 * kKept), st>>>(ids, n, V, plan.range, order, start);
-    const auto rows = past_caches(static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T))) ? rows_kernel<T, SMALL, true> : rows_kernel<T, SMALL, false>;
+    const int bytes = static_cast<int>(sizeof(int32_t)) * kIndexWaves * (plan.range + kKept);  // 128 KB at most; more than 64 have to be asked for
+    if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(index_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes); e != hipSuccess) return e;
+    index_kernel<<<plan.workgroups, kIndexThreads, bytes, st>>>(ids, n, V, plan.range, order, start);
+    const bool stream = past_caches(static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T)));
+    const auto rows = four ? (stream ? rows_kernel<T, SMALL, 4, true> : rows_kernel<T, SMALL, 4, false>)
+                           : (stream ? rows_kernel<T, SMALL, 1, true> : rows_kernel<T, SMALL, 1, false>);
     rows<<<static_cast<unsigned>(piece_blocks + row_blocks), 256, 0, st>>>(a, dout.as<T>(), static_cast<T*>(grad), static_cast<int>(piece_blocks));
     if (pieces) join_kernel<T, SMALL><<<static_cast<unsigned>((pieces * cpr + 255) / 256), 256, 0, st>>>(a, static_cast<T*>(grad));
     return hipGetLastError();
