@@ -177,11 +177,11 @@ inline ScanPlan scan_plan(int B, int N, int D, int G, int waves_a_tile, int room
     p.segments = (N + p.seg_len - 1) / p.seg_len;
     return p;
 }
-inline ScanPlan forward_plan(int B, int N, int D, int G) { return scan_plan(B, N, D, G, 1, 2048, 3); }
+inline ScanPlan forward_plan(int B, int N, int D, int S, int G) { return scan_plan(B, N, D, G, S <= 16 ? 1 : S <= 32 ? 2 : 4, 2048, 3); }
 
 inline bool scan_fits(int B, int N, int D, int S, int G, const ScanPlan& p) {
     const int64_t most = (int64_t{1} << 32) - 1024, b = B;
-    return b * p.segments * G * p.tiles * 256 < most && b * D * quads(S) < most && b * N * G * S < most;
+    return b * p.segments * G * p.tiles * 512 < most && b * D * quads(S) < most && b * N * G * S < most;
 }
 
 // Runs the scan for the saved states alone (out and final_state null), or with them.

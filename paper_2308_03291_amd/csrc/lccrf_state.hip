@@ -23,15 +23,21 @@ struct ScanRun {
     ScanPlan plan;
 };
 
-template <typename T, int SP, int MODE, bool GATED>
+// SW waves share a tile's states, SP each (more than 16 states: two or four).  Alone, a wave keeps all it knows of a position in
+// registers; together they share the positions (sw, sw + SW, ... are this wave's: it computes their steps and finishes their outputs) and
+// meet in LDS.
+template <typename T, int SP, int SW, int MODE, bool GATED>
 __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
-    extern __shared__ float lds[];  // [waves][kP][2 * SP]
+    extern __shared__ float lds[];  // [waves][kP][2 * SP]; SW > 1: then steps and step x [2][kP][64], sums over the states [SW][kP][64]
+    constexpr int P = kP / SW;
     const ScanIn& in = r.in;
     const int lane = threadIdx.x & 63, tiles = in.G * r.plan.tiles;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned at_work = blockIdx.x * (blockDim.x >> 6) + wave, which = at_work / tiles;
-    const int tile = at_work - which * tiles;
+    const unsigned at_work = SW > 1 ? blockIdx.x : blockIdx.x * (blockDim.x >> 6) + wave, which = at_work / tiles;
+    const int tile = at_work - which * tiles, sw = SW > 1 ? wave : 0, s0 = sw * SP;
     float* bc = lds + wave * (kP * 2 * SP);
+    float* shared = lds + SW * (kP * 2 * SP) + lane;
+    float* sums = shared + 2 * kP * 64;
     int b = which / r.plan.segments;
     const int seg = which - b * r.plan.segments;
     // Whole sequences, as many waves as there is room for at once: long ones first, then the short ones from the shortest on, so that a
@@ -49,7 +55,7 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
     float h[SP], A[SP], total = 0.0f;
 #pragma unroll
     for (int s = 0; s < SP; ++s) {
-        A[s] = s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s]) : 0.0f;
+        A[s] = s0 + s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s0 + s]) : 0.0f;
         h[s] = 0.0f;
     }
     if (!(MODE & kEnds)) {
@@ -57,37 +63,44 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
             const int64_t from = static_cast<int64_t>(b) * r.plan.segments + seg;
 #pragma unroll
             for (int s = 0; s < SP; ++s)
-                if (s < in.S) h[s] = r.ends[quad_at(from, in.S, in.D_, s / 4, d) + s % 4];
+                if (s0 + s < in.S) h[s] = r.ends[quad_at(from, in.S, in.D_, (s0 + s) / 4, d) + s % 4];
         } else if (r.state) {
 #pragma unroll
             for (int s = 0; s < SP; ++s)
-                if (s < in.S) h[s] = r.state[(static_cast<int64_t>(b) * in.D_ + d) * in.S + s];
+                if (s0 + s < in.S) h[s] = r.state[(static_cast<int64_t>(b) * in.D_ + d) * in.S + s0 + s];
         }
     }
 
     if (begin < end) {
-        T xr[kP], tr[kP], zr[kP];
+        T xr[P], tr[P], zr[P];
         GroupVectors<T, SP> gv;
-        const T *px = at<T>(in.x, b, begin), *pt = at<T>(in.dt, b, begin), *pz = at<T>(in.z, b, begin);
+        const T *px = at<T>(in.x, b, begin + sw), *pt = at<T>(in.dt, b, begin + sw), *pz = at<T>(in.z, b, begin + sw);
         const auto fetch_whole = [&](int ahead) {
             px += ahead * kP * in.x.row;
             pt += ahead * kP * in.dt.row;
             pz += ahead * kP * in.z.row;
             gv.next(in, ahead);
-            load_whole<T, kP>(px, in.x.row, bytes, xr);
-            load_whole<T, kP>(pt, in.dt.row, bytes, tr);
-            if (GATED) load_whole<T, kP>(pz, in.z.row, bytes, zr);
+            load_whole<T, P>(px, SW * in.x.row, bytes, xr);
+            load_whole<T, P>(pt, SW * in.dt.row, bytes, tr);
+            if (GATED) load_whole<T, P>(pz, SW * in.z.row, bytes, zr);
         };
-        float step[kP], put[kP], x[kP], z[kP];
+        float step[kP], put[kP], x[P], z[P];  // (SW > 1: step and put are in LDS)
         const auto settle = [&](auto whole, int l0) {  // what fetch has brought
             constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
-            for (int i = 0; i < kP; ++i) {
+            for (int k = 0; k < P; ++k) {
+                const int i = sw + k * SW;
                 const bool on = WHOLE || l0 + i < end;
-                step[i] = on ? softplus(widen(tr[i]) + bias).value : 0.0f;
-                x[i] = on ? widen(xr[i]) : 0.0f;
-                put[i] = step[i] * x[i];
-                if (GATED) z[i] = widen(zr[i]);
+                const float st = on ? softplus(widen(tr[k]) + bias).value : 0.0f;
+                x[k] = on ? widen(xr[k]) : 0.0f;
+                if (GATED) z[k] = widen(zr[k]);
+                if constexpr (SW > 1) {
+                    shared[i * 64] = st;
+                    shared[(kP + i) * 64] = st * x[k];
+                } else {
+                    step[k] = st;
+                    put[k] = st * x[k];
+                }
             }
             wave_sync();
             gv.template put<WHOLE>(bc, l0, len, lane);
@@ -99,102 +112,109 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
                 float* place = r.saved + quad_at(static_cast<int64_t>(b) * ((in.N + kP - 1) / kP) + l0 / kP, in.S, in.D_, 0, 0);
 #pragma unroll
                 for (int q = 0; q < SP / 4; ++q)
-                    *reinterpret_cast<f32x4*>(reinterpret_cast<char*>(place) + quad_bytes(in.D_, q, d)) = f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]};
+                    *reinterpret_cast<f32x4*>(reinterpret_cast<char*>(place) + quad_bytes(in.D_, s0 / 4 + q, d)) = f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]};
             }
             // The next block, or behind the last whole one that one again: without a branch nothing has to wait for it here.
             if (WHOLE) fetch_whole(l0 + 2 * kP <= end);
             const f32x4* bc4 = reinterpret_cast<const f32x4*>(bc);
             constexpr int Q = SP / 4, R = MODE & kOut ? 2 * Q : Q;
-            // Bm and Cm of a position; the next one's are read while this one's are used (up to 16 states: more registers there are not)
-            constexpr bool AHEAD = SP <= 16;
-            f32x4 v[AHEAD ? 2 : 1][AHEAD ? R : 1];
-            if constexpr (AHEAD) {
+            f32x4 v[2][R];  // Bm and Cm of a position; the next one's are read while this one's are used
 #pragma unroll
-                for (int q = 0; q < R; ++q) v[0][q] = bc4[q];
-            }
-            float o[kP];
+            for (int q = 0; q < R; ++q) v[0][q] = bc4[q];
+            float o[P];
 #pragma unroll
             for (int i = 0; i < kP; ++i) {
-                if constexpr (AHEAD) {
-                    if (i + 1 < kP) {
+                if (i + 1 < kP) {
 #pragma unroll
-                        for (int q = 0; q < R; ++q) v[(i + 1) & 1][q] = bc4[(i + 1) * 2 * Q + q];
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int q = 0; q < R; ++q) v[(i + 1) & 1][q] = bc4[(i + 1) * 2 * Q + q];
                 }
-                const auto now = [&](int q) {
-                    if constexpr (AHEAD) return v[i & 1][q];
-                    else return bc4[i * 2 * Q + q];
-                };
+                __builtin_amdgcn_sched_barrier(0);
+                const float step_i = SW > 1 ? shared[i * 64] : step[i], put_i = SW > 1 ? shared[(kP + i) * 64] : put[i];
+                const f32x4(&now)[R] = v[i & 1];
                 float y0 = 0.0f, y1 = 0.0f;
 #pragma unroll
                 for (int q = 0; q < Q; ++q) {
-                    const f32x4 Bq = now(q);
+                    const f32x4 Bq = now[q];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int s = 4 * q + j;
-                        h[s] = fmaf(exp2_fast(step[i] * A[s]), h[s], put[i] * Bq[j]);
+                        h[s] = fmaf(exp2_fast(step_i * A[s]), h[s], put_i * Bq[j]);
                     }
                     if constexpr ((MODE & kOut) != 0) {
-                        const f32x4 Cq = now(Q + q);
+                        const f32x4 Cq = now[Q + q];
                         y0 = fmaf(h[4 * q], Cq[0], y0);
                         y1 = fmaf(h[4 * q + 1], Cq[1], y1);
                         y0 = fmaf(h[4 * q + 2], Cq[2], y0);
                         y1 = fmaf(h[4 * q + 3], Cq[3], y1);
                     }
                 }
-                if (MODE & kOut) {
+                if (MODE & kEnds) total += step_i;
+                if constexpr ((MODE & kOut) != 0 && SW > 1) {
+                    sums[(sw * kP + i) * 64] = y0 + y1;
+                } else if constexpr ((MODE & kOut) != 0) {
                     const float y = fmaf(skip, x[i], y0 + y1);
                     o[i] = GATED ? y * z[i] * sigmoid(z[i]) : y;
                     asm volatile("" : "+v"(o[i]));  // computed here: moved behind a store's condition, it would keep the states of all eight positions
                 }
             }
-            if (MODE & kEnds) {
+            if constexpr (SW > 1) {
+                __syncthreads();
+                if (MODE & kOut) {
 #pragma unroll
-                for (int i = 0; i < kP; ++i) total += step[i];
+                    for (int k = 0; k < P; ++k) {
+                        float y = 0.0f;
+#pragma unroll
+                        for (int w = 0; w < SW; ++w) y += sums[(w * kP + sw + k * SW) * 64];
+                        y = fmaf(skip, x[k], y);
+                        o[k] = GATED ? y * z[k] * sigmoid(z[k]) : y;
+                    }
+                }
             }
             if (WHOLE) settle(std::true_type{}, l0 + kP);
             if (MODE & kOut) {
-                T* to = out + static_cast<int64_t>(l0) * in.D_;
+                T* to = out + static_cast<int64_t>(l0 + sw) * in.D_;
                 unsigned at = bytes;
                 asm volatile("" : "+v"(at));
 #pragma unroll
-                for (int i = 0; i < kP; ++i, to += in.D_)
-                    if (WHOLE || l0 + i < end) give(to, at, o[i]);
+                for (int k = 0; k < P; ++k, to += SW * in.D_)
+                    if (WHOLE || l0 + sw + k * SW < end) give(to, at, o[k]);
             }
+            if (SW > 1) __syncthreads();  // steps are there for the other waves, sums are free
         };
-        gv.place(in, b, begin, group, 0, lane);
+        gv.place(in, b, begin, group, s0, lane);
         int l0 = begin;
         if (begin + kP <= end) {
             fetch_whole(0);
             settle(std::true_type{}, begin);
+            if (SW > 1) __syncthreads();
             for (; l0 + kP <= end; l0 += kP) block(std::true_type{}, l0);
         }
         if (l0 < end) {
-            gv.place(in, b, l0, group, 0, lane);
+            gv.place(in, b, l0, group, s0, lane);
             gv.load(in, l0, len);
-            load_rows<T, kP>(in.x, b, l0, 1, len, bytes, xr);
-            load_rows<T, kP>(in.dt, b, l0, 1, len, bytes, tr);
-            if (GATED) load_rows<T, kP>(in.z, b, l0, 1, len, bytes, zr);
+            load_rows<T, P>(in.x, b, l0 + sw, SW, len, bytes, xr);
+            load_rows<T, P>(in.dt, b, l0 + sw, SW, len, bytes, tr);
+            if (GATED) load_rows<T, P>(in.z, b, l0 + sw, SW, len, bytes, zr);
             settle(std::false_type{}, l0);
+            if (SW > 1) __syncthreads();
             block(std::false_type{}, l0);
         }
     }
     if (MODE & kOut)
         for (int l = begin < end ? end : begin; l < stop; ++l)
-            if (is) give(out + static_cast<int64_t>(l) * in.D_, bytes, 0.0f);
+            if (is && sw == 0) give(out + static_cast<int64_t>(l) * in.D_, bytes, 0.0f);
     if (MODE & kEnds) {
         const int64_t to = static_cast<int64_t>(b) * r.plan.segments + seg;
         if (is) {
 #pragma unroll
             for (int s = 0; s < SP; ++s)
-                if (s < in.S) r.ends[quad_at(to, in.S, in.D_, s / 4, d) + s % 4] = h[s];
-            r.steps[to * in.D_ + d] = total;
+                if (s0 + s < in.S) r.ends[quad_at(to, in.S, in.D_, (s0 + s) / 4, d) + s % 4] = h[s];
+            if (sw == 0) r.steps[to * in.D_ + d] = total;
         }
     } else if (r.final_state && is && (end == len && (begin < len || seg == 0))) {
 #pragma unroll
         for (int s = 0; s < SP; ++s)
-            if (s < in.S) r.final_state[(static_cast<int64_t>(b) * in.D_ + d) * in.S + s] = h[s];
+            if (s0 + s < in.S) r.final_state[(static_cast<int64_t>(b) * in.D_ + d) * in.S + s0 + s] = h[s];
     }
 }
 
@@ -322,32 +342,33 @@ hipError_t step_of(const ScanIn& in, float* state, void* out, hipStream_t st) {
 
 // ---- launches -------------------------------------------------------------------------------------------------
 
-template <typename T, int SP, int MODE>
+template <typename T, int SP, int SW, int MODE>
 void scan_launch(const ScanRun& r, hipStream_t st) {
-    const int64_t waves = static_cast<int64_t>(r.in.G) * r.plan.tiles * r.in.B * r.plan.segments;
-    const auto kernel = (MODE & kOut) && r.in.z.data ? scan_kernel<T, SP, MODE, (MODE & kOut) != 0> : scan_kernel<T, SP, MODE, false>;
-    const int w = waves_together(r.in.G * r.plan.tiles);
-    kernel<<<static_cast<unsigned>(waves / w), 64 * w, sizeof(float) * w * kP * 2 * SP, st>>>(r);
+    const int64_t tiles = static_cast<int64_t>(r.in.G) * r.plan.tiles * r.in.B * r.plan.segments;
+    const auto kernel = (MODE & kOut) && r.in.z.data ? scan_kernel<T, SP, SW, MODE, (MODE & kOut) != 0> : scan_kernel<T, SP, SW, MODE, false>;
+    const int w = SW > 1 ? SW : waves_together(r.in.G * r.plan.tiles);
+    const size_t bytes = sizeof(float) * (w * kP * 2 * SP + (SW > 1 ? (2 + SW) * kP * 64 : 0));
+    kernel<<<static_cast<unsigned>(tiles * SW / w), 64 * w, bytes, st>>>(r);
 }
 
-template <typename T, int SP>
+template <typename T, int SP, int SW>
 void scan_run(ScanRun& r, hipStream_t st) {
     if (r.plan.segments > 1) {
-        scan_launch<T, SP, kEnds>(r, st);
+        scan_launch<T, SP, SW, kEnds>(r, st);
         (void)launch_join_segments(r.in, r.plan, r.state, r.ends, r.steps, false, st);
     }
-    if (!r.out) scan_launch<T, SP, kSave>(r, st);
-    else if (r.saved) scan_launch<T, SP, kOut | kSave>(r, st);
-    else scan_launch<T, SP, kOut>(r, st);
+    if (!r.out) scan_launch<T, SP, SW, kSave>(r, st);
+    else if (r.saved) scan_launch<T, SP, SW, kOut | kSave>(r, st);
+    else scan_launch<T, SP, SW, kOut>(r, st);
 }
 
 template <typename T>
 void scan_of(ScanRun& r, hipStream_t st) {
-    if (r.in.S <= 4) scan_run<T, 4>(r, st);
-    else if (r.in.S <= 8) scan_run<T, 8>(r, st);
-    else if (r.in.S <= 16) scan_run<T, 16>(r, st);
-    else if (r.in.S <= 32) scan_run<T, 32>(r, st);
-    else scan_run<T, 64>(r, st);
+    if (r.in.S <= 4) scan_run<T, 4, 1>(r, st);
+    else if (r.in.S <= 8) scan_run<T, 8, 1>(r, st);
+    else if (r.in.S <= 16) scan_run<T, 16, 1>(r, st);
+    else if (r.in.S <= 32) scan_run<T, 16, 2>(r, st);
+    else scan_run<T, 16, 4>(r, st);
 }
 
 size_t ends_bytes(const ScanPlan& p, int B, int D, int S) {
@@ -367,13 +388,13 @@ hipError_t launch_join_segments(const ScanIn& in, const ScanPlan& p, const float
 size_t scan_saved_bytes(int B, int N, int D, int S) { return up256(static_cast<size_t>(B) * scan_blocks(N) * quads(S) * D * 16); }
 
 size_t scan_workspace(int B, int N, int D, int S, int G) {
-    const ScanPlan p = forward_plan(B, N, D, G);
+    const ScanPlan p = forward_plan(B, N, D, S, G);
     if (p.segments == 1) return 256;
     return ends_bytes(p, B, D, S) + up256(static_cast<size_t>(B) * p.segments * D * 4);
 }
 
 hipError_t run_state_scan(int dtype, const ScanIn& in, const float* state, void* out, float* final_state, float* saved, void* ws, hipStream_t st) {
-    ScanRun r{in, state, out, final_state, saved, nullptr, nullptr, forward_plan(in.B, in.N, in.D_, in.G)};
+    ScanRun r{in, state, out, final_state, saved, nullptr, nullptr, forward_plan(in.B, in.N, in.D_, in.S, in.G)};
     if (!scan_fits(in.B, in.N, in.D_, in.S, in.G, r.plan)) return hipErrorInvalidValue;
     if (r.plan.segments > 1) {
         r.ends = static_cast<float*>(ws);

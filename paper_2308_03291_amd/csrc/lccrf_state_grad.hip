@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
     const int lane = threadIdx.x & 63, tiles = in.G * plan.tiles;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned at_work = blockIdx.x * (blockDim.x >> 6) + wave, which = at_work / tiles;
-    const int tile = at_work - which * tiles;
+    const int tile = at_work - which * tiles, s0 = blockIdx.y * SP;
     float* bc = lds + wave * (kP * 2 * SP);
     const int b = which / plan.segments, seg = which - b * plan.segments;
     const int width = in.D_ / in.G, group = tile / plan.tiles, c0 = (tile - group * plan.tiles) * 64 + lane;
@@ -108,14 +108,14 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
     float dh[SP], A[SP], total = 0.0f;
 #pragma unroll
     for (int s = 0; s < SP; ++s) {
-        A[s] = s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s]) : 0.0f;
+        A[s] = s0 + s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s0 + s]) : 0.0f;
         dh[s] = 0.0f;
     }
     if (begin < end) {
         T tr[kP], zr[kP], dr[kP];
         GroupVectors<T, SP> gv;
         const int last = begin + (end - begin - 1) / kP * kP;
-        gv.place(in, b, last, group, 0, lane);
+        gv.place(in, b, last, group, s0, lane);
         gv.load(in, last, len);
         load_rows<T, kP>(in.dt, b, last, 1, len, bytes, tr);
         load_rows<T, kP>(r.dout, b, last, 1, len, bytes, dr);
@@ -158,8 +158,8 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
     if (is) {
 #pragma unroll
         for (int s = 0; s < SP; ++s)
-            if (s < in.S) r.ends[quad_at(to, in.S, in.D_, s / 4, d) + s % 4] = dh[s];
-        r.steps[to * in.D_ + d] = total;
+            if (s0 + s < in.S) r.ends[quad_at(to, in.S, in.D_, (s0 + s) / 4, d) + s % 4] = dh[s];
+        if (s0 == 0) r.steps[to * in.D_ + d] = total;
     }
 }
 
@@ -482,7 +482,7 @@ template <typename T, int SP>
 void back_ends(const GradRun& r, hipStream_t st) {
     const int64_t waves = static_cast<int64_t>(r.in.G) * r.plan.scan.tiles * r.in.B * r.plan.scan.segments;
     const int w = waves_together(r.in.G * r.plan.scan.tiles);
-    back_ends_kernel<T, SP><<<static_cast<unsigned>(waves / w), 64 * w, sizeof(float) * w * kP * 2 * SP, st>>>(r);
+    back_ends_kernel<T, SP><<<dim3(static_cast<unsigned>(waves / w), (r.in.S + SP - 1) / SP), 64 * w, sizeof(float) * w * kP * 2 * SP, st>>>(r);
 }
 
 template <typename T, int SP, int SW>
@@ -505,9 +505,7 @@ hipError_t grad_of(const GradRun& r, hipStream_t st) {
     if (r.plan.scan.segments > 1) {
         if (S <= 4) back_ends<T, 4>(r, st);
         else if (S <= 8) back_ends<T, 8>(r, st);
-        else if (S <= 16) back_ends<T, 16>(r, st);
-        else if (S <= 32) back_ends<T, 32>(r, st);
-        else back_ends<T, 64>(r, st);
+        else back_ends<T, 16>(r, st);
         (void)launch_join_segments(r.in, r.plan.scan, nullptr, r.ends, r.steps, true, st);
     }
     const hipError_t e = S <= 4 ? grad_main<T, 4, 1>(r, st) : S <= 8 ? grad_main<T, 8, 1>(r, st) : S <= 16 ? grad_main<T, 8, 2>(r, st)
