@@ -353,8 +353,10 @@ hipError_t embed_grad_of(AnyRows dout, const int32_t* ids, int B, int N, int V, 
     const bool four = static_cast<int64_t>(V) * cpr >= (int64_t{1} << 20);
     const int64_t row_blocks = ((four ? (V + 3) / 4 : V) * static_cast<int64_t>(cpr) + 255) / 256;
     if (!fits(piece_blocks + row_blocks, 256)) return hipErrorInvalidValue;
-    const int bytes = static_cast<int>(sizeof(int32_t)) * kIndexWaves * (plan.range + kKept);  // 128 KB at most; more than 64 have to be asked for
-    if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(index_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes); e != hipSuccess) return e;
+    const int bytes = static_cast<int>(sizeof(int32_t)) * kIndexWaves * (plan.range + kKept);
+    static std::atomic<uint64_t> asked{0};
+    if (const hipError_t e = ask_lds(reinterpret_cast<const void*>(index_kernel), static_cast<int>(sizeof(int32_t)) * kIndexWaves * (kMaxRange + kKept), asked); e != hipSuccess)
+        return e;
     index_kernel<<<plan.workgroups, kIndexThreads, bytes, st>>>(ids, n, V, plan.range, order, start);
     const bool stream = past_caches(static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T)));
     const auto rows = four ? (stream ? rows_kernel<T, SMALL, 4, true> : rows_kernel<T, SMALL, 4, false>)

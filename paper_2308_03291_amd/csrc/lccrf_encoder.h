@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace lccrf {
 namespace enc {
 
@@ -165,6 +167,16 @@ hipError_t launch_state_step(int dtype, const ScanIn& in, float* state, void* ou
 inline bool past_caches(int64_t bytes) { return bytes > (int64_t{32} << 20); }
 // A launch has fewer than 2^32 threads; the entry points refuse what would take more.
 inline bool fits(int64_t blocks, int threads) { return blocks * threads < (int64_t{1} << 32); }
+// More than 64 KB of LDS has to be asked for, once a kernel and device (`asked`: a bit a device).
+inline hipError_t ask_lds(const void* kernel, int bytes, std::atomic<uint64_t>& asked) {
+    int dev = 0;
+    if (const hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
+    const uint64_t bit = uint64_t{1} << (dev & 63);
+    if (asked.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) asked.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace enc

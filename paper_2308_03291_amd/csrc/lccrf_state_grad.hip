@@ -490,10 +490,10 @@ hipError_t grad_main(const GradRun& r, hipStream_t st) {
     const int bytes = static_cast<int>(sizeof(float)) * grad_lds<SP, SW>(r.plan.tile_waves);
     const int64_t blocks = static_cast<int64_t>(r.in.B) * r.plan.scan.segments * r.in.G * r.plan.parts;
     const auto kernel = r.in.z.data ? scan_grad_kernel<T, SP, SW, true> : scan_grad_kernel<T, SP, SW, false>;
-    // more than 64 KB of LDS has to be asked for
     if (bytes > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e != hipSuccess) return e;
+        static std::atomic<uint64_t> asked[2];
+        if (const hipError_t e = ask_lds(reinterpret_cast<const void*>(kernel), static_cast<int>(sizeof(float)) * grad_lds<SP, SW>(SW >= 4 ? 1 : 4 / SW), asked[r.in.z.data != nullptr]); e != hipSuccess)
+            return e;
     }
     kernel<<<static_cast<unsigned>(blocks), 64 * SW * r.plan.tile_waves, bytes, st>>>(r);
     return hipSuccess;

@@ -99,18 +99,16 @@ def _dense(t: Optional[torch.Tensor], name: str, shape, dtype, dev: int, optiona
     return t.data_ptr()
 
 
-def _result(t: Optional[torch.Tensor], name: str, shape, dtype, device, dev: int) -> torch.Tensor:
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """Memory of t's shape and type (empty_like takes half of empty's two microseconds; strides other than dense ones it must not take over)."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _result(t: Optional[torch.Tensor], name: str, shape, dtype, device, dev: int, like: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The caller's tensor, or a new one (``like``: one of the same shape and type, if there is one)."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(shape, dtype=dtype, device=device) if like is None else _like(like)
     _dense(t, name, shape, dtype, dev)
-    return t
-
-
-def _result_like(t: Optional[torch.Tensor], name: str, x: torch.Tensor, dev: int) -> torch.Tensor:
-    """A result of x's shape and type (empty_like takes half of empty's two microseconds; other strides than x's it must not take over)."""
-    if t is None:
-        return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _dense(t, name, x.shape, x.dtype, dev)
     return t
 
 
@@ -199,8 +197,8 @@ def lccrf_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
     dt, dev, D, K, strides, pw, pb, ps = _conv_args(x, weight, bias, state)
     (B, N, _), device = x.shape, x.device
     plen = _lengths(lengths, B, dev)
-    out = _result_like(out, "out", x, dev)
-    final = _result(final, "final", (B, K - 1, D), x.dtype, device, dev)
+    out = _result(out, "out", x.shape, x.dtype, None, dev, x)
+    final = _result(final, "final", (B, K - 1, D), x.dtype, device, dev, state)
     _call("lccrf_conv", dev, _lib().lccrf_conv, _Rows(x.data_ptr(), strides[0], strides[1]), dt, pw, pb, ps, plen, B, N, D, K, out.data_ptr(), final.data_ptr())
     return out, final
 
@@ -220,13 +218,11 @@ def lccrf_conv_grad(dout: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, b
     if x.dim() != 3:
         raise ValueError(f"x must be [B, N, D], got {list(x.shape)}")
     dt, dev, D, K, strides, pw, pb, ps = _conv_args(x, weight, bias, state)
-    shape, dtype, device, f32 = x.shape, x.dtype, x.device, torch.float32
+    shape, dtype, device = x.shape, x.dtype, x.device
     dstrides = _activation(dout, "dout", shape, dtype, dev)
     B, N, _ = shape
     plen = _lengths(lengths, B, dev)
-    g = ConvGrad(torch.empty(shape, dtype=dtype, device=device), torch.empty((D, K), dtype=f32, device=device),
-                 None if bias is None else torch.empty((D,), dtype=f32, device=device),
-                 None if state is None else torch.empty((B, K - 1, D), dtype=dtype, device=device))
+    g = ConvGrad(_like(x), _like(weight), None if bias is None else _like(bias), None if state is None else _like(state))
     ws = _scratch(_bytes("lccrf_conv_grad_workspace_bytes", B, N, D, K), "lccrf_conv_grad", device, workspace)
     _call("lccrf_conv_grad", dev, _lib().lccrf_conv_grad, _Rows(dout.data_ptr(), dstrides[0], dstrides[1]), _Rows(x.data_ptr(), strides[0], strides[1]), dt, pw, pb,
           ps, plen, B, N, D, K, *[0 if t is None else t.data_ptr() for t in g], ws.data_ptr(), ws.numel())
@@ -242,7 +238,7 @@ def lccrf_conv_step(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.
         raise ValueError("state is missing")
     dt, dev, D, K, strides, pw, pb, ps = _conv_args(x, weight, bias, state)
     shape = x.shape
-    out = _result_like(out, "out", x, dev)
+    out = _result(out, "out", x.shape, x.dtype, None, dev, x)
     _call("lccrf_conv_step", dev, _lib().lccrf_conv_step, x.data_ptr(), strides[0], dt, pw, pb, ps, shape[0], D, K, out.data_ptr())
     return out
 
@@ -259,13 +255,17 @@ def _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias):
         raise ValueError(f"1 to {MAX_STATES} states a channel are served, got {S}")
     if G < 1 or width % G:
         raise ValueError(f"{width} channels cannot be shared by {G} groups")
-    xs, ts = _activation(x, "x", shape, dtype, dev), _activation(dt, "dt", shape, dtype, dev)
     vectors = (*shape[:-1], G, S)
-    bs, cs = _activation(Bm, "Bm", vectors, dtype, dev), _activation(Cm, "Cm", vectors, dtype, dev)
-    if z is None:
-        pz, zs = 0, (0, 0)
-    else:
-        pz, zs = z.data_ptr(), _activation(z, "z", shape, dtype, dev)
+    xs, ts, bs, cs, zs, pz = x.stride(), dt.stride(), Bm.stride(), Cm.stride(), (0, 0, 1), 0
+    if z is not None:
+        zs, pz = z.stride(), z.data_ptr()
+    # all at once; one by one only to say what is wrong
+    if not (dt.shape == shape and Bm.shape == vectors and Cm.shape == vectors and dt.dtype is dtype and Bm.dtype is dtype and Cm.dtype is dtype
+            and xs[-1] == ts[-1] == bs[-1] == cs[-1] == zs[-1] == 1 and dt.get_device() == Bm.get_device() == Cm.get_device() == dev
+            and (z is None or (z.shape == shape and z.dtype is dtype and z.get_device() == dev))):
+        for t, name, want in ((x, "x", shape), (dt, "dt", shape), (Bm, "Bm", vectors), (Cm, "Cm", vectors), (z, "z", shape)):
+            if t is not None:
+                _activation(t, name, want, dtype, dev)
     f32 = torch.float32
     # (one position: the second stride is that of the channels, which nothing looks at)
     return code, dev, width, S, G, shape, dtype, _ScanInputs(
@@ -307,8 +307,8 @@ def lccrf_state_scan(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, Bm: tor
     plen = _lengths(lengths, B, dev)
     pstate = _dense(state, "state", (B, width, S), f32, dev, True)
     psaved = _saved_ptr(saved, shape, S, dev)
-    out = _result_like(out, "out", x, dev)
-    final = _result(final, "final", (B, width, S), f32, device, dev)
+    out = _result(out, "out", x.shape, x.dtype, None, dev, x)
+    final = _result(final, "final", (B, width, S), f32, device, dev, state)
     ws = _scratch(_bytes("lccrf_state_scan_workspace_bytes", B, N, width, S, G), "lccrf_state_scan", device, workspace)
     _call("lccrf_state_scan", dev, _lib().lccrf_state_scan, block, code, plen, B, N, width, S, G, pstate, out.data_ptr(), final.data_ptr(), psaved, ws.data_ptr(),
           ws.numel())
@@ -343,13 +343,7 @@ def lccrf_state_scan_grad(dout: torch.Tensor, x: torch.Tensor, dt: torch.Tensor,
     pstate = _dense(state, "state", (B, width, S), f32, dev, True)
     psaved = _saved_ptr(saved, shape, S, dev)
 
-    def like(shape, dtype, wanted=True):
-        return torch.empty(shape, dtype=dtype, device=device) if wanted else None
-
-    vectors = (B, N, G, S)
-    g = ScanGrad(like(shape, dtype), like(shape, dtype), like(vectors, dtype), like(vectors, dtype), like(shape, dtype, z is not None),
-                 like((width, S), f32), like((width,), f32, D is not None), like((width,), f32, dt_bias is not None),
-                 like((B, width, S), f32, state is not None))
+    g = ScanGrad(_like(x), _like(x), _like(Bm), _like(Cm), *[None if t is None else _like(t) for t in (z, A, D, dt_bias, state)])
     ws = _scratch(_bytes("lccrf_state_scan_grad_workspace_bytes", B, N, width, S, G, int(saved is not None)), "lccrf_state_scan_grad", device, workspace)
     _call("lccrf_state_scan_grad", dev, _lib().lccrf_state_scan_grad, _Rows(dout.data_ptr(), strides[0], strides[1]), block, code, plen, B, N, width, S, G, pstate,
           psaved, _ScanGrads(*[0 if t is None else t.data_ptr() for t in g]), ws.data_ptr(), ws.numel())
@@ -365,6 +359,6 @@ def lccrf_state_step(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, Bm: tor
     code, dev, width, S, G, shape, dtype, block = _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias)
     B = shape[0]
     pstate = _dense(state, "state", (B, width, S), torch.float32, dev)
-    out = _result_like(out, "out", x, dev)
+    out = _result(out, "out", x.shape, x.dtype, None, dev, x)
     _call("lccrf_state_step", dev, _lib().lccrf_state_step, block, code, B, width, S, G, pstate, out.data_ptr())
     return out
