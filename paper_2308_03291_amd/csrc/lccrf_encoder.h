@@ -93,7 +93,8 @@ __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf
 // log(1 + exp(v)) and its derivative.  With e = exp(-|v|): max(v, 0) + log1p(e), and log1p(e) = e (1 + e q(e)) with q of degree 8
 // fitted to it on [0, 1] (off by at most 1.4 units in the last place): a logarithm of 1 + e would lose the steps near 0.001 that
 // such scans live on.  e is exp2(t), t = -|v| log2(e) rounded, times 1 + (-|v| - t ln2): the rounding of t alone would cost 2^-20
-// at |v| = 16.  exp(-126) is 0 in float already, so -|v| may stop there; a NaN stays one.
+// at |v| = 16.  exp(-126) is 0 in float already, so -|v| may stop there; a NaN stays one
+// (this maximum, unlike fmaxf, hands it on).
 struct Softplus { float value, slope; };
 __device__ __forceinline__ Softplus softplus(float v) {
     const float a = fmaxf(-fabsf(v), -126.0f);
@@ -111,8 +112,8 @@ __device__ __forceinline__ Softplus softplus(float v) {
     q = fmaf(q, e, 0.3333289325237274f);
     q = fmaf(q, e, -0.49999997f);
     q = fmaf(q, e, 1.0f);
-    const float value = fmaf(q, e, fmaxf(v, 0.0f)), r = __builtin_amdgcn_rcpf(1.0f + e);
-    return {v == v ? value : v, v >= 0.0f ? r : e * r};
+    const float r = __builtin_amdgcn_rcpf(1.0f + e);
+    return {fmaf(q, e, __builtin_elementwise_maximum(v, 0.0f)), v >= 0.0f ? r : e * r};
 }
 
 // Rows of an input: element strides between sequences and positions.
