@@ -26,26 +26,31 @@ struct ScanRun {
 // SW waves share a tile's states, SP each (more than 16 states: two or four).  Alone, a wave keeps all it knows of a position in
 // registers; together they share the positions (sw, sw + SW, ... are this wave's: it computes their steps and finishes their outputs) and
 // meet in LDS.
-template <typename T, int SP, int SW, int MODE, bool GATED>
+template <typename T, int SP, int SW, int MODE, bool GATED, bool FLAT>
 __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
-    extern __shared__ float lds[];  // [waves][kP][2 * SP]; SW > 1: then steps and step x [2][kP][64], sums over the states [SW][kP][64]
+    constexpr int kSet = kP * 2 * SP, kBc = FLAT ? 2 * kSet + 4 : kSet;  // FLAT: the second group's vectors, four banks on
+    extern __shared__ float lds[];  // [waves][kBc]; SW > 1: then steps and step x [2][kP][64], sums over the states [SW][kP][64]
     constexpr int P = kP / SW;
     const ScanIn& in = r.in;
-    const int lane = threadIdx.x & 63, tiles = in.G * r.plan.tiles;
+    const int lane = threadIdx.x & 63, tiles = r.plan.all_tiles;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned at_work = SW > 1 ? blockIdx.x : blockIdx.x * (blockDim.x >> 6) + wave, which = at_work / tiles;
     const int tile = at_work - which * tiles, sw = SW > 1 ? wave : 0, s0 = sw * SP;
-    float* bc = lds + wave * (kP * 2 * SP);
-    float* shared = lds + SW * (kP * 2 * SP) + lane;
+    float* bc = lds + wave * kBc;
+    float* shared = lds + SW * kBc + lane;
     float* sums = shared + 2 * kP * 64;
     int b = which / r.plan.segments;
     const int seg = which - b * r.plan.segments;
     // Whole sequences, as many waves as there is room for at once: long ones first, then the short ones from the shortest on, so that a
     // SIMD's waves are about as long together everywhere.
     if (r.plan.segments == 1) b = ranked(in.lengths, in.B, in.N, b < (in.B + 1) / 2 ? b : in.B - 1 - (b - (in.B + 1) / 2), lane);
-    const int width = in.D_ / in.G, group = tile / r.plan.tiles, c0 = (tile - group * r.plan.tiles) * 64 + lane;
-    const bool is = c0 < width;
-    const int d = group * width + (is ? c0 : width - 1);
+    const int width = in.D_ / in.G, group = FLAT ? tile * 64 / width : tile / r.plan.tiles;
+    const int first = FLAT ? 0 : group * width, wide = FLAT ? in.D_ : width;  // the channels that the tiles are cut from
+    const int c0 = (FLAT ? tile : tile - group * r.plan.tiles) * 64 + lane;
+    const bool is = c0 < wide;
+    const int d = first + (is ? c0 : wide - 1);
+    const int next_group = group + 1 < in.G ? group + 1 : group;
+    const f32x4* bc4 = reinterpret_cast<const f32x4*>(bc + (FLAT && d / width != group ? kSet + 4 : 0));
     const int len = clamp_length(in.lengths, b, in.N), begin = seg * r.plan.seg_len;
     const int stop = begin + r.plan.seg_len < in.N ? begin + r.plan.seg_len : in.N, end = stop < len ? stop : len;
     const unsigned bytes = static_cast<unsigned>(d) * sizeof(T);
@@ -73,13 +78,14 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
 
     if (begin < end) {
         T xr[P], tr[P], zr[P];
-        GroupVectors<T, SP> gv;
+        GroupVectors<T, SP> gv, gv2;  // (FLAT: and of the next group)
         const T *px = at<T>(in.x, b, begin + sw), *pt = at<T>(in.dt, b, begin + sw), *pz = at<T>(in.z, b, begin + sw);
         const auto fetch_whole = [&](int ahead) {
             px += ahead * kP * in.x.row;
             pt += ahead * kP * in.dt.row;
             pz += ahead * kP * in.z.row;
             gv.next(in, ahead);
+            if (FLAT) gv2.next(in, ahead);
             load_whole<T, P>(px, SW * in.x.row, bytes, xr);
             load_whole<T, P>(pt, SW * in.dt.row, bytes, tr);
             if (GATED) load_whole<T, P>(pz, SW * in.z.row, bytes, zr);
@@ -104,6 +110,7 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
             }
             wave_sync();
             gv.template put<WHOLE>(bc, l0, len, lane);
+            if (FLAT) gv2.template put<WHOLE>(bc + kSet + 4, l0, len, lane);
             wave_sync();
         };
         const auto block = [&](auto whole, int l0) {
@@ -116,7 +123,6 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
             }
             // The next block, or behind the last whole one that one again: without a branch nothing has to wait for it here.
             if (WHOLE) fetch_whole(l0 + 2 * kP <= end);
-            const f32x4* bc4 = reinterpret_cast<const f32x4*>(bc);
             constexpr int Q = SP / 4, R = MODE & kOut ? 2 * Q : Q;
             f32x4 v[2][R];  // Bm and Cm of a position; the next one's are read while this one's are used
 #pragma unroll
@@ -182,6 +188,7 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
             if (SW > 1) __syncthreads();  // steps are there for the other waves, sums are free
         };
         gv.place(in, b, begin, group, s0, lane);
+        if (FLAT) gv2.place(in, b, begin, next_group, s0, lane);
         int l0 = begin;
         if (begin + kP <= end) {
             fetch_whole(0);
@@ -192,6 +199,10 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
         if (l0 < end) {
             gv.place(in, b, l0, group, s0, lane);
             gv.load(in, l0, len);
+            if (FLAT) {
+                gv2.place(in, b, l0, next_group, s0, lane);
+                gv2.load(in, l0, len);
+            }
             load_rows<T, P>(in.x, b, l0 + sw, SW, len, bytes, xr);
             load_rows<T, P>(in.dt, b, l0 + sw, SW, len, bytes, tr);
             if (GATED) load_rows<T, P>(in.z, b, l0 + sw, SW, len, bytes, zr);
@@ -344,10 +355,13 @@ hipError_t step_of(const ScanIn& in, float* state, void* out, hipStream_t st) {
 
 template <typename T, int SP, int SW, int MODE>
 void scan_launch(const ScanRun& r, hipStream_t st) {
-    const int64_t tiles = static_cast<int64_t>(r.in.G) * r.plan.tiles * r.in.B * r.plan.segments;
-    const auto kernel = (MODE & kOut) && r.in.z.data ? scan_kernel<T, SP, SW, MODE, (MODE & kOut) != 0> : scan_kernel<T, SP, SW, MODE, false>;
-    const int w = SW > 1 ? SW : waves_together(r.in.G * r.plan.tiles);
-    const size_t bytes = sizeof(float) * (w * kP * 2 * SP + (SW > 1 ? (2 + SW) * kP * 64 : 0));
+    const int64_t tiles = static_cast<int64_t>(r.plan.all_tiles) * r.in.B * r.plan.segments;
+    constexpr bool kGate = (MODE & kOut) != 0, kFlat = SW == 1;
+    const bool gated = kGate && r.in.z.data;
+    const auto kernel = r.plan.flat ? (gated ? scan_kernel<T, SP, SW, MODE, kGate, kFlat> : scan_kernel<T, SP, SW, MODE, false, kFlat>)
+                                    : (gated ? scan_kernel<T, SP, SW, MODE, kGate, false> : scan_kernel<T, SP, SW, MODE, false, false>);
+    const int w = SW > 1 ? SW : waves_together(r.plan.all_tiles);
+    const size_t bytes = sizeof(float) * (w * (r.plan.flat ? 2 * kP * 2 * SP + 4 : kP * 2 * SP) + (SW > 1 ? (2 + SW) * kP * 64 : 0));
     kernel<<<static_cast<unsigned>(tiles * SW / w), 64 * w, bytes, st>>>(r);
 }
 
