@@ -229,11 +229,13 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
     }
 }
 
-// A thread has four states of a channel and goes from segment to segment.
+// A thread has four states of a channel and goes from segment to segment.  There are few of them, so workgroups are small: every compute
+// unit has its own way to memory (56 segments of B=4 D=514 S=16: 8 us, in workgroups of 256 14).
+constexpr int kJoin = 64;
 template <bool BACK>
-__global__ __launch_bounds__(256) void join_segments_kernel(ScanIn in, ScanPlan p, const float* __restrict__ state, float* __restrict__ ends,
+__global__ __launch_bounds__(kJoin) void join_segments_kernel(ScanIn in, ScanPlan p, const float* __restrict__ state, float* __restrict__ ends,
                                                             const float* __restrict__ steps) {
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * kJoin + threadIdx.x;
     const int64_t rest = id / in.D_;
     const int d = static_cast<int>(id - rest * in.D_), q = static_cast<int>(rest % quads(in.S));
     const int64_t b = rest / quads(in.S);
@@ -245,28 +247,33 @@ __global__ __launch_bounds__(256) void join_segments_kernel(ScanIn in, ScanPlan 
         A[j] = s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s]) : 0.0f;
         h[j] = state && s < in.S ? state[(b * in.D_ + d) * in.S + s] : 0.0f;
     }
-    constexpr int U = 8;
-    for (int k0 = 0; k0 < p.segments; k0 += U) {
-        f32x4 e[U];
-        float t[U];
+    // From the first segment on, or from the last: places and strides of `ends` and `steps`.
+    const int64_t first = b * p.segments + (BACK ? p.segments - 1 : 0);
+    const int64_t e_stride = (BACK ? -4 : 4) * static_cast<int64_t>(quads(in.S)) * in.D_, t_stride = BACK ? -in.D_ : in.D_;
+    float* e = ends + quad_at(first, in.S, in.D_, q, d);
+    const float* t = steps + first * in.D_ + d;
+    const auto some = [&](auto many) {  // that many segments, their loads in flight together: the way along them is all waiting
+        constexpr int U = decltype(many)::value;
+        f32x4 made[U];
+        float step[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int k = k0 + u < p.segments ? k0 + u : p.segments - 1;
-            const int64_t seg = b * p.segments + (BACK ? p.segments - 1 - k : k);
-            e[u] = *reinterpret_cast<const f32x4*>(ends + quad_at(seg, in.S, in.D_, q, d));
-            t[u] = steps[seg * in.D_ + d];
+            made[u] = *reinterpret_cast<const f32x4*>(e + u * e_stride);
+            step[u] = t[u * t_stride];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int k = k0 + u;
-            if (k < p.segments) {
-                const int64_t seg = b * p.segments + (BACK ? p.segments - 1 - k : k);
-                *reinterpret_cast<f32x4*>(ends + quad_at(seg, in.S, in.D_, q, d)) = f32x4{h[0], h[1], h[2], h[3]};
+            *reinterpret_cast<f32x4*>(e) = f32x4{h[0], h[1], h[2], h[3]};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) h[j] = fmaf(exp2_fast(t[u] * A[j]), h[j], 4 * q + j < in.S ? e[u][j] : 0.0f);
-            }
+            for (int j = 0; j < 4; ++j) h[j] = fmaf(exp2_fast(step[u] * A[j]), h[j], 4 * q + j < in.S ? made[u][j] : 0.0f);
+            e += e_stride;
         }
-    }
+        t += U * t_stride;
+    };
+    int k = 0;
+    for (; k + 16 <= p.segments; k += 16) some(std::integral_constant<int, 16>{});
+    for (; k + 4 <= p.segments; k += 4) some(std::integral_constant<int, 4>{});
+    for (; k < p.segments; ++k) some(std::integral_constant<int, 1>{});
 }
 
 // ---- one position ---------------------------------------------------------------------------------------------
@@ -393,9 +400,9 @@ size_t ends_bytes(const ScanPlan& p, int B, int D, int S) {
 
 hipError_t launch_join_segments(const ScanIn& in, const ScanPlan& p, const float* state, float* ends, const float* steps, bool back, hipStream_t st) {
     const int64_t threads = static_cast<int64_t>(in.B) * in.D_ * quads(in.S);
-    const unsigned blocks = static_cast<unsigned>((threads + 255) / 256);
-    if (back) join_segments_kernel<true><<<blocks, 256, 0, st>>>(in, p, state, ends, steps);
-    else join_segments_kernel<false><<<blocks, 256, 0, st>>>(in, p, state, ends, steps);
+    const unsigned blocks = static_cast<unsigned>((threads + kJoin - 1) / kJoin);
+    if (back) join_segments_kernel<true><<<blocks, kJoin, 0, st>>>(in, p, state, ends, steps);
+    else join_segments_kernel<false><<<blocks, kJoin, 0, st>>>(in, p, state, ends, steps);
     return hipGetLastError();
 }
 

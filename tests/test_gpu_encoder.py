@@ -248,6 +248,29 @@ def test_scan_shapes(crf, t, gate, rich, carry, ragged, B, N, D, S, G):
     check_scan(crf, inputs, lens, state, strided(g, B, N, D, dtype=t), saved=gate)
 
 
+@pytest.mark.parametrize("S", (3, 8, 16, 24))
+@pytest.mark.parametrize("D,G", [(201, 3), (130, 2), (260, 4), (1001, 7), (258, 2)])
+def test_groups_that_fill_no_tile(crf, S, D, G):
+    """Waves that reach from a group into the next."""
+    g = generator(S * D)
+    inputs = scan_inputs(g, torch.float32, 3, 83, D, S, G, gate=D != 130)
+    check_scan(crf, inputs, conv_lengths(3, 83, g), normal(g, 3, D, S), normal(g, 3, 83, D))
+
+
+def test_what_is_not_a_number_stays_in_its_channel(crf):
+    g = generator(44)
+    inputs = scan_inputs(g, torch.float32, 2, 40, 70, 16, 1)
+    want, _ = crf.lccrf_state_scan(*inputs.values())
+    inputs["dt"] = inputs["dt"].clone()
+    inputs["dt"][1, 11, 5] = float("nan")
+    out, final = crf.lccrf_state_scan(*inputs.values())
+    assert torch.isnan(out[1, 11:, 5]).all() and torch.isnan(final[1, 5]).all()
+    out[1, 11:, 5] = want[1, 11:, 5]
+    assert torch.equal(out, want)
+    ids = torch.tensor([0, 2], dtype=torch.int32, device=DEV)
+    assert torch.isnan(crf.lccrf_embed(inputs["dt"][1, 9:12], ids)).nonzero().tolist() == [[1, 5]]
+
+
 @pytest.mark.parametrize("t", TYPES)
 def test_scan_of_a_long_sequence(crf, t):
     """Cut into segments, every one of them needed: slow decays carry the first positions to the end."""
