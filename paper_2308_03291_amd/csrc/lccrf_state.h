@@ -19,7 +19,6 @@ namespace enc {
 
 constexpr int kP = kScanBlock;
 
-
 struct ScanPlan {
     int tiles;      // waves that cover a group's channels
     int all_tiles;  // and all groups' (forward pass, `flat`: tiles run on from a group into the next)

@@ -3,12 +3,16 @@
 // With dh[l] = dy[l] Cm[l] + a[l+1] dh[l+1] running backwards,
 //     dCm = sum_channels dy h,   dBm = sum_channels dh put,   dput = sum_s dh Bm,   back = dh a h[l-1]  (by the decay's logarithm),
 //     dx = dput step + D dy,     dv = (dput x + sum_s back A) sigmoid(v),    dA = sum_positions back step.
-// The states in front of every eighth position are saved by the forward pass; eight positions are run again from there, states
-// and decays kept in registers, and then gone through backwards.  About 22 issue slots an update with 16 states: vector arithmetic bounds it.
+// The states in front of every eighth position are saved by the forward pass; eight positions are run again from there, their
+// states kept in registers, and then gone through backwards.  27 vector instructions an update with 16 states (counted: 5 forwards, 10
+// backwards, the rest for sums over the channels and what is computed once a channel), two of them exponentials: vector arithmetic
+// bounds it (B=128 N=256 D=1024 S=16, bfloat16, ragged: 345 us, the vector pipes busy 95 % of them).
 //
-// A wave has 64 channels and up to 8 states (128 registers of states and decays of eight positions; with 16 states a wave the registers that remain hold
-// neither the next positions' inputs nor a second and third wave's work, and it took three times as long); more states are shared by
-// several waves of a workgroup, which also share what is computed once a channel, and whose sums over the states meet in LDS.
+// A wave has 64 channels and up to 8 states: 72 registers of states, three waves a SIMD.  Measured on the whole training step of that
+// batch: 16 states a wave spilled, and left no registers for the next positions' inputs (1290 us against 536 at that time); the
+// decays kept as well would save the second exponential, but take 64 registers and with them the third wave (470 us against 448).
+// More states are shared by several waves of a workgroup, which also share what is computed once a channel, and whose sums over
+// the states meet in LDS.
 // The sums over the channels are taken by halving: two registers and two halves of the wave become one register whose
 // halves hold one sum each (a swap and an addition), and so on, 35 instructions for the 16 sums of a position; the waves of a
 // workgroup meet in LDS, workgroups through memory, always in the same order.
@@ -68,17 +72,12 @@ __device__ __forceinline__ float halve16(float x, float y) {
 // The rest of the way for n = SP / 2 registers, each of which holds two sums of every half of the wave (halve32 of dBm and dCm of a
 // state, halve16 of states s and s + n): lane k ends with sum k / (32 / SP) of (dBm of all states, dCm of all states).
 template <int N> __device__ __forceinline__ float lane_sums(float (&v)[N], int lane) {
-    static_assert(N == 2 || N == 4 || N == 8, "");
+    static_assert(N == 2 || N == 4, "");
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) v[i] = halve<kRor8>(v[i], v[i + N / 2], lane & 8);
-    if constexpr (N >= 4) {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) v[i] = halve<kHalfMirror>(v[i], v[i + N / 4], lane & 4);
-    } else {
-        v[0] += from_lane<kHalfMirror>(v[0]);
-    }
-    if constexpr (N >= 8) v[0] = halve<kXor2>(v[0], v[1], lane & 2);
-    else v[0] += from_lane<kXor2>(v[0]);
+    if constexpr (N == 4) v[0] = halve<kHalfMirror>(v[0], v[1], lane & 4);
+    else v[0] += from_lane<kHalfMirror>(v[0]);
+    v[0] += from_lane<kXor2>(v[0]);
     return v[0] + from_lane<kXor1>(v[0]);
 }
 
