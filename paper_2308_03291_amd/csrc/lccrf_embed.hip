@@ -361,13 +361,7 @@ hipError_t embed_grad_of(AnyRows dout, const int32_t* ids, int B, int N, int V, 
     if (const hipError_t e = ask_lds(reinterpret_cast<const void*>(index_kernel), static_cast<int>(sizeof(int32_t)) * kIndexWaves * (kMaxRange + kKept), asked); e != hipSuccess)
         return e;
     index_kernel<<<plan.workgroups, kIndexThreads, bytes, st>>>(ids, n, V, plan.range, order, start);
-    // Past the caches where the gradients that are read have use for them, or the table is more than the memory-side cache holds (256 MB).
-    // With a position for eight rows and fewer there is little to read, and rows that begin anywhere are better put together there, us
-    // through / past: 1653 positions into 93091 rows of 666 floats 45 / 77, 2048 into 500000 of 100 bfloat16 33 / 59, into 100003 of 512 floats
-    // 37 / 45, 8192 into 100003 of 1024 bfloat16 42 / 46.  More positions: 8192 into 50000 of 1024 floats 54 / 47, 32768 into 100003 of 1024
-    // bfloat16 92 / 63 (but 32768 into 100000 of 301 floats 50 / 62).  More than 256 MB: 8000 into 70000 of 2001 bfloat16 108 / 90.
-    const int64_t table_bytes = static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T));
-    const bool stream = past_caches(table_bytes) && (int64_t{n} * 8 > V || table_bytes > int64_t{256} << 20);
+    const bool stream = past_caches(static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T)));
     const auto rows = four ? (stream ? rows_kernel<T, SMALL, 4, true> : rows_kernel<T, SMALL, 4, false>)
                            : (stream ? rows_kernel<T, SMALL, 1, true> : rows_kernel<T, SMALL, 1, false>);
     rows<<<static_cast<unsigned>(piece_blocks + row_blocks), 256, 0, st>>>(a, dout.as<T>(), static_cast<T*>(grad), static_cast<int>(piece_blocks));
