@@ -89,11 +89,32 @@ __device__ __forceinline__ void four_ids(const int32_t* __restrict__ ids, int p,
     }
 }
 
+// This workgroup's share of `bytes` zeros from p on (elements of two bytes and more): 16-byte pieces, one a thread in turn over
+// the whole launch, so that the chip writes one place after the other; the ends, by twos, are the first workgroup's.
+__device__ __forceinline__ void clear(char* p, int64_t bytes, int t) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    int64_t head = -reinterpret_cast<intptr_t>(p) & 15;
+    if (head > bytes) head = bytes;
+    const int64_t pieces = (bytes - head) / 16, tail = bytes - head - pieces * 16;
+    u32x4* const whole = reinterpret_cast<u32x4*>(p + head);
+    const int64_t all = static_cast<int64_t>(gridDim.x) * kIndexThreads;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kIndexThreads + t; i < pieces; i += all) __builtin_nontemporal_store(u32x4{}, whole + i);
+    if (blockIdx.x == 0) {
+        if (2 * t < head) reinterpret_cast<uint16_t*>(p)[t] = 0;
+        if (2 * t < tail) reinterpret_cast<uint16_t*>(whole + pieces)[t] = 0;
+    }
+}
+
+// zero: the table's gradient of zero_bytes, which this launch clears as well; or null.  Workgroups behind the last range have only that to do.
 __global__ __launch_bounds__(kIndexThreads) void index_kernel(const int32_t* __restrict__ ids, int n, int V, int range, int32_t* __restrict__ order,
-                                                              int32_t* __restrict__ start) {
+                                                              int32_t* __restrict__ start, char* __restrict__ zero, int64_t zero_bytes) {
     extern __shared__ int32_t lds[];  // counters [kIndexWaves][range], then kept positions with their tokens [kIndexWaves][kKept]
     __shared__ int32_t wave_sum[kIndexWaves], below_sum[kIndexWaves];
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    if (static_cast<int64_t>(blockIdx.x) * range >= V) {
+        clear(zero, zero_bytes, t);
+        return;
+    }
     const int lo = blockIdx.x * range, hi = lo + range < V ? lo + range : V;
     const unsigned here = hi - lo;
     int32_t* const count = lds;
@@ -203,6 +224,7 @@ __global__ __launch_bounds__(kIndexThreads) void index_kernel(const int32_t* __r
             for (int i = 0; i < 4; ++i) place(static_cast<unsigned>(id[i] - lo) < here, id[i] - lo, p0 + 4 * lane + i);
         }
     }
+    if (zero) clear(zero, zero_bytes, t);
 }
 
 struct GradArgs {
@@ -241,7 +263,8 @@ __device__ __forceinline__ void sum_rows(const GradArgs& a, Rows<T> dout, int fr
 
 // The first `piece_blocks` workgroups: partial sums of long rows.  Slot 0 of piece j is for the row that its first
 // position belongs to, slot 1 for the one of its last position, if that is another: a row of more than `piece` positions
-// reaches over an end of every piece it has a part in.
+// reaches over an end of every piece it has a part in.  The others: ROWS rows a thread, or with ROWS = 0, where the rows are cleared
+// already, the row that begins at a sorted position, if one does.
 template <typename T, bool SMALL, int ROWS, bool STREAM>
 __global__ __launch_bounds__(256) void rows_kernel(GradArgs a, Rows<T> dout, T* __restrict__ grad, int piece_blocks) {
     constexpr int W = Wide<T>::V;
@@ -264,9 +287,20 @@ __global__ __launch_bounds__(256) void rows_kernel(GradArgs a, Rows<T> dout, T* 
         return;
     }
     const int64_t k = static_cast<int64_t>(blockIdx.x - piece_blocks) * 256 + threadIdx.x;
+    const int c = piece_start<W, SMALL>(static_cast<int>(k % a.cpr), a.D);
+    if constexpr (ROWS == 0) {
+        const int64_t from = k / a.cpr;
+        if (from >= a.start[a.V]) return;
+        const int row = a.ids[a.order[from]], s = a.start[row], e = a.start[row + 1];
+        if (s != from || e - s > a.piece) return;
+        sum_rows<T, W, SMALL>(a, dout, s, e, c, sum);
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum[j] *= a.scale;
+        Piece<T, W, SMALL>::template put<STREAM>(grad + static_cast<int64_t>(row) * a.D + c, a.D, sum);
+        return;
+    }
     const int64_t row0 = k / a.cpr * ROWS;
     if (row0 >= a.V) return;
-    const int c = piece_start<W, SMALL>(static_cast<int>(k % a.cpr), a.D);
     int s[ROWS + 1];
 #pragma unroll
     for (int i = 0; i <= ROWS; ++i) s[i] = a.start[row0 + i < a.V ? row0 + i : a.V];
@@ -328,6 +362,13 @@ __global__ __launch_bounds__(256) void join_kernel(GradArgs a, T* __restrict__ g
 inline int piece_of(int64_t n) { return n >= 16384 ? 128 : 32; }
 inline int64_t pieces_of(int64_t n) { return n > piece_of(n) ? (n + piece_of(n) - 1) / piece_of(n) : 0; }
 
+// Rows whose ends lie inside a line of memory (128 bytes) are written past the caches in parts of lines; where few of them hold
+// anything, the index clears all rows in one sweep of whole lines and the rows that hold something are written once more.  us, swept / row
+// by row (results in turn in five places): 1653 positions into 93091 rows of 666 floats 59 / 77, 4096 into 98000 64 / 82, 2048 into 500000 of
+// 100 bfloat16 36 / 58, 512 into 300000 of 33 floats 23 / 32; at eight rows a position 8192 into 65536 of 666 floats 53 / 59, 2048 into
+// 16384 22.3 / 21.4; at three 32768 into 100000 of 301 floats 62 / 61.  Rows of whole lines: 2048 into 100003 of 512 floats 50 / 44.
+inline bool rows_are_few(int64_t n, int V, int64_t row_bytes) { return V >= 8 * n && row_bytes % 128 != 0 && past_caches(V * row_bytes); }
+
 template <typename T, bool SMALL>
 hipError_t embed_of(const void* table, int V, int D, int64_t table_row, const int32_t* ids, int64_t n, float scale, void* out, hipStream_t st) {
     const int cpr = (D + Wide<T>::V - 1) / Wide<T>::V;
@@ -354,17 +395,19 @@ hipError_t embed_grad_of(AnyRows dout, const int32_t* ids, int B, int N, int V, 
     const int64_t piece_blocks = (2 * pieces * cpr + 255) / 256;
     // Four rows a thread once that leaves a quarter of a million threads: their starts are loaded together, and rows of zeros cost little else.
     const bool four = static_cast<int64_t>(V) * cpr >= (int64_t{1} << 20);
-    const int64_t row_blocks = ((four ? (V + 3) / 4 : V) * static_cast<int64_t>(cpr) + 255) / 256;
+    const bool sparse = rows_are_few(n, V, D * static_cast<int64_t>(sizeof(T)));
+    const int64_t row_blocks = ((sparse ? n : four ? (V + 3) / 4 : V) * static_cast<int64_t>(cpr) + 255) / 256;
     if (!fits(piece_blocks + row_blocks, 256)) return hipErrorInvalidValue;
     const int bytes = static_cast<int>(sizeof(int32_t)) * kIndexWaves * (plan.range + kKept);
     static std::atomic<uint64_t> asked{0};
     if (const hipError_t e = ask_lds(reinterpret_cast<const void*>(index_kernel), static_cast<int>(sizeof(int32_t)) * kIndexWaves * (kMaxRange + kKept), asked); e != hipSuccess)
         return e;
-    index_kernel<<<plan.workgroups, kIndexThreads, bytes, st>>>(ids, n, V, plan.range, order, start);
-    const bool stream = past_caches(static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T)));
-    const auto rows = four ? (stream ? rows_kernel<T, SMALL, 4, true> : rows_kernel<T, SMALL, 4, false>)
+    const int64_t table_bytes = static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T));
+    const bool stream = past_caches(table_bytes);
+    index_kernel<<<sparse && plan.workgroups < 256 ? 256 : plan.workgroups, kIndexThreads, bytes, st>>>(ids, n, V, plan.range, order, start, sparse ? static_cast<char*>(grad) : nullptr, table_bytes);
+    const auto rows = sparse ? rows_kernel<T, SMALL, 0, false> : four ? (stream ? rows_kernel<T, SMALL, 4, true> : rows_kernel<T, SMALL, 4, false>)
                            : (stream ? rows_kernel<T, SMALL, 1, true> : rows_kernel<T, SMALL, 1, false>);
-    rows<<<static_cast<unsigned>(piece_blocks + row_blocks), 256, 0, st>>>(a, dout.as<T>(), static_cast<T*>(grad), static_cast<int>(piece_blocks));
+    if (piece_blocks + row_blocks) rows<<<static_cast<unsigned>(piece_blocks + row_blocks), 256, 0, st>>>(a, dout.as<T>(), static_cast<T*>(grad), static_cast<int>(piece_blocks));
     if (pieces) join_kernel<T, SMALL><<<static_cast<unsigned>((pieces * cpr + 255) / 256), 256, 0, st>>>(a, static_cast<T*>(grad));
     return hipGetLastError();
 }

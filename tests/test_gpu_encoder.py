@@ -117,6 +117,30 @@ def test_embed_grad(crf, t, kind, V, D, B, N):
         assert torch.equal(got, crf.lccrf_embed_grad(dout, ids, V, scale=1.5)), "not the same again"
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("offset", (0, 1, 3))
+@pytest.mark.parametrize("V,D,B,N", [(180001, 101, 3, 41), (9001, 2001, 2, 40), (300007, 60, 1, 1), (180001, 101, 0, 5)])
+def test_embed_grad_of_few_positions(crf, t, offset, V, D, B, N):
+    """Tables of which few rows hold anything, rows and the table itself beginning anywhere; one token holds half of the positions."""
+    g = generator(V + D + B * N + offset)
+    ids = torch.randint(0, V, (B, N), generator=g, device=DEV, dtype=torch.int32)
+    if B:
+        ids.view(-1)[::2] = V - 1
+        ids.view(-1)[0] = 0
+    dout = normal(g, B, N, D, dtype=t)
+    memory = torch.full((V * D + 16,), float("nan"), dtype=t, device=DEV)
+    out = memory[offset:offset + V * D].view(V, D)
+    got = crf.lccrf_embed_grad(dout, ids, V, scale=0.7, out=out)
+    assert got.data_ptr() == out.data_ptr()
+    assert bool(memory[:offset].isnan().all()) and bool(memory[offset + V * D:].isnan().all())
+    held = torch.unique(ids.flatten().long())
+    if B:
+        check(got[held], ref.embed_grad(dout, ids, V, 0.7)[held.cpu()], ref.embed_grad(dout, ids, V, 0.7, absolute=True)[held.cpu()], B * N + 2, "grad")
+    empty = torch.ones(V, dtype=torch.bool, device=DEV)
+    empty[held] = False
+    assert not bool(got[empty].count_nonzero())
+
+
 def test_embed_grad_of_nothing(crf):
     out = crf.lccrf_embed_grad(torch.empty(0, 5, 8, device=DEV), torch.empty(0, 5, dtype=torch.int32, device=DEV), 70)
     assert out.shape == (70, 8) and (out == 0).all()
