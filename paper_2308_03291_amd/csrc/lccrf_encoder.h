@@ -163,9 +163,9 @@ hipError_t launch_state_scan_grad(int dtype, AnyRows dout, const ScanIn& in, con
                                   hipStream_t st);
 hipError_t launch_state_step(int dtype, const ScanIn& in, float* state, void* out, hipStream_t st);
 
-// Results that the L2 caches could not hold (eight of 4 MB) are written past them, us past / through them: embedding gradient of
-// 205 MB 63 / 91; lookup of 67 MB 14.1 / 15.0; convolution and gradient of 66 MB each 67 / 74, ragged; convolutions alone of 66 MB with an
-// odd width 32.6 / 38.6, of 268 MB 107 / 111, of 537 MB 234 / 237; it loses at two, of 134 MB with even widths (66.6 / 62, 50.8 / 47.2).
+// Results that the L2 caches could not hold (eight of 4 MB) are written past them, us past / through them (inputs and results in turn in
+// several places): lookup of 67 MB 13.7 / 23.1; embedding gradient of 205 MB 76 / 96; convolutions of 67 MB 35 / 41, 134 MB 62.5 / 64.4, 268 MB
+// 106 / 110, 537 MB 232 / 235, of 66 MB with an odd width 41 / 47; convolution and gradient of 134 MB each 147 / 157.
 inline bool past_caches(int64_t bytes) { return bytes > (int64_t{32} << 20); }
 // A launch has fewer than 2^32 threads; the entry points refuse what would take more.
 inline bool fits(int64_t blocks, int threads) { return blocks * threads < (int64_t{1} << 32); }
