@@ -302,6 +302,7 @@ hipError_t conv_grad_of(ConvArgs a, void* dx, float* dweight, float* dbias, void
     const bool stream = past_caches(static_cast<int64_t>(a.B) * a.N * a.D * static_cast<int64_t>(sizeof(T)));
     const auto kernel = a.D < 4 ? conv_grad_kernel<T, K, true, false> : stream ? conv_grad_kernel<T, K, false, true> : conv_grad_kernel<T, K, false, false>;
     kernel<<<grid, 256, sizeof(float) * 256 * (K + 1) * 4, st>>>(a, static_cast<T*>(dx), static_cast<T*>(dstate), partial, p.lx);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     conv_sums_kernel<K><<<dim3((a.D + 63) / 64, K + 1), 1024, 0, st>>>(partial, p.high, a.D, dweight, dbias);
     return hipGetLastError();
 }

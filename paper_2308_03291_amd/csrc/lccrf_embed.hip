@@ -405,9 +405,11 @@ hipError_t embed_grad_of(AnyRows dout, const int32_t* ids, int B, int N, int V, 
     const int64_t table_bytes = static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T));
     const bool stream = past_caches(table_bytes);
     index_kernel<<<sparse && plan.workgroups < 256 ? 256 : plan.workgroups, kIndexThreads, bytes, st>>>(ids, n, V, plan.range, order, start, sparse ? static_cast<char*>(grad) : nullptr, table_bytes);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const auto rows = sparse ? rows_kernel<T, SMALL, 0, false> : four ? (stream ? rows_kernel<T, SMALL, 4, true> : rows_kernel<T, SMALL, 4, false>)
                            : (stream ? rows_kernel<T, SMALL, 1, true> : rows_kernel<T, SMALL, 1, false>);
     if (piece_blocks + row_blocks) rows<<<static_cast<unsigned>(piece_blocks + row_blocks), 256, 0, st>>>(a, dout.as<T>(), static_cast<T*>(grad), static_cast<int>(piece_blocks));
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (pieces) join_kernel<T, SMALL><<<static_cast<unsigned>((pieces * cpr + 255) / 256), 256, 0, st>>>(a, static_cast<T*>(grad));
     return hipGetLastError();
 }

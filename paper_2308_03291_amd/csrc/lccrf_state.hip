@@ -364,7 +364,7 @@ hipError_t step_of(const ScanIn& in, float* state, void* out, hipStream_t st) {
 // ---- launches -------------------------------------------------------------------------------------------------
 
 template <typename T, int SP, int SW, int MODE>
-void scan_launch(const ScanRun& r, hipStream_t st) {
+hipError_t scan_launch(const ScanRun& r, hipStream_t st) {
     const int64_t tiles = static_cast<int64_t>(r.plan.all_tiles) * r.in.B * r.plan.segments;
     constexpr bool kGate = (MODE & kOut) != 0, kFlat = SW == 1;
     const bool gated = kGate && r.in.z.data;
@@ -373,26 +373,25 @@ void scan_launch(const ScanRun& r, hipStream_t st) {
     const int w = SW > 1 ? SW : waves_together(r.plan.all_tiles);
     const size_t bytes = sizeof(float) * (w * (r.plan.flat ? 2 * kP * 2 * SP + 4 : kP * 2 * SP) + (SW > 1 ? (2 + SW) * kP * 64 : 0));
     kernel<<<static_cast<unsigned>(tiles * SW / w), 64 * w, bytes, st>>>(r);
+    return hipGetLastError();
 }
 
 template <typename T, int SP, int SW>
-void scan_run(ScanRun& r, hipStream_t st) {
+hipError_t scan_run(const ScanRun& r, hipStream_t st) {
     if (r.plan.segments > 1) {
-        scan_launch<T, SP, SW, kEnds>(r, st);
-        (void)launch_join_segments(r.in, r.plan, r.state, r.ends, r.steps, false, st);
+        if (const hipError_t e = scan_launch<T, SP, SW, kEnds>(r, st); e != hipSuccess) return e;
+        if (const hipError_t e = launch_join_segments(r.in, r.plan, r.state, r.ends, r.steps, false, st); e != hipSuccess) return e;
     }
-    if (!r.out) scan_launch<T, SP, SW, kSave>(r, st);
-    else if (r.saved) scan_launch<T, SP, SW, kOut | kSave>(r, st);
-    else scan_launch<T, SP, SW, kOut>(r, st);
+    if (!r.out) return scan_launch<T, SP, SW, kSave>(r, st);
+    return r.saved ? scan_launch<T, SP, SW, kOut | kSave>(r, st) : scan_launch<T, SP, SW, kOut>(r, st);
 }
 
 template <typename T>
-void scan_of(ScanRun& r, hipStream_t st) {
-    if (r.in.S <= 4) scan_run<T, 4, 1>(r, st);
-    else if (r.in.S <= 8) scan_run<T, 8, 1>(r, st);
-    else if (r.in.S <= 16) scan_run<T, 16, 1>(r, st);
-    else if (r.in.S <= 32) scan_run<T, 16, 2>(r, st);
-    else scan_run<T, 16, 4>(r, st);
+hipError_t scan_of(const ScanRun& r, hipStream_t st) {
+    if (r.in.S <= 4) return scan_run<T, 4, 1>(r, st);
+    if (r.in.S <= 8) return scan_run<T, 8, 1>(r, st);
+    if (r.in.S <= 16) return scan_run<T, 16, 1>(r, st);
+    return r.in.S <= 32 ? scan_run<T, 16, 2>(r, st) : scan_run<T, 16, 4>(r, st);
 }
 
 size_t ends_bytes(const ScanPlan& p, int B, int D, int S) {
@@ -424,9 +423,7 @@ hipError_t run_state_scan(int dtype, const ScanIn& in, const float* state, void*
         r.ends = static_cast<float*>(ws);
         r.steps = reinterpret_cast<float*>(static_cast<char*>(ws) + ends_bytes(r.plan, in.B, in.D_, in.S));
     }
-    if (dtype) scan_of<uint16_t>(r, st);
-    else scan_of<float>(r, st);
-    return hipGetLastError();
+    return dtype ? scan_of<uint16_t>(r, st) : scan_of<float>(r, st);
 }
 
 hipError_t launch_state_scan(int dtype, const ScanIn& in, const float* state, void* out, float* final_state, void* saved, void* ws, hipStream_t st) {

@@ -478,41 +478,51 @@ Carve carve(int B, int N, int D, int S, int G, bool with_saved) {
 }
 
 template <typename T, int SP>
-void back_ends(const GradRun& r, hipStream_t st) {
+hipError_t back_ends(const GradRun& r, hipStream_t st) {
     const int64_t waves = static_cast<int64_t>(r.in.G) * r.plan.scan.tiles * r.in.B * r.plan.scan.segments;
     const int w = waves_together(r.in.G * r.plan.scan.tiles);
     back_ends_kernel<T, SP><<<dim3(static_cast<unsigned>(waves / w), (r.in.S + SP - 1) / SP), 64 * w, sizeof(float) * w * kP * 2 * SP, st>>>(r);
+    return hipGetLastError();
 }
 
+// The kernel's LDS is asked for ahead of the call's first launch (nothing has gone out where that fails); `launch`: the kernel itself.
 template <typename T, int SP, int SW>
-hipError_t grad_main(const GradRun& r, hipStream_t st) {
+hipError_t grad_main(const GradRun& r, bool launch, hipStream_t st) {
     const int bytes = static_cast<int>(sizeof(float)) * grad_lds<SP, SW>(r.plan.tile_waves);
     const int64_t blocks = static_cast<int64_t>(r.in.B) * r.plan.scan.segments * r.in.G * r.plan.parts;
     const auto kernel = r.in.z.data ? scan_grad_kernel<T, SP, SW, true> : scan_grad_kernel<T, SP, SW, false>;
-    if (bytes > 65536) {
+    if (!launch) {
         static std::atomic<uint64_t> asked[2];
-        if (const hipError_t e = ask_lds(reinterpret_cast<const void*>(kernel), static_cast<int>(sizeof(float)) * grad_lds<SP, SW>(SW >= 4 ? 1 : 4 / SW), asked[r.in.z.data != nullptr]); e != hipSuccess)
-            return e;
+        if (bytes <= 65536) return hipSuccess;
+        return ask_lds(reinterpret_cast<const void*>(kernel), static_cast<int>(sizeof(float)) * grad_lds<SP, SW>(SW >= 4 ? 1 : 4 / SW), asked[r.in.z.data != nullptr]);
     }
     kernel<<<static_cast<unsigned>(blocks), 64 * SW * r.plan.tile_waves, bytes, st>>>(r);
-    return hipSuccess;
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t grad_main_of(const GradRun& r, bool launch, hipStream_t st) {
+    const int S = r.in.S;
+    return S <= 4 ? grad_main<T, 4, 1>(r, launch, st) : S <= 8 ? grad_main<T, 8, 1>(r, launch, st) : S <= 16 ? grad_main<T, 8, 2>(r, launch, st)
+           : S <= 32 ? grad_main<T, 8, 4>(r, launch, st) : grad_main<T, 8, 8>(r, launch, st);
 }
 
+// forward: the workspace of the pass that saves the states; null where they are there.
 template <typename T>
-hipError_t grad_of(const GradRun& r, hipStream_t st) {
+hipError_t grad_of(const GradRun& r, const float* state, void* forward, hipStream_t st) {
     const int S = r.in.S;
-    if (r.plan.scan.segments > 1) {
-        if (S <= 4) back_ends<T, 4>(r, st);
-        else if (S <= 8) back_ends<T, 8>(r, st);
-        else back_ends<T, 16>(r, st);
-        (void)launch_join_segments(r.in, r.plan.scan, nullptr, r.ends, r.steps, true, st);
+    if (const hipError_t e = grad_main_of<T>(r, false, st); e != hipSuccess) return e;
+    if (forward) {
+        if (const hipError_t e = run_state_scan(std::is_same<T, float>::value ? 0 : 1, r.in, state, nullptr, nullptr, const_cast<float*>(r.saved), forward, st); e != hipSuccess) return e;
     }
-    const hipError_t e = S <= 4 ? grad_main<T, 4, 1>(r, st) : S <= 8 ? grad_main<T, 8, 1>(r, st) : S <= 16 ? grad_main<T, 8, 2>(r, st)
-                         : S <= 32 ? grad_main<T, 8, 4>(r, st) : grad_main<T, 8, 8>(r, st);
-    if (e != hipSuccess) return e;
+    if (r.plan.scan.segments > 1) {
+        if (const hipError_t e = S <= 4 ? back_ends<T, 4>(r, st) : S <= 8 ? back_ends<T, 8>(r, st) : back_ends<T, 16>(r, st); e != hipSuccess) return e;
+        if (const hipError_t e = launch_join_segments(r.in, r.plan.scan, nullptr, r.ends, r.steps, true, st); e != hipSuccess) return e;
+    }
+    if (const hipError_t e = grad_main_of<T>(r, true, st); e != hipSuccess) return e;
     if (r.plan.parts > 1) {
         const int64_t all = static_cast<int64_t>(r.in.B) * r.in.N * r.in.G * S;
         group_sums_kernel<T><<<static_cast<unsigned>((all + 255) / 256), 256, 0, st>>>(r);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     const int a_blocks = static_cast<int>((static_cast<int64_t>(r.in.D_) * S + 63) / 64);
     column_sums_kernel<<<a_blocks + (2 * r.in.D_ + 63) / 64, 1024, 0, st>>>(r, a_blocks);
@@ -529,14 +539,10 @@ hipError_t launch_state_scan_grad(int dtype, AnyRows dout, const ScanIn& in, con
     char* base = static_cast<char*>(ws);
     const auto floats = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
     if (!scan_fits(in.B, in.N, in.D_, in.S, in.G, grad_plan(in.B, in.N, in.D_, in.S, in.G).scan)) return hipErrorInvalidValue;
-    if (!saved) {
-        const hipError_t e = run_state_scan(dtype, in, state, nullptr, nullptr, floats(c.saved), base + c.scan, st);
-        if (e != hipSuccess) return e;
-        saved = floats(c.saved);
-    }
-    const GradRun r{in, dout, g, static_cast<const float*>(saved), floats(c.ends), floats(c.steps), floats(c.bc), floats(c.a), floats(c.d),
+    const GradRun r{in, dout, g, saved ? static_cast<const float*>(saved) : floats(c.saved), floats(c.ends), floats(c.steps), floats(c.bc), floats(c.a), floats(c.d),
                     grad_plan(in.B, in.N, in.D_, in.S, in.G)};
-    return dtype ? grad_of<uint16_t>(r, st) : grad_of<float>(r, st);
+    void* const forward = saved ? nullptr : base + c.scan;
+    return dtype ? grad_of<uint16_t>(r, state, forward, st) : grad_of<float>(r, state, forward, st);
 }
 
 }  // namespace enc
