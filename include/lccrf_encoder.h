@@ -16,7 +16,8 @@
  *    read; outputs and gradients there are 0.
  *  - outputs may not overlap inputs, except where stated.
  *  - LCCRF_EINVAL where a size is below 1 or above its limit (LCCRF_MAX_TAPS, LCCRF_MAX_STATES;
- *    B * N and D below 2^31, the scan's D at most 2^22 and a multiple of G, G * S below 2^27), LCCRF_EALIGN where a pointer is not aligned to its
+ *    B * N at most 2^31 - 1024, so that positions and what a kernel goes beyond them fit 32 bits; D below 2^31, the
+ *    scan's D at most 2^22 and a multiple of G, G * S below 2^27), LCCRF_EALIGN where a pointer is not aligned to its
  *    element (workspaces and `saved`: 256 bytes).
  */
 #ifndef LCCRF_ENCODER_H

@@ -140,6 +140,9 @@ struct ScanGrads {
     float *dA, *dD, *ddt_bias, *dstate;
 };
 
+// Of a call of the convolution or scan.  Kernels count positions in 32 bits, and go past a sequence's end by less than a run or a block.
+constexpr int64_t kMaxPositions = (int64_t{1} << 31) - 1024;
+
 constexpr int kScanBlock = 8;  // positions between two saved states
 
 // dtype 0: float, 1: bfloat16.  All return the status of their launches.

@@ -11,7 +11,7 @@ inline bool type_ok(int dt) { return dt == LCCRF_F32 || dt == LCCRF_BF16; }
 inline size_t size_of(int dt) { return dt == LCCRF_F32 ? 4 : 2; }
 inline bool lies(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline AnyRows rows(const lccrf_rows& r) { return {r.data, r.batch, r.row}; }
-inline bool positions_ok(int B, int N, int D) { return B >= 1 && N >= 1 && D >= 1 && static_cast<int64_t>(B) * N < (int64_t{1} << 31); }
+inline bool positions_ok(int B, int N, int D) { return B >= 1 && N >= 1 && D >= 1 && static_cast<int64_t>(B) * N <= kMaxPositions; }
 inline bool conv_ok(int B, int N, int D, int K) { return positions_ok(B, N, D) && K >= LCCRF_MIN_TAPS && K <= LCCRF_MAX_TAPS; }
 inline bool scan_ok(int B, int N, int D, int S, int G) {
     return positions_ok(B, N, D) && D <= 1 << 22 && S >= 1 && S <= LCCRF_MAX_STATES && G >= 1 && G <= D && D % G == 0 && static_cast<int64_t>(G) * S < (1 << 27);

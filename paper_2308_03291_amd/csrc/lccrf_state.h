@@ -160,6 +160,9 @@ __device__ __forceinline__ int64_t quad_at(int64_t block, int S, int D, int q, i
 // The same as a place for the whole wave and a byte offset (a channel's 16 bytes; D <= 2^22).
 __device__ __forceinline__ unsigned quad_bytes(int D, int q, int d) { return (static_cast<unsigned>(q) * D + d) * 16; }
 
+// Where the segment that starts at `begin` ends (the last one's full length may reach past 32 bits).
+__device__ __forceinline__ int segment_stop(const ScanPlan& p, int begin, int N) { return N - begin < p.seg_len ? N : begin + p.seg_len; }
+
 inline int scan_blocks(int N) { return (N + kP - 1) / kP; }
 
 // Segments: the recursion over a segment needs the state in front of it, which takes a pass of its own over all segments (eight
@@ -178,7 +181,7 @@ inline ScanPlan scan_plan(int B, int N, int D, int G, bool flat, int waves_a_til
     const int64_t most = (N + 63) / 64;
     if (segments > most) segments = most;
     p.seg_len = static_cast<int>(((N + segments - 1) / segments + kP - 1) / kP * kP);
-    p.segments = (N + p.seg_len - 1) / p.seg_len;
+    p.segments = static_cast<int>((static_cast<int64_t>(N) + p.seg_len - 1) / p.seg_len);
     return p;
 }
 // Groups of 64 channels and more whose tiles would not be full (up to 16 states): tiles run on into the next group, and a wave holds the

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
     const int next_group = group + 1 < in.G ? group + 1 : group;
     const f32x4* bc4 = reinterpret_cast<const f32x4*>(bc + (FLAT && d / width != group ? kSet + 4 : 0));
     const int len = clamp_length(in.lengths, b, in.N), begin = seg * r.plan.seg_len;
-    const int stop = begin + r.plan.seg_len < in.N ? begin + r.plan.seg_len : in.N, end = stop < len ? stop : len;
+    const int stop = segment_stop(r.plan, begin, in.N), end = stop < len ? stop : len;
     const unsigned bytes = static_cast<unsigned>(d) * sizeof(T);
     T* out = MODE & kOut ? static_cast<T*>(r.out) + static_cast<int64_t>(b) * in.N * in.D_ : nullptr;
     const float skip = in.D ? in.D[d] : 0.0f, bias = in.dt_bias ? in.dt_bias[d] : 0.0f;

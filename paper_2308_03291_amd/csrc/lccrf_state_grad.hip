@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
     const bool is = c0 < width;
     const int d = group * width + (is ? c0 : width - 1);
     const int len = clamp_length(in.lengths, b, in.N), begin = seg * plan.seg_len;
-    const int stop = begin + plan.seg_len < in.N ? begin + plan.seg_len : in.N, end = stop < len ? stop : len;
+    const int stop = segment_stop(plan, begin, in.N), end = stop < len ? stop : len;
     const bool gated = in.z.data != nullptr;
     const unsigned bytes = static_cast<unsigned>(d) * sizeof(T);
     const float bias = in.dt_bias ? in.dt_bias[d] : 0.0f;
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 4 ? 4 : SW == 1 ? 2 : 3)
     const bool is = c0 < width, full_tile = tile * 64 + 64 <= width;
     const int d = group * width + (is ? c0 : width - 1);
     const int len = clamp_length(in.lengths, b, in.N), begin = seg * plan.seg_len;
-    const int stop = begin + plan.seg_len < in.N ? begin + plan.seg_len : in.N, end = stop < len ? stop : len;
+    const int stop = segment_stop(plan, begin, in.N), end = stop < len ? stop : len;
     const int64_t from = static_cast<int64_t>(b) * plan.segments + seg;
 
     float* bc = lds + wave * (kP * 2 * SP);

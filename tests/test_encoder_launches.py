@@ -101,3 +101,40 @@ def test_shared_memory_is_asked_for_before_anything_goes_out(ask):
     for call in (("scan_grad", 2, 5000, 250, 8, 1), ("scan_grad", 2, 5000, 250, 8, 1, 4096)):
         (rc, made), = ask([call], attribute=1)
         assert rc == ELAUNCH and made == [], f"{call}: status {rc}, {len(made)} launches"
+
+
+# ---- sizes at their limits ------------------------------------------------------------------------------------
+
+MOST = 2 ** 31 - 1024  # positions of a call
+
+
+def up256(n):
+    return -(-n // 256) * 256
+
+
+def test_sizes_of_the_longest_sequences(ask):
+    """Rounded up past 2^31 on the way: sizes of workspaces and numbers of workgroups at the limit, refusals past it."""
+    def sizes(*calls):
+        return [rc for rc, _ in ask([("size", *c) for c in calls])]
+    for B, N in ((1, MOST), (1, MOST - 63), (MOST, 1), (3, MOST // 3)):
+        blocks = -(-N // 8)
+        assert sizes(("lccrf_state_scan_saved_bytes", B, N, 1, 1), ("lccrf_state_scan_saved_bytes", B, N, 3, 13)) == [up256(B * blocks * 16), up256(B * blocks * 4 * 3 * 16)]
+        assert sizes(("lccrf_conv_grad_workspace_bytes", B, N, 1, 4)) == [2048 * 5 * 4]  # as many partial sums as workgroups
+        need, grad, more = sizes(("lccrf_state_scan_workspace_bytes", B, N, 1, 1, 1), ("lccrf_state_scan_grad_workspace_bytes", B, N, 1, 1, 1, 1),
+                                 ("lccrf_state_scan_grad_workspace_bytes", B, N, 1, 1, 1, 0))
+        if B == 1:  # one wave by itself: 2048 segments, 3072 in the gradient, but for what rounding their length up takes off
+            assert 2000 * 20 <= need <= 2048 * 20 and 3000 * 32 <= grad <= 3072 * 32 + 1024
+        assert 0 < need and 0 < grad and more == grad + up256(B * blocks * 16) + need
+    assert sizes(*[(name, 1, MOST + 1, *rest) for name, *rest in (("lccrf_state_scan_saved_bytes", 1, 1), ("lccrf_state_scan_workspace_bytes", 1, 1, 1),
+                                                                  ("lccrf_state_scan_grad_workspace_bytes", 1, 1, 1, 1), ("lccrf_conv_grad_workspace_bytes", 1, 4))]) == [0] * 4
+
+
+def test_launches_of_the_longest_sequences(ask):
+    for (rc, made), runs in zip(ask([("conv", 1, MOST, 1, 4), ("conv", 1, MOST, 1, 5, 1), ("conv", 2, MOST // 2, 1, 3)]), (-(-MOST // 64), -(-MOST // 60), 2 * -(-(MOST // 2) // 60))):
+        assert rc == OK and made == [[-(-runs // 256), 1, 1, 256, 1, 1]]
+    for rc, made in ask([("conv_grad", 1, MOST, 1, 4), ("scan", 1, MOST, 1, 1, 1), ("scan_grad", 1, MOST, 1, 1, 1)]):
+        assert rc == OK and all(v[0] <= 1 << 20 for v in made), made
+    for call in (("conv", 1, MOST + 1, 1, 4), ("conv", MOST + 1, 1, 1, 4), ("conv_grad", 1, MOST + 1, 1, 4), ("scan", 1, MOST + 1, 1, 1, 1),
+                 ("scan_grad", 1, MOST + 1, 1, 1, 1), ("scan_grad", 1 << 16, 1 << 15, 1, 1, 1)):
+        (rc, made), = ask([call])
+        assert rc == EINVAL and made == [], call
