@@ -203,21 +203,25 @@ __global__ __launch_bounds__(256) void conv_grad_kernel(ConvArgs a, T* __restric
     }
 }
 
-// Workgroups of 64 channels of one tap, sixteen threads a channel over the partial sums.
+// Workgroups of 64 channels of one tap (`blocks` such in all), sixteen threads a channel over the partial sums.
 template <int K>
-__global__ __launch_bounds__(1024) void conv_sums_kernel(const float* __restrict__ partial, int parts, int D, float* __restrict__ dweight,
+__global__ __launch_bounds__(1024) void conv_sums_kernel(const float* __restrict__ partial, int parts, int D, int blocks, float* __restrict__ dweight,
                                                          float* __restrict__ dbias) {
     __shared__ float sums[16][64];
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6, ch = blockIdx.x * 64 + x, k = blockIdx.y;
-    float sum = 0.0f;
-    if (ch < D)
-        for (int p = y; p < parts; p += 16) sum += partial[(static_cast<int64_t>(p) * (K + 1) + k) * D + ch];
-    sums[y][x] = sum;
-    __syncthreads();
-    if (y == 0 && ch < D) {
-        for (int i = 1; i < 16; ++i) sum += sums[i][x];
-        if (k < K) dweight[static_cast<int64_t>(ch) * K + k] = sum;
-        else if (dbias) dbias[ch] = sum;
+    const int x = threadIdx.x & 63, y = threadIdx.x >> 6, k = blockIdx.y;
+    for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const int64_t ch = static_cast<int64_t>(block) * 64 + x;
+        float sum = 0.0f;
+        if (ch < D)
+            for (int p = y; p < parts; p += 16) sum += partial[(static_cast<int64_t>(p) * (K + 1) + k) * D + ch];
+        sums[y][x] = sum;
+        __syncthreads();
+        if (y == 0 && ch < D) {
+            for (int i = 1; i < 16; ++i) sum += sums[i][x];
+            if (k < K) dweight[ch * K + k] = sum;
+            else if (dbias) dbias[ch] = sum;
+        }
+        __syncthreads();
     }
 }
 
@@ -264,7 +268,7 @@ constexpr int64_t kForwardThreads = 128 << 10, kGradThreads = 64 << 10;
 struct GradPlan { int run, runs, lx, high; };
 GradPlan grad_plan(int B, int N, int D, int K) {
     GradPlan p;
-    const int cpr = (D + 3) / 4;
+    const int cpr = pieces_of_row(D, 4);
     p.lx = 1;
     while (p.lx < 64 && p.lx < cpr) p.lx *= 2;
     p.run = run_length(K, static_cast<int64_t>(B) * cpr, N, kGradThreads);
@@ -280,7 +284,7 @@ GradPlan grad_plan(int B, int N, int D, int K) {
 
 template <typename T, int K>
 hipError_t conv_of(ConvArgs a, void* out, void* final_state, hipStream_t st) {
-    a.cpr = (a.D + Wide<T>::V - 1) / Wide<T>::V;
+    a.cpr = pieces_of_row(a.D, Wide<T>::V);
     a.run = run_length(K, static_cast<int64_t>(a.B) * a.cpr, a.N, kForwardThreads);
     a.runs = (a.N + a.run - 1) / a.run;
     const int64_t threads = static_cast<int64_t>(a.B) * a.runs * a.cpr;
@@ -294,7 +298,7 @@ hipError_t conv_of(ConvArgs a, void* out, void* final_state, hipStream_t st) {
 template <typename T, int K>
 hipError_t conv_grad_of(ConvArgs a, void* dx, float* dweight, float* dbias, void* dstate, void* ws, hipStream_t st) {
     const GradPlan p = grad_plan(a.B, a.N, a.D, K);
-    a.cpr = (a.D + 3) / 4;
+    a.cpr = pieces_of_row(a.D, 4);
     a.run = p.run;
     a.runs = p.runs;
     float* partial = static_cast<float*>(ws);
@@ -303,7 +307,8 @@ hipError_t conv_grad_of(ConvArgs a, void* dx, float* dweight, float* dbias, void
     const auto kernel = a.D < 4 ? conv_grad_kernel<T, K, true, false> : stream ? conv_grad_kernel<T, K, false, true> : conv_grad_kernel<T, K, false, false>;
     kernel<<<grid, 256, sizeof(float) * 256 * (K + 1) * 4, st>>>(a, static_cast<T*>(dx), static_cast<T*>(dstate), partial, p.lx);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    conv_sums_kernel<K><<<dim3((a.D + 63) / 64, K + 1), 1024, 0, st>>>(partial, p.high, a.D, dweight, dbias);
+    const int blocks = pieces_of_row(a.D, 64);
+    conv_sums_kernel<K><<<dim3(blocks < kColumnBlocks ? blocks : kColumnBlocks, K + 1), 1024, 0, st>>>(partial, p.high, a.D, blocks, dweight, dbias);
     return hipGetLastError();
 }
 

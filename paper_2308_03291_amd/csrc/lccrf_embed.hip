@@ -371,7 +371,7 @@ inline bool rows_are_few(int64_t n, int V, int64_t row_bytes) { return V >= 8 * 
 
 template <typename T, bool SMALL>
 hipError_t embed_of(const void* table, int V, int D, int64_t table_row, const int32_t* ids, int64_t n, float scale, void* out, hipStream_t st) {
-    const int cpr = (D + Wide<T>::V - 1) / Wide<T>::V;
+    const int cpr = pieces_of_row(D, Wide<T>::V);
     // positions a workgroup: its threads' kItems pieces, one position at least
     const int per_block = cpr >= 256 * kItems ? 1 : 256 * kItems / cpr;
     if (!fits((n + per_block - 1) / per_block, 256)) return hipErrorInvalidValue;
@@ -389,7 +389,7 @@ hipError_t embed_grad_of(AnyRows dout, const int32_t* ids, int B, int N, int V, 
     int32_t* start = reinterpret_cast<int32_t*>(base);
     int32_t* order = reinterpret_cast<int32_t*>(base + up256((static_cast<size_t>(V) + 1) * 4));
     float* partial = reinterpret_cast<float*>(base + up256((static_cast<size_t>(V) + 1) * 4) + up256(static_cast<size_t>(n) * 4));
-    const int cpr = (D + Wide<T>::V - 1) / Wide<T>::V;
+    const int cpr = pieces_of_row(D, Wide<T>::V);
     const GradArgs a{ids, order, start, n, N < 1 ? 1 : N, V, D, cpr, piece_of(n), scale, partial};
     const int64_t pieces = pieces_of(n);  // without a row that can be long there is nothing to cut
     const int64_t piece_blocks = (2 * pieces * cpr + 255) / 256;

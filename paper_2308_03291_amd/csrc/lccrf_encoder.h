@@ -83,8 +83,10 @@ template <typename T, int W> struct Piece<T, W, true> {
 };
 template <int W, bool SMALL> __device__ __forceinline__ int piece_start(int piece, int D) {
     if (SMALL) return 0;
-    return piece * W + W <= D ? piece * W : D - W;
+    return piece * W <= D - W ? piece * W : D - W;
 }
+// Pieces of a row (D up to 2^31 - 1: nothing here or above goes past it).
+__host__ __device__ inline int pieces_of_row(int D, int W) { return (D - 1) / W + 1; }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -170,7 +172,9 @@ hipError_t launch_state_step(int dtype, const ScanIn& in, float* state, void* ou
 // several places): lookup of 67 MB 13.7 / 23.1; embedding gradient of 205 MB 76 / 96; convolutions of 67 MB 35 / 41, 134 MB 62.5 / 64.4, 268 MB
 // 106 / 110, 537 MB 232 / 235, of 66 MB with an odd width 41 / 47; convolution and gradient of 134 MB each 147 / 157.
 inline bool past_caches(int64_t bytes) { return bytes > (int64_t{32} << 20); }
-// A launch has fewer than 2^32 threads; the entry points refuse what would take more.
+// A launch has fewer than 2^32 threads; the entry points refuse what would take more, before anything is enqueued.  The sums over
+// columns behind a gradient would pass that where nothing else does: at most kColumnBlocks workgroups take their blocks of columns in turn.
+constexpr int kColumnBlocks = 1 << 16;
 inline bool fits(int64_t blocks, int threads) { return blocks * threads < (int64_t{1} << 32); }
 // More than 64 KB of LDS has to be asked for, once a kernel and device (`asked`: a bit a device).
 inline hipError_t ask_lds(const void* kernel, int bytes, std::atomic<uint64_t>& asked) {

@@ -434,27 +434,30 @@ __global__ __launch_bounds__(256) void group_sums_kernel(GradRun r) {
 }
 
 // dA, dD and ddt_bias: columns summed over their rows, sixteen threads a column (the same batch: 5 us).
-__global__ __launch_bounds__(1024) void column_sums_kernel(GradRun r, int a_blocks) {
+__global__ __launch_bounds__(1024) void column_sums_kernel(GradRun r, int a_blocks, int blocks) {
     __shared__ float sums[16][64];
     const ScanIn& in = r.in;
     const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-    const bool isA = static_cast<int>(blockIdx.x) < a_blocks;
-    const int64_t columns = isA ? static_cast<int64_t>(in.D_) * in.S : 2 * static_cast<int64_t>(in.D_);
-    const int64_t col = static_cast<int64_t>(isA ? blockIdx.x : blockIdx.x - a_blocks) * 64 + x;
-    const int rows = in.B * r.plan.scan.segments * (isA ? 1 : r.plan.state_waves);
-    const float* from = isA ? r.part_a : r.part_d;
-    float sum = 0.0f;
-    if (col < columns) {
+    for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const bool isA = block < a_blocks;
+        const int64_t columns = isA ? static_cast<int64_t>(in.D_) * in.S : 2 * static_cast<int64_t>(in.D_);
+        const int64_t col = static_cast<int64_t>(isA ? block : block - a_blocks) * 64 + x;
+        const int rows = in.B * r.plan.scan.segments * (isA ? 1 : r.plan.state_waves);
+        const float* from = isA ? r.part_a : r.part_d;
+        float sum = 0.0f;
+        if (col < columns) {
 #pragma unroll 4
-        for (int k = y; k < rows; k += 16) sum += from[k * columns + col];
-    }
-    sums[y][x] = sum;
-    __syncthreads();
-    if (y == 0 && col < columns) {
-        for (int i = 1; i < 16; ++i) sum += sums[i][x];
-        if (isA) r.g.dA[col] = sum;
-        else if (col < in.D_) { if (r.g.dD) r.g.dD[col] = sum; }
-        else if (r.g.ddt_bias) r.g.ddt_bias[col - in.D_] = sum;
+            for (int k = y; k < rows; k += 16) sum += from[k * columns + col];
+        }
+        sums[y][x] = sum;
+        __syncthreads();
+        if (y == 0 && col < columns) {
+            for (int i = 1; i < 16; ++i) sum += sums[i][x];
+            if (isA) r.g.dA[col] = sum;
+            else if (col < in.D_) { if (r.g.dD) r.g.dD[col] = sum; }
+            else if (r.g.ddt_bias) r.g.ddt_bias[col - in.D_] = sum;
+        }
+        __syncthreads();
     }
 }
 
@@ -525,7 +528,8 @@ hipError_t grad_of(const GradRun& r, const float* state, void* forward, hipStrea
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     const int a_blocks = static_cast<int>((static_cast<int64_t>(r.in.D_) * S + 63) / 64);
-    column_sums_kernel<<<a_blocks + (2 * r.in.D_ + 63) / 64, 1024, 0, st>>>(r, a_blocks);
+    const int blocks = a_blocks + (2 * r.in.D_ + 63) / 64;
+    column_sums_kernel<<<blocks < kColumnBlocks ? blocks : kColumnBlocks, 1024, 0, st>>>(r, a_blocks, blocks);
     return hipGetLastError();
 }
 

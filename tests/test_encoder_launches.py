@@ -138,3 +138,23 @@ def test_launches_of_the_longest_sequences(ask):
                  ("scan_grad", 1, MOST + 1, 1, 1, 1), ("scan_grad", 1 << 16, 1 << 15, 1, 1, 1)):
         (rc, made), = ask([call])
         assert rc == EINVAL and made == [], call
+
+
+WIDEST = 2 ** 31 - 1
+
+
+def test_launches_of_the_widest_rows(ask):
+    """Up to the documented widths every launch has a grid that the runtime takes; the stand-in refuses the others."""
+    for call in (("conv_grad", 1, 1, 1 << 28, 2), ("conv_grad", 1, 1, 1 << 28, 8), ("conv_grad", 1, 1, WIDEST, 8, 1), ("conv", 1, 1, WIDEST, 4), ("conv", 1, 1, WIDEST, 4, 1),
+                 ("conv_step", 1, WIDEST, 4), ("scan", 1, 1, 1 << 22, 64, 1), ("scan_grad", 1, 1, 1 << 22, 64, 1), ("scan_grad", 1, 1, 1 << 22, 62, 1 << 20, 4096),
+                 ("state_step", 1, 1 << 22, 64, 1), ("embed", 2, 5, WIDEST), ("embed", 2, 5, WIDEST, 1)):
+        (rc, made), = ask([call])
+        assert rc == OK and made, (call, rc, made)
+        assert all(v[0] * v[3] < 2 ** 32 for v in made), (call, made)
+
+
+def test_what_no_grid_can_hold_is_refused_first(ask):
+    for call in (("conv", 8, 64, WIDEST, 4), ("conv_step", 64, WIDEST - 3, 4), ("scan", 1 << 23, 64, 64, 4, 1), ("scan_grad", 1 << 23, 64, 64, 4, 1), ("scan_grad", 8192, 8192, 64, 64, 1),
+                 ("state_step", 1 << 16, 1 << 16, 64, 1), ("embed_grad", 1 << 14, 1 << 14, 100, 1 << 13), ("embed_grad", 2, 5, 1 << 30, 1 << 6), ("embed", 1 << 25, 100, 1 << 20)):
+        (rc, made), = ask([call])
+        assert rc == EINVAL and made == [], (call, rc, made)

@@ -62,3 +62,59 @@ def test_the_longest_scan(crf):
     alike(g.dCm[:, inner], -0.5 * h, 80)
     alike(g.dD, -0.5 * 1.5 * MOST, 2 ** 20 + 400)  # a wave adds a segment's positions, 3072 of them are joined
     alike(g.dA, back * step * MOST, 2 ** 20 + 400)
+
+
+def near(got, want, bound, roundings, what):
+    """check() of test_gpu_encoder.py on the GPU, in pieces; want and bound: functions of a slice of the last dimension's entries."""
+    half = torch.finfo(got.dtype).eps / 2
+    for at in range(0, got.shape[-1], 1 << 25):
+        part = slice(at, at + (1 << 25))
+        w, b = want(part), bound(part)
+        off = (got[..., part].double() - w).abs()
+        assert bool((off <= half * w.abs() + roundings * U * b + 1e-30).all()), f"{what} from {at} on: off by {float(off.max())}"
+
+
+def test_gradients_of_the_widest_rows(crf):
+    """So wide that the sums over columns, a workgroup of 1024 threads for 64 of them, would take 2^32 threads."""
+    g = generator(1)
+    D = 2 ** 28 + 5
+    x, dout, w = normal(g, 1, 2, D), normal(g, 1, 2, D), normal(g, D, 2)
+    got = crf.lccrf_conv_grad(dout, x, w, torch.zeros(D, device=DEV))
+
+    def slopes(p):
+        x0, x1, w0, w1 = x[0, 0, p].double(), x[0, 1, p].double(), w[p, 0].double(), w[p, 1].double()
+        pre = torch.stack([w1 * x0, w0 * x0 + w1 * x1])
+        gate = torch.sigmoid(pre)
+        return x0, x1, w0, w1, dout[0, :, p].double() * gate * (1 + pre * (1 - gate)), 1.1 * dout[0, :, p].double().abs()
+
+    def of(k):  # (the gradient by what it says, the sum of absolute values)
+        def values(p, absolute=False):
+            x0, x1, w0, w1, d, most = slopes(p)
+            if absolute:
+                x0, x1, w0, w1, d = x0.abs(), x1.abs(), w0.abs(), w1.abs(), most
+            return {"dx0": w1 * d[0] + w0 * d[1], "dx1": w1 * d[1], "dw0": d[1] * x0, "dw1": d[0] * x0 + d[1] * x1, "db": d[0] + d[1]}[k]
+        return values, lambda p: values(p, True)
+
+    # (K + 14) roundings times 1 + the largest input of a gate, about 6 * 6 * 2; and the sums
+    for name, t in (("dx0", got.dx[0, 0]), ("dx1", got.dx[0, 1]), ("dw0", got.dweight[:, 0]), ("dw1", got.dweight[:, 1]), ("db", got.dbias)):
+        near(t, *of(name), 16 * 73 + 4, name)
+
+
+def test_gradient_of_the_widest_scan(crf):
+    g = generator(2)
+    D, S = 2 ** 22, 64
+    x, dt, dout = (normal(g, 1, 1, D) for _ in range(3))
+    A, Bm, Cm, state = -torch.rand(D, S, generator=g, device=DEV) - 0.1, normal(g, 1, 1, 1, S), normal(g, 1, 1, 1, S), normal(g, 1, D, S)
+    got = crf.lccrf_state_scan_grad(dout, x, dt, A, Bm, Cm, state=state)
+    v, d, x64 = dt[0, 0].double(), dout[0, 0].double(), x[0, 0].double()
+    step = torch.logaddexp(v, torch.zeros_like(v))
+    near(got.dx[0, 0], lambda p: d[p] * float((Bm.double() * Cm.double()).sum()) * step[p], lambda p: d[p].abs() * float((Bm.double() * Cm.double()).abs().sum()) * step[p], 200, "dx")
+    dBm = Cm[0, 0, 0].double() * (d * step * x64).sum()
+    assert bool(((got.dBm[0, 0, 0].double() - dBm).abs() <= (2 ** 16 + 200) * U * Cm[0, 0, 0].double().abs() * (d * step * x64).abs().sum()).all())
+    for s in (0, 1, 31, 62, 63):
+        a, h0, c, b = torch.exp(step * A[:, s].double()), state[0, :, s].double(), float(Cm[0, 0, 0, s]), float(Bm[0, 0, 0, s])
+        near(got.dA[:, s], lambda p: (d * c * a * h0 * step)[p], lambda p: (d * c * a * h0 * step)[p].abs(), 200, f"dA {s}")
+        near(got.dstate[0, :, s], lambda p: (d * c * a)[p], lambda p: (d * c * a)[p].abs(), 200, f"dstate {s}")
+        h = a * h0 + step * x64 * b
+        big = (d * a * h0).abs().sum() + (d * step * x64 * b).abs().sum()
+        assert float((got.dCm[0, 0, 0, s].double() - (d * h).sum()).abs()) <= (2 ** 16 + 200) * U * float(big)
