@@ -20,6 +20,7 @@ import torch
 from . import binding as _b
 
 MIN_TAPS, MAX_TAPS, MAX_STATES = 2, 8, 64
+_MOST = 2 ** 31 - 1  # the C ABI takes sizes as int: ctypes would cut larger ones (an expanded view can have them) to 32 bits without a word
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
@@ -144,6 +145,8 @@ def lccrf_embed(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, o
     if table.dim() != 2 or 0 in table.shape:
         raise ValueError(f"table must be [V, D], got {list(table.shape)}")
     V, D = table.shape
+    if V > _MOST or D > _MOST:
+        raise ValueError(f"a table of at most {_MOST} rows and columns is served, got {list(table.shape)}")
     row = _activation(table, "table", table.shape, dtype, dev)[0]
     shape = ids.shape
     pids = _dense(ids, "ids", shape, torch.int32, dev)
@@ -160,8 +163,8 @@ def lccrf_embed_grad(dout: torch.Tensor, ids: torch.Tensor, V: int, *, scale: fl
     if dout.dim() == 2:
         dout, ids = dout[None], ids[None]
     shape = dout.shape
-    if len(shape) != 3 or shape[2] == 0 or V < 1:
-        raise ValueError(f"dout must be [B, N, D] and V positive, got {list(shape)} and {V}")
+    if len(shape) != 3 or shape[2] == 0 or not 1 <= V <= _MOST or max(shape) > _MOST:
+        raise ValueError(f"dout must be [B, N, D] and V positive, all of them at most {_MOST}, got {list(shape)} and {V}")
     B, N, D = shape
     strides = _activation(dout, "dout", shape, dtype, dev)
     pids = _dense(ids, "ids", (B, N), torch.int32, dev)
@@ -177,8 +180,8 @@ def _conv_args(x: torch.Tensor, weight: torch.Tensor, bias, state):
     """Checks what all calls of the convolution share; (dtype's code, device number, D, K, strides of x, the others' addresses)."""
     dt, dtype, dev = _first(x, "x")
     shape = x.shape
-    if weight.dim() != 2 or 0 in shape:
-        raise ValueError(f"x must be [B, N, D] (one position: [B, D]) and weight [D, K], got {list(shape)} and {list(weight.shape)}")
+    if weight.dim() != 2 or 0 in shape or max(shape) > _MOST:
+        raise ValueError(f"x must be [B, N, D] (one position: [B, D]), its sizes at most {_MOST}, and weight [D, K], got {list(shape)} and {list(weight.shape)}")
     D, K = shape[-1], weight.shape[1]
     if not MIN_TAPS <= K <= MAX_TAPS:
         raise ValueError(f"{MIN_TAPS} to {MAX_TAPS} taps are served, got {K}")
@@ -247,8 +250,8 @@ def _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias):
     """Checks what all calls of the scan share; (dtype's code, device number, channels, S, G, shape of x, dtype, the inputs' block)."""
     code, dtype, dev = _first(x, "x")
     shape = x.shape
-    if 0 in shape or A.dim() != 2 or Bm.dim() != len(shape) + 1:
-        raise ValueError(f"x must be [B, N, D], A [D, S] and Bm [B, N, G, S] (one position: [B, D] and [B, G, S]), got {list(shape)}, {list(A.shape)} "
+    if 0 in shape or max(shape) > _MOST or A.dim() != 2 or Bm.dim() != len(shape) + 1:
+        raise ValueError(f"x must be [B, N, D], its sizes at most {_MOST}, A [D, S] and Bm [B, N, G, S] (one position: [B, D] and [B, G, S]), got {list(shape)}, {list(A.shape)} "
                          f"and {list(Bm.shape)}")
     width, S, G = shape[-1], A.shape[1], Bm.shape[-2]
     if not 1 <= S <= MAX_STATES:
@@ -276,8 +279,8 @@ def _scan_args(x, dt, A, Bm, Cm, D, z, dt_bias):
 def state_scan_saved(x: torch.Tensor, A: torch.Tensor) -> torch.Tensor:
     """Device memory for ``saved=`` of ``lccrf_state_scan`` on x [B, N, D] and A [D, S]: what the gradient would otherwise compute
     again.  To be kept until ``lccrf_state_scan_grad`` has it; its layout is the library's."""
-    if x.dim() != 3 or A.dim() != 2 or A.shape[0] != x.shape[2]:
-        raise ValueError(f"x must be [B, N, D] and A [D, S], got {list(x.shape)} and {list(A.shape)}")
+    if x.dim() != 3 or A.dim() != 2 or A.shape[0] != x.shape[2] or max(x.shape) > _MOST or A.shape[1] > MAX_STATES:
+        raise ValueError(f"x must be [B, N, D], its sizes at most {_MOST}, and A [D, S] of at most {MAX_STATES} states, got {list(x.shape)} and {list(A.shape)}")
     return _scratch(_bytes("lccrf_state_scan_saved_bytes", *x.shape, A.shape[1]), "state_scan_saved", x.device, None)
 
 

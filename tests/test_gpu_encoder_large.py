@@ -118,3 +118,29 @@ def test_gradient_of_the_widest_scan(crf):
         h = a * h0 + step * x64 * b
         big = (d * a * h0).abs().sum() + (d * step * x64 * b).abs().sum()
         assert float((got.dCm[0, 0, 0, s].double() - (d * h).sum()).abs()) <= (2 ** 16 + 200) * U * float(big)
+
+
+def test_sizes_past_32_bits_are_refused(crf):
+    """Views can be that large without memory; a size cut to 32 bits would pass for a small one."""
+    def t(*s, dtype=torch.float32):
+        return torch.zeros(s, dtype=dtype, device=DEV)
+    many = 2 ** 32 + 5
+    ids = t(2, 3, dtype=torch.int32)
+    x, v, A = t(1, 1, 1).expand(many, 1, 1), t(1, 1, 1, 1).expand(many, 1, 1, 1), -torch.ones(1, 1, device=DEV)
+    wide, vectors = t(1, 1, 1).expand(1, many, 1), t(1, 1, 1, 1).expand(1, many, 1, 1)
+    bad = [
+        lambda: crf.lccrf_embed(t(1, 1).expand(many, 1), ids),
+        lambda: crf.lccrf_embed_grad(t(2, 3, 1), ids, many),
+        lambda: crf.lccrf_conv(x, t(1, 2)),
+        lambda: crf.lccrf_conv(wide, t(1, 2)),
+        lambda: crf.lccrf_conv_grad(x, x, t(1, 2)),
+        lambda: crf.lccrf_conv_grad(wide, wide, t(1, 2)),
+        lambda: crf.state_scan_saved(x, A),
+        lambda: crf.lccrf_state_scan(x, x, A, v, v),
+        lambda: crf.lccrf_state_scan(wide, wide, A, vectors, vectors),
+        lambda: crf.lccrf_state_scan_grad(x, x, x, A, v, v),
+    ]
+    for k, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {k} was taken")
