@@ -91,6 +91,8 @@ __host__ __device__ inline int pieces_of_row(int D, int W) { return (D - 1) / W 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exp2_fast(-x * kLog2e)); }
+// The gate by itself, to be multiplied in afterwards: |silu| <= |x|, where a value times x could pass the largest float on its way to a number.
+__device__ __forceinline__ float silu(float x) { return x * sigmoid(x); }
 
 // log(1 + exp(v)) and its derivative.  With e = exp(-|v|): max(v, 0) + log1p(e), and log1p(e) = e (1 + e q(e)) with q of degree 8
 // fitted to it on [0, 1] (off by at most 1.4 units in the last place): a logarithm of 1 + e would lose the steps near 0.001 that

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
                     sums[(sw * kP + i) * 64] = y0 + y1;
                 } else if constexpr ((MODE & kOut) != 0) {
                     const float y = fmaf(skip, x[i], y0 + y1);
-                    o[i] = GATED ? y * z[i] * sigmoid(z[i]) : y;
+                    o[i] = GATED ? y * silu(z[i]) : y;
                     asm volatile("" : "+v"(o[i]));  // computed here: moved behind a store's condition, it would keep the states of all eight positions
                 }
             }
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
 #pragma unroll
                         for (int w = 0; w < SW; ++w) y += sums[(w * kP + sw + k * SW) * 64];
                         y = fmaf(skip, x[k], y);
-                        o[k] = GATED ? y * z[k] * sigmoid(z[k]) : y;
+                        o[k] = GATED ? y * silu(z[k]) : y;
                     }
                 }
             }
@@ -329,10 +329,7 @@ __global__ __launch_bounds__(256) void step_kernel(ScanIn in, float* __restrict_
 #pragma unroll
         for (int k = 1; k < LQ; k *= 2) y += __shfl_xor(y, k);
         y = fmaf(skip, x, y);
-        if (in.z.data) {
-            const float z = widen(zr[m]);
-            y = y * z * sigmoid(z);
-        }
+        if (in.z.data) y *= silu(widen(zr[m]));
         if (b0 + m < in.B) {
             float* mine = state + (static_cast<int64_t>(b0 + m) * in.D_ + d) * in.S + s0;
             if (WHOLE) {

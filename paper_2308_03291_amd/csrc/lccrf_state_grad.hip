@@ -82,7 +82,7 @@ template <int N> __device__ __forceinline__ float lane_sums(float (&v)[N], int l
 }
 
 // dy of a position: the gradient by y.
-__device__ __forceinline__ float through_gate(float dout, float z, bool gated) { return gated ? dout * z * sigmoid(z) : dout; }
+__device__ __forceinline__ float through_gate(float dout, float z, bool gated) { return gated ? dout * silu(z) : dout; }
 
 // What a segment makes of 0 behind it, and the sum of its steps.
 template <typename T, int SP>
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 4 ? 4 : SW == 1 ? 2 : 3)
                 const float x = widen(xr[k]), dout = widen(dr[k]), z = GATED ? widen(zr[k]) : 0.0f, gate = sigmoid(z);
                 float* to = scal + i * 64;
                 to[kStep * kP * 64] = on ? sp.value : 0.0f;
-                to[kDy * kP * 64] = on ? (GATED ? dout * z * gate : dout) : 0.0f;
+                to[kDy * kP * 64] = on ? (GATED ? dout * (z * gate) : dout) : 0.0f;
                 to[kX * kP * 64] = on ? x : 0.0f;
                 to[kSlope * kP * 64] = sp.slope;
                 if (GATED) to[kDz * kP * 64] = dout * gate * fmaf(z, 1.0f - gate, 1.0f);

@@ -1,0 +1,78 @@
+"""The encoder's scan where inputs are infinite or far apart: what its formulas in 64 bits (tests/encoder_reference.py) make infinite is
+infinite, what they make NaN is NaN, and all else is a number within the roundings of test_gpu_encoder.py."""
+import pytest
+import torch
+
+import encoder_reference as ref
+from test_gpu_encoder import DEV, TYPES, _dirty_memory, check, crf, generator, normal, scan_roundings  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+PER_CHANNEL = ("A", "D", "dt_bias")
+
+
+def positive(g, t, B, N, D, S, G, *, gate=True):
+    """Inputs above 0 but for A, so that sums of infinities have one sign; a state as well."""
+    def above(*shape, dtype=t):
+        return (torch.rand(shape, generator=g, device=DEV) + 0.25).to(dtype)
+    inputs = {"x": above(B, N, D), "dt": normal(g, B, N, D, dtype=t) - 2, "A": -above(D, S, dtype=torch.float32) * 4, "Bm": above(B, N, G, S), "Cm": above(B, N, G, S),
+              "D": above(D, dtype=torch.float32), "z": above(B, N, D) if gate else None, "dt_bias": normal(g, D, scale=0.1)}
+    return inputs, above(B, D, S, dtype=torch.float32)
+
+
+def same(got, want, bound, roundings, what):
+    got64 = got.double().cpu()
+    assert torch.equal(torch.isnan(got64), torch.isnan(want)), f"{what}: NaN at {torch.isnan(got64).nonzero()[:3].tolist()}, not at {torch.isnan(want).nonzero()[:3].tolist()}"
+    infinite = torch.isinf(want)
+    assert torch.equal(torch.isinf(got64), infinite) and torch.equal(got64[infinite], want[infinite]), f"{what}: infinities"
+    finite = torch.isfinite(want)
+    assert torch.isfinite(bound[finite]).all()
+    if finite.any():
+        check(got.cpu()[finite], want[finite], bound[finite], roundings, what)
+
+
+def rounds(inputs):
+    B, N, D = inputs["x"].shape
+    return scan_roundings(N, inputs["A"].shape[1], D, inputs["z"])
+
+
+def forwards(crf, inputs, state, steps=True):
+    """The scan and, position by position, its single-token form."""
+    N = inputs["x"].shape[1]
+    want, big = (ref.scan(*inputs.values(), None, state, absolute=a) for a in (False, True))
+    R = rounds(inputs)
+    out, final = crf.lccrf_state_scan(*inputs.values(), state=state)
+    same(out, want["out"], big["out"], R, "out")
+    same(final, want["final"], big["final"], R, "final")
+    if steps:
+        moving = state.clone()
+        made = [crf.lccrf_state_step(*[v if k in PER_CHANNEL or v is None else v[:, l] for k, v in inputs.items()], moving) for l in range(N)]
+        same(torch.stack(made, 1), want["out"], big["out"], R, "out by positions")
+        same(moving, want["final"], big["final"], R, "final by positions")
+
+
+def backwards(crf, inputs, state, dout):
+    B, N, D = inputs["x"].shape
+    want, big = (ref.scan(*inputs.values(), None, state, dout, absolute=a) for a in (False, True))
+    R = rounds(inputs)
+    for saved in (crf.state_scan_saved(inputs["x"], inputs["A"]), None):
+        if saved is not None:
+            crf.lccrf_state_scan(*inputs.values(), state=state, saved=saved)
+        got = crf.lccrf_state_scan_grad(dout, *inputs.values(), state=state, saved=saved)
+        for name in got._fields:
+            if getattr(got, name) is not None:
+                same(getattr(got, name), want[name], big[name], R + (B * N if name in ("dA", "dD", "ddt_bias") else 0), name)
+
+
+def test_gates_that_all_but_close(crf):
+    """y silu(z) where y z is past the largest float and the result is not; the same of its gradient."""
+    g = generator(3)
+    inputs, state = positive(g, torch.float32, 2, 11, 70, 16, 1)
+    inputs["z"] = torch.linspace(-80, -20, 70, device=DEV).repeat(2, 11, 1)
+    inputs["x"][:, 3] = 5e36
+    forwards(crf, inputs, state)
+    inputs["x"][:, 3] = 1.0
+    dout = torch.rand(2, 11, 70, generator=g, device=DEV) + 0.25
+    dout[:, 3] = 1e37
+    backwards(crf, inputs, state, dout)
