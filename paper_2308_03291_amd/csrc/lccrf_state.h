@@ -108,20 +108,27 @@ __device__ __forceinline__ float base2(float A) {
     return a < -3.0e38f ? -3.0e38f : a;
 }
 
+// Kernels hold 4 quads(S) states a channel.  Places past S hold states of the front once more (one state: four times), each of the
+// copies, as many as a power of two, with its share of Cm: what they add up to is exact, by way of the gradients too, and infinite or NaN where the
+// states by themselves are.  Places of zeros would make NaN of an infinite x, step or gradient.
+__host__ __device__ inline int quads(int S) { return S <= 4 ? 1 : S <= 8 ? 2 : S <= 16 ? 4 : S <= 32 ? 8 : 16; }
+__device__ __forceinline__ int state_at(int place, int S) { return place < S ? place : S == 1 ? 0 : place - S; }
+__device__ __forceinline__ float copies_of(int s, int S) { return S == 1 ? 4.0f : s + S < 4 * quads(S) ? 2.0f : 1.0f; }
+
 // Bm and Cm of kP positions for the states s0 .. s0 + SP - 1, on their way from memory to LDS [kP][2 * SP] (Bm, then Cm).
-// Positions past the end and states past S count as 0.  A lane has state lane % SP of the positions lane / SP + i * kStep.
+// Positions past the end count as 0.  A lane has state lane % SP of the positions lane / SP + i * kStep.
 template <typename T, int SP> struct GroupVectors {
     static constexpr int R = kP * SP / 64 ? kP * SP / 64 : 1, kStep = 64 / SP;
     T vb[R], vc[R];
     const T *pb, *pc;  // of this lane's first position
     int first;
-    bool state;
+    float share;  // of its state's copies, for Cm
     __device__ __forceinline__ void place(const ScanIn& in, int b, int l0, int group, int s0, int lane) {
-        const int s = s0 + lane % SP;
+        const int s = state_at(s0 + lane % SP, in.S);
         first = lane / SP % kP;
-        state = s < in.S;
-        pb = at<T>(in.Bm, b, l0 + first) + group * in.b_group + (state ? s : 0);
-        pc = at<T>(in.Cm, b, l0 + first) + group * in.c_group + (state ? s : 0);
+        share = 1.0f / copies_of(s, in.S);
+        pb = at<T>(in.Bm, b, l0 + first) + group * in.b_group + s;
+        pc = at<T>(in.Cm, b, l0 + first) + group * in.c_group + s;
     }
     // A block that the end may lie in: past it the last position stands in.
     __device__ __forceinline__ void load(const ScanIn& in, int l0, int len) {
@@ -146,15 +153,14 @@ template <typename T, int SP> struct GroupVectors {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int pos = first + i * kStep;
-            const bool is = state && (WHOLE || l0 + pos < len);
+            const bool is = WHOLE || l0 + pos < len;
             lds[pos * 2 * SP + lane % SP] = is ? widen(vb[i]) : 0.0f;
-            lds[pos * 2 * SP + SP + lane % SP] = is ? widen(vc[i]) : 0.0f;
+            lds[pos * 2 * SP + SP + lane % SP] = is ? widen(vc[i]) * share : 0.0f;
         }
     }
 };
 
 // Saved states: [B][ceil(N / kP)][quads][D][4] floats, the states rounded up to what a kernel holds.
-__host__ __device__ inline int quads(int S) { return S <= 4 ? 1 : S <= 8 ? 2 : S <= 16 ? 4 : S <= 32 ? 8 : 16; }
 __device__ __forceinline__ int64_t quad_at(int64_t block, int S, int D, int q, int d) { return ((block * quads(S) + q) * D + d) * 4; }
 
 // The same as a place for the whole wave and a byte offset (a channel's 16 bytes; D <= 2^22).

@@ -62,19 +62,20 @@ __global__ __launch_bounds__(256, SP <= 8 ? 3 : 2) void scan_kernel(ScanRun r) {
     float h[SP], A[SP], total = 0.0f;
 #pragma unroll
     for (int s = 0; s < SP; ++s) {
-        A[s] = s0 + s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s0 + s]) : 0.0f;
+        A[s] = base2(in.A[static_cast<int64_t>(d) * in.S + state_at(s0 + s, in.S)]);
         h[s] = 0.0f;
     }
     if (!(MODE & kEnds)) {
         if (r.plan.segments > 1) {
             const int64_t from = static_cast<int64_t>(b) * r.plan.segments + seg;
 #pragma unroll
-            for (int s = 0; s < SP; ++s)
-                if (s0 + s < in.S) h[s] = r.ends[quad_at(from, in.S, in.D_, (s0 + s) / 4, d) + s % 4];
+            for (int s = 0; s < SP; ++s) {
+                const int k = state_at(s0 + s, in.S);
+                h[s] = r.ends[quad_at(from, in.S, in.D_, k / 4, d) + k % 4];
+            }
         } else if (r.state) {
 #pragma unroll
-            for (int s = 0; s < SP; ++s)
-                if (s0 + s < in.S) h[s] = r.state[(static_cast<int64_t>(b) * in.D_ + d) * in.S + s0 + s];
+            for (int s = 0; s < SP; ++s) h[s] = r.state[(static_cast<int64_t>(b) * in.D_ + d) * in.S + state_at(s0 + s, in.S)];
         }
     }
 

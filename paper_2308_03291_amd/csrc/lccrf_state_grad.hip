@@ -3,6 +3,8 @@
 // With dh[l] = dy[l] Cm[l] + a[l+1] dh[l+1] running backwards,
 //     dCm = sum_channels dy h,   dBm = sum_channels dh put,   dput = sum_s dh Bm,   back = dh a h[l-1]  (by the decay's logarithm),
 //     dx = dput step + D dy,     dv = (dput x + sum_s back A) sigmoid(v),    dA = sum_positions back step.
+// (A state that is held several times has a share of Cm, so of dh and of what follows from it; dA, dBm and dstate, which look at one
+// copy, take it times the copies.)
 // The states in front of every eighth position are saved by the forward pass; eight positions are run again from there, their
 // states kept in registers, and then gone through backwards.  27 vector instructions an update with 16 states (counted: 5 forwards, 10
 // backwards, the rest for sums over the channels and what is computed once a channel), two of them exponentials: vector arithmetic
@@ -107,7 +109,7 @@ __global__ __launch_bounds__(256, 2) void back_ends_kernel(GradRun r) {
     float dh[SP], A[SP], total = 0.0f;
 #pragma unroll
     for (int s = 0; s < SP; ++s) {
-        A[s] = s0 + s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s0 + s]) : 0.0f;
+        A[s] = base2(in.A[static_cast<int64_t>(d) * in.S + state_at(s0 + s, in.S)]);
         dh[s] = 0.0f;
     }
     if (begin < end) {
@@ -208,14 +210,16 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 4 ? 4 : SW == 1 ? 2 : 3)
     float dh[SP], A[SP], dA[SP], sum_dD = 0.0f, sum_dv = 0.0f;
 #pragma unroll
     for (int s = 0; s < SP; ++s) {
-        A[s] = s0 + s < in.S ? base2(in.A[static_cast<int64_t>(d) * in.S + s0 + s]) : 0.0f;
+        A[s] = base2(in.A[static_cast<int64_t>(d) * in.S + state_at(s0 + s, in.S)]);
         dh[s] = 0.0f;
         dA[s] = 0.0f;
     }
     if (plan.segments > 1) {
 #pragma unroll
-        for (int s = 0; s < SP; ++s)
-            if (s0 + s < in.S) dh[s] = r.ends[quad_at(from, in.S, in.D_, (s0 + s) / 4, d) + s % 4];
+        for (int s = 0; s < SP; ++s) {
+            const int k = state_at(s0 + s, in.S);
+            dh[s] = r.ends[quad_at(from, in.S, in.D_, k / 4, d) + k % 4];
+        }
     }
 
     if (begin < end) {
@@ -371,6 +375,7 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 4 ? 4 : SW == 1 ? 2 : 3)
                     const float* from = red + (s / SP * kP + i) * (2 * SP) + c * SP + s % SP;
                     float sum = from[0];
                     for (int t = 1; t < CT; ++t) sum += from[t * (SW * kP * 2 * SP)];
+                    if (!c) sum *= copies_of(s, in.S);
                     const int to = (i * in.G + group) * in.S + s;
                     if (r.plan.parts == 1) put1((c ? static_cast<T*>(r.g.dCm) : static_cast<T*>(r.g.dBm)) + group_row + to, sum);
                     else (r.part_bc + (static_cast<int64_t>(part) * 2 + c) * in.B * in.N * in.G * in.S + group_row)[to] = sum;
@@ -403,14 +408,14 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 4 ? 4 : SW == 1 ? 2 : 3)
     if (is) {
 #pragma unroll
         for (int s = 0; s < SP; ++s)
-            if (s0 + s < in.S) r.part_a[(from * in.D_ + d) * in.S + s0 + s] = dA[s];
+            if (s0 + s < in.S) r.part_a[(from * in.D_ + d) * in.S + s0 + s] = dA[s] * copies_of(s0 + s, in.S);
         float* pd = r.part_d + (from * SW + sw) * 2 * in.D_ + d;
         pd[0] = sum_dD;
         pd[in.D_] = sum_dv;
         if (r.g.dstate && seg == 0) {
 #pragma unroll
             for (int s = 0; s < SP; ++s)
-                if (s0 + s < in.S) r.g.dstate[(static_cast<int64_t>(b) * in.D_ + d) * in.S + s0 + s] = dh[s];
+                if (s0 + s < in.S) r.g.dstate[(static_cast<int64_t>(b) * in.D_ + d) * in.S + s0 + s] = dh[s] * copies_of(s0 + s, in.S);
         }
     }
 }

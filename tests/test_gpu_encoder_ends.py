@@ -23,9 +23,9 @@ def positive(g, t, B, N, D, S, G, *, gate=True):
 
 def same(got, want, bound, roundings, what):
     got64 = got.double().cpu()
-    assert torch.equal(torch.isnan(got64), torch.isnan(want)), f"{what}: NaN at {torch.isnan(got64).nonzero()[:3].tolist()}, not at {torch.isnan(want).nonzero()[:3].tolist()}"
+    assert bool((torch.isnan(got64) == torch.isnan(want)).all()), f"{what}: NaN at {torch.isnan(got64).nonzero()[:3].tolist()}, not at {torch.isnan(want).nonzero()[:3].tolist()}"
     infinite = torch.isinf(want)
-    assert torch.equal(torch.isinf(got64), infinite) and torch.equal(got64[infinite], want[infinite]), f"{what}: infinities"
+    assert bool((torch.isinf(got64) == infinite).all()) and bool((got64[infinite] == want[infinite]).all()), f"{what}: infinities"
     finite = torch.isfinite(want)
     assert torch.isfinite(bound[finite]).all()
     if finite.any():
@@ -63,6 +63,46 @@ def backwards(crf, inputs, state, dout):
         for name in got._fields:
             if getattr(got, name) is not None:
                 same(getattr(got, name), want[name], big[name], R + (B * N if name in ("dA", "dD", "ddt_bias") else 0), name)
+
+
+STATES = (1, 2, 3, 4, 5, 7, 8, 9, 13, 16, 17, 24, 33, 50, 64)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("S", STATES)
+@pytest.mark.parametrize("where", ("x", "dt", "state"))
+def test_an_infinite_input(crf, t, S, where):
+    """From where it is on, its channel is infinite, and no other: in a call for the prompt and in calls for single tokens."""
+    g = generator(S)
+    inputs, state = positive(g, t, 2, 19, 70, S, 2, gate=where != "dt")
+    if where == "state":
+        state[1, 40] = INF
+    else:
+        inputs[where][1, 6, 40] = INF
+    forwards(crf, inputs, state)
+
+
+@pytest.mark.parametrize("S", STATES)
+@pytest.mark.parametrize("where", ("Bm", "Cm"))
+def test_an_infinite_vector(crf, S, where):
+    g = generator(S)
+    inputs, state = positive(g, torch.float32, 2, 19, 70, S, 2)
+    inputs[where][0, 6, 1, S - 1] = INF
+    forwards(crf, inputs, state)
+
+
+def an_infinite_gradient(crf, t, S, D, G):
+    g = generator(S * D)
+    inputs, state = positive(g, t, 2, 19, D, S, G, gate=D != 5)
+    dout = (torch.rand(2, 19, D, generator=g, device=DEV) + 0.25).to(t)
+    dout[1, 11, D - 1] = INF
+    backwards(crf, inputs, state, dout)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("S", STATES)
+def test_an_infinite_gradient(crf, t, S):
+    an_infinite_gradient(crf, t, S, 64, 1)
 
 
 def test_gates_that_all_but_close(crf):
