@@ -314,7 +314,8 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 4 ? 4 : SW == 1 ? 2 : 3)
                 const auto one = [&](int s, float Bs, float Cs, float& dput, float& sum) {
                     const float e = fmaf(dy, Cs, dh[s]);
                     dh[s] = e * exp2_fast(step * A[s]);
-                    const float back = dh[s] * h[i][s];
+                    // (past the end dh is 0, but the last state, which no decay works on, may be infinite)
+                    const float back = WHOLE || l0 + i < end ? dh[s] * h[i][s] : 0.0f;
                     dput = fmaf(e, Bs, dput);
                     sum = fmaf(back, A[s], sum);
                     dA[s] = fmaf(back, step, dA[s]);

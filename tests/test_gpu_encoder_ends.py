@@ -99,10 +99,32 @@ def an_infinite_gradient(crf, t, S, D, G):
     backwards(crf, inputs, state, dout)
 
 
+def gradients_of_an_infinite_input(crf, S, D, G, where):
+    g = generator(S * D)
+    inputs, state = positive(g, torch.float32, 2, 19, D, S, G)
+    inputs[where][(1, 11, D // 2) if where == "x" else (1, 11, G - 1, S - 1)] = INF
+    backwards(crf, inputs, state, torch.rand(2, 19, D, generator=g, device=DEV) + 0.25)
+
+
 @pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("S", STATES)
 def test_an_infinite_gradient(crf, t, S):
     an_infinite_gradient(crf, t, S, 64, 1)
+
+
+@pytest.mark.parametrize("S", STATES)
+@pytest.mark.parametrize("where", ("x", "Bm", "Cm"))
+def test_gradients_of_an_infinite_input(crf, S, where):
+    gradients_of_an_infinite_input(crf, S, 64, 1, where)
+
+
+@pytest.mark.parametrize("N", (1, 5, 8, 13, 16))
+def test_an_infinite_input_at_the_last_position(crf, N):
+    """No decay works on the state that it makes: the gradient by A is a number, wherever the last eight positions end."""
+    g = generator(N)
+    inputs, state = positive(g, torch.float32, 2, N, 70, 16, 1)
+    inputs["x"][1, N - 1, 9] = INF
+    backwards(crf, inputs, state, torch.rand(2, N, 70, generator=g, device=DEV) + 0.25)
 
 
 def test_gates_that_all_but_close(crf):
