@@ -6,8 +6,8 @@
 //
 // Blocks of eight positions are worked on while the next one's inputs are on their way.  Loads and stores come back in order, and
 // a wait can only leave in flight what is known to have been issued behind what it waits for.  So the next block's inputs are taken up in
-// front of this block's stores, and a whole block has no condition around a store (lanes past a group's end repeat its last
-// channel and write the same value there again); only the block that ends a sequence is taken with conditions.
+// front of this block's stores, and a whole block has no condition around a store (lanes past a group's end repeat a channel
+// of it and write the same value there again); only the block that ends a sequence is taken with conditions.
 #pragma once
 
 #include "lccrf_encoder.h"

@@ -83,6 +83,19 @@ template <int N> __device__ __forceinline__ float lane_sums(float (&v)[N], int l
     return v[0] + from_lane<kXor1>(v[0]);
 }
 
+// A tile of fewer than 64 channels: lanes past them hold channels once more, m = 2^k times or 2m times in all, and count in the sums over
+// the channels for 1/m or 1/(2m): what the copies add up to is exact, and infinite or NaN where the channel by itself is (a count of 0 would make
+// NaN of an infinite one).
+struct LaneShare { int channel; float share; };
+__device__ __forceinline__ LaneShare lane_share(int channels, int lane) {
+    if (channels >= 64) return {lane, 1.0f};
+    int m = 1;
+    while (2 * m * channels <= 64) m *= 2;
+    const int more = 64 / m - channels;  // channels with 2m lanes: the first ones
+    const int channel = lane < channels * m ? lane % channels : (lane - channels * m) % (more > 0 ? more : 1);
+    return {channel, channel < more ? 0.5f / m : 1.0f / m};
+}
+
 // dy of a position: the gradient by y.
 __device__ __forceinline__ float through_gate(float dout, float z, bool gated) { return gated ? dout * silu(z) : dout; }
 
@@ -188,9 +201,10 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 4 ? 4 : SW == 1 ? 2 : 3)
     int b = bs / plan.segments;
     const int seg = bs - b * plan.segments;
     if (plan.segments == 1) b = ranked(in.lengths, in.B, in.N, b, lane);
-    const int tile = part * CT + ct, width = in.D_ / in.G, c0 = tile * 64 + lane;
-    const bool is = c0 < width, full_tile = tile * 64 + 64 <= width;
-    const int d = group * width + (is ? c0 : width - 1);
+    const int tile = part * CT + ct, width = in.D_ / in.G;
+    const LaneShare held = lane_share(width - tile * 64, lane);
+    const bool is = lane < width - tile * 64, full_tile = tile * 64 + 64 <= width;
+    const int d = group * width + tile * 64 + held.channel;
     const int len = clamp_length(in.lengths, b, in.N), begin = seg * plan.seg_len;
     const int stop = segment_stop(plan, begin, in.N), end = stop < len ? stop : len;
     const int64_t from = static_cast<int64_t>(b) * plan.segments + seg;
@@ -307,9 +321,9 @@ __global__ __launch_bounds__(SW == 8 ? 512 : 256, SP == 4 ? 4 : SW == 1 ? 2 : 3)
                 const f32x4* B4 = reinterpret_cast<const f32x4*>(bc + i * 2 * SP);
                 const float step = scal[(kStep * kP + i) * 64], put = step * scal[(kX * kP + i) * 64], dy = scal[(kDy * kP + i) * 64];
                 float v[SP / 2], dput0 = 0.0f, dput1 = 0.0f, back0 = 0.0f, back1 = 0.0f, own_put = put, own_dy = dy;
-                if (!full_tile) {  // a channel that a lane only repeats is not to be counted twice
-                    own_put = is ? put : 0.0f;
-                    own_dy = is ? dy : 0.0f;
+                if (!full_tile) {
+                    own_put = put * held.share;
+                    own_dy = dy * held.share;
                 }
                 const auto one = [&](int s, float Bs, float Cs, float& dput, float& sum) {
                     const float e = fmaf(dy, Cs, dh[s]);

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import encoder_reference as ref
-from test_gpu_encoder import DEV, TYPES, _dirty_memory, check, crf, generator, normal, scan_roundings  # noqa: F401
+from test_gpu_encoder import DEV, TYPES, _dirty_memory, check, check_scan, crf, generator, normal, scan_inputs, scan_roundings  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -116,6 +116,32 @@ def test_an_infinite_gradient(crf, t, S):
 @pytest.mark.parametrize("where", ("x", "Bm", "Cm"))
 def test_gradients_of_an_infinite_input(crf, S, where):
     gradients_of_an_infinite_input(crf, S, 64, 1, where)
+
+
+# Channels that fill one lane, a part of a tile, a tile and a part of another, tiles of several waves: lanes past them hold some again.
+PARTS = [(1, 1), (5, 1), (3, 3), (70, 2), (130, 1), (250, 1)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("S", STATES)
+@pytest.mark.parametrize("D,G", PARTS)
+def test_an_infinite_gradient_in_part_of_a_tile(crf, t, S, D, G):
+    an_infinite_gradient(crf, t, S, D, G)
+
+
+@pytest.mark.parametrize("S", STATES)
+@pytest.mark.parametrize("D,G", PARTS)
+@pytest.mark.parametrize("where", ("x", "Bm", "Cm"))
+def test_gradients_of_an_infinite_input_in_part_of_a_tile(crf, S, D, G, where):
+    gradients_of_an_infinite_input(crf, S, D, G, where)
+
+
+@pytest.mark.parametrize("width", range(1, 65))
+def test_every_part_of_a_tile(crf, width):
+    """The sums over the channels take every channel once, however many lanes hold it."""
+    g = generator(width)
+    inputs = scan_inputs(g, torch.float32, 2, 17, width, 8, 1)
+    check_scan(crf, inputs, None, normal(g, 2, width, 8), normal(g, 2, 17, width))
 
 
 @pytest.mark.parametrize("N", (1, 5, 8, 13, 16))
