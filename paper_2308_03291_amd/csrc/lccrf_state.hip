@@ -264,13 +264,28 @@ __global__ __launch_bounds__(kJoin) void join_segments_kernel(ScanIn in, ScanPla
             made[u] = *reinterpret_cast<const f32x4*>(e + u * e_stride);
             step[u] = t[u * t_stride];
         }
+        const auto along = [&](auto careful) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            *reinterpret_cast<f32x4*>(e) = f32x4{h[0], h[1], h[2], h[3]};
+            for (int u = 0; u < U; ++u) {
+                *reinterpret_cast<f32x4*>(e + u * e_stride) = f32x4{h[0], h[1], h[2], h[3]};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) h[j] = fmaf(exp2_fast(step[u] * A[j]), h[j], 4 * q + j < in.S ? made[u][j] : 0.0f);
-            e += e_stride;
+                for (int j = 0; j < 4; ++j) {
+                    const float power = step[u] * A[j], made_j = 4 * q + j < in.S ? made[u][j] : 0.0f;
+                    const bool stays = decltype(careful)::value && __builtin_isinf(h[j]) && __builtin_isfinite(power);
+                    h[j] = stays ? h[j] + made_j : fmaf(exp2_fast(power), h[j], made_j);
+                }
+            }
+        };
+        // The decays of a segment together may be below every float where each by itself is not, and make NaN of an infinite state that
+        // stays one.  Where there is a NaN at the end, the same segments once more with a look at that.
+        const float h0[4] = {h[0], h[1], h[2], h[3]};
+        along(std::false_type{});
+        if (__builtin_isnan(h[0] + h[1] + h[2] + h[3])) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) h[j] = h0[j];
+            along(std::true_type{});
         }
+        e += U * e_stride;
         t += U * t_stride;
     };
     int k = 0;

@@ -153,6 +153,20 @@ def test_an_infinite_input_at_the_last_position(crf, N):
     backwards(crf, inputs, state, torch.rand(2, N, 70, generator=g, device=DEV) + 0.25)
 
 
+@pytest.mark.parametrize("S", (4, 13, 24))
+def test_infinities_in_a_sequence_that_is_cut(crf, S):
+    """Every decay is above 0, so an infinite state stays what it is, though the decays of a segment together are below every float."""
+    g = generator(S)
+    inputs, state = positive(g, torch.float32, 1, 700, 6, S, 2)
+    inputs["dt_bias"] += 4.0
+    state[0, 1] = INF
+    forwards(crf, inputs, state, steps=False)
+    state[0, 1] = 1.0
+    dout = torch.rand(1, 700, 6, generator=g, device=DEV) + 0.25
+    dout[0, 690, 4] = INF
+    backwards(crf, inputs, state, dout)
+
+
 def test_gates_that_all_but_close(crf):
     """y silu(z) where y z is past the largest float and the result is not; the same of its gradient."""
     g = generator(3)
