@@ -254,7 +254,9 @@ __global__ __launch_bounds__(256) void conv_step_kernel(const T* __restrict__ x,
 }
 
 // Positions of a run: 64, or half and half again of that while there would be fewer than `least` threads; always a multiple of the
-// positions in flight, two of them at least.  Measured: forward B=64 N=512 D=2048 bfloat16 67 us with runs of 64 (131072 threads), 72 of 32,
+// positions in flight, two of them at least but for five taps, whose 60 goes by 30 and 15 to 5: one.  (Held at 10 there, us 10 / 5: small forward calls
+// 5.9 / 5.0, B=4 N=100 D=256, small gradients 12.1 + 3.9 / 10.4 + 3.9; B=32 N=128 D=512 9.2 / 7.8 and 13.8 + 3.8 / 14.0 + 5.0, B=2 N=4000 D=200
+// 6.9 / 6.5 and 13.5 + 4.9 / 13.6 + 8.3.)  Measured: forward B=64 N=512 D=2048 bfloat16 67 us with runs of 64 (131072 threads), 72 of 32,
 // 77 of 16 (what a run reads in front of it, and its taps, come to more); forward and gradient of B=128 N=128 D=1001 float, ragged, 69 us
 // with 64K threads at least in the gradient (runs of 32), 79 with 128K (of 16), 73 with 32K (of 64).
 int run_length(int K, int64_t threads_a_position, int N, int64_t least) {

@@ -27,12 +27,6 @@ struct ScanPlan {
     int seg_len;    // positions each, a multiple of kP
 };
 
-// Where a wave's work lies.
-struct Where {
-    int b, seg, group, channel;  // channel of this lane (clamped into the group)
-    bool is;                     // lane has a channel of its own
-};
-
 __device__ __forceinline__ int clamp_length(const int32_t* lengths, int b, int N) {
     if (!lengths) return N;
     const int n = lengths[b];
