@@ -2,7 +2,9 @@
 import pytest
 import torch
 
-from test_gpu_encoder import DEV, U, _dirty_memory, crf, generator, normal  # noqa: F401
+import encoder_reference as ref
+from test_gpu_encoder import (DEV, TYPES, U, _dirty_memory, check, check_scan, conv_lengths, crf, generator, normal, scan_inputs,  # noqa: F401
+                              scan_roundings)
 
 pytestmark = pytest.mark.gpu
 
@@ -144,3 +146,116 @@ def test_sizes_past_32_bits_are_refused(crf):
         with pytest.raises(ValueError):
             call()
             pytest.fail(f"call {k} was taken")
+
+
+# ---- kernels that only large calls take -----------------------------------------------------------------------
+
+def ids_of(kind, n, V, g):
+    if kind == "spread":
+        ids = torch.randint(-5, V + 5, (n,), generator=g, device=DEV)
+    elif kind == "heavy":  # as in text
+        ids = (float(V) ** torch.rand(n, generator=g, device=DEV, dtype=torch.float64) - 1).long().clamp(0, V - 1)
+    else:  # one token holds most positions, two others the rest: waves that keep no list of theirs, pieces without end
+        ids = torch.full((n,), V // 2, device=DEV)
+        ids[::97], ids[5::101] = V - 1, 0
+    return ids.to(torch.int32)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("kind", ("spread", "heavy", "most"))
+@pytest.mark.parametrize("V,D,n", [(5000, 40, 40000), (300, 33, 40001), (70000, 5, 33000), (100000, 192, 3000), (50000, 100, 20000), (33000, 301, 16384), (4000000, 3, 2000)])
+def test_embed_grad_of_many_positions(crf, t, kind, V, D, n):
+    """More positions than a wave of the index reads or keeps at a time; tables written four rows a thread, past the caches and through them."""
+    g = generator(V + n)
+    ids, dout = ids_of(kind, n, V, g), normal(g, n, D, dtype=t)
+    got = crf.lccrf_embed_grad(dout, ids, V, scale=0.75)
+    most = int(torch.bincount(ids.long().clamp(0, V - 1)).max())
+    # positions one by one in pieces of at most 128, those one by one; the scale
+    check(got, ref.embed_grad(dout, ids, V, 0.75), ref.embed_grad(dout, ids, V, 0.75, absolute=True), min(most, 128 + most // 32) + 4, f"embed_grad {kind}")
+    assert torch.equal(got, crf.lccrf_embed_grad(dout, ids, V, scale=0.75)), "not the same again"
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("D", (1024, 1031, 3))
+def test_embed_of_many_positions(crf, t, D):
+    g = generator(D)
+    n = (36 << 20) // (D * (4 if t == torch.float32 else 2))
+    table, ids = normal(g, 999, D, dtype=t), torch.randint(-1, 1000, (n,), generator=g, device=DEV).to(torch.int32)
+    want = ref.embed(table, ids, 1.5)
+    check(crf.lccrf_embed(table, ids, scale=1.5), want, want.abs(), 1, "embed")
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("D,K", [(1024, 4), (1031, 3)])
+def test_conv_of_many_positions(crf, t, D, K):
+    """Results of more than 32 MB."""
+    g = generator(D + K)
+    B, N = 8, (36 << 20) // (8 * D * (4 if t == torch.float32 else 2))
+    x, dout, state = normal(g, B, N, 2 * D, dtype=t)[..., :D], normal(g, B, N, D, dtype=t), normal(g, B, K - 1, D, dtype=t)
+    w, bias, lens = normal(g, D, K, scale=K ** -0.5), normal(g, D, scale=0.1), conv_lengths(B, N, g)
+    want, big = (ref.conv(x, w, bias, lens, state, dout, absolute=a) for a in (False, True))
+    P = float(big["pre"].max())
+    out, final = crf.lccrf_conv(x, w, bias, lens, state=state)
+    check(out, want["out"], big["pre"], 2 * K + 10 + 2 * P, "out")
+    assert torch.equal(final.double().cpu(), want["final"]), "final"
+    got = crf.lccrf_conv_grad(dout, x, w, bias, lens, state=state)
+    E = (K + 14) * (1 + P)
+    for name, more in (("dx", K), ("dstate", K), ("dweight", B * N), ("dbias", B * N)):
+        check(getattr(got, name), want[name], big[name], E + more, name)
+
+
+@pytest.mark.parametrize("K", (2, 3, 5, 8))
+def test_conv_in_long_runs(crf, K):
+    """So many threads that a run is as long as it gets: every sequence as in a call of its own, where runs are short."""
+    g = generator(K)
+    t, B, N, D = torch.bfloat16, 64, 2100, 512
+    x, dout, state = normal(g, B, N, D, dtype=t), normal(g, B, N, D, dtype=t), normal(g, B, K - 1, D, dtype=t)
+    w, bias, lens = normal(g, D, K), normal(g, D), conv_lengths(B, N, g)
+    out, final = crf.lccrf_conv(x, w, bias, lens, state=state)
+    grad = crf.lccrf_conv_grad(dout, x, w, bias, lens, state=state)
+    dweight, dbias = torch.zeros(D, K, dtype=torch.float64, device=DEV), torch.zeros(D, dtype=torch.float64, device=DEV)
+    for b in range(B):
+        at = slice(b, b + 1)
+        one, last = crf.lccrf_conv(x[at], w, bias, lens[at], state=state[at])
+        assert torch.equal(out[at], one) and torch.equal(final[at], last), b
+        own = crf.lccrf_conv_grad(dout[at], x[at], w, bias, lens[at], state=state[at])
+        assert torch.equal(grad.dx[at], own.dx) and torch.equal(grad.dstate[at], own.dstate), b
+        dweight, dbias = dweight + own.dweight.double(), dbias + own.dbias.double()
+    # sums of B N terms of about 1: either side's error stays below their number's root times their size
+    assert float((grad.dweight.double() - dweight).abs().max()) <= B * N * U * 100 and float((grad.dbias.double() - dbias).abs().max()) <= B * N * U * 100
+
+
+@pytest.mark.parametrize("S", (4, 8, 16))
+@pytest.mark.parametrize("D,G", [(256, 1), (193, 1), (512, 2), (768, 3)])
+def test_gradient_of_four_tiles_a_workgroup(crf, S, D, G):
+    g = generator(S * D)
+    inputs = scan_inputs(g, torch.float32, 3, 45, D, S, G, gate=G != 3)
+    check_scan(crf, inputs, conv_lengths(3, 45, g), normal(g, 3, D, S), normal(g, 3, 45, D))
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("B", (65, 130, 256, 257))
+@pytest.mark.parametrize("S", (4, 16, 24))
+def test_scan_of_many_ragged_sequences(crf, t, B, S):
+    """None is cut; up to 256 are worked on by length."""
+    g = generator(B + S)
+    inputs = scan_inputs(g, t, B, 40, 20, S, 1)
+    check_scan(crf, inputs, conv_lengths(B, 40, g), normal(g, B, 20, S), normal(g, B, 40, 20, dtype=t))
+
+
+@pytest.mark.parametrize("S", (3, 16, 24))
+def test_roundings_of_wide_rows(crf, S):
+    """Only the vectors' gradients add up over the channels: all other results are as near the formula as those of one channel."""
+    g = generator(S)
+    B, N, D = 2, 24, 2048
+    inputs = scan_inputs(g, torch.float32, B, N, D, S, 1)
+    state, dout = normal(g, B, D, S), normal(g, B, N, D)
+    want, big = (ref.scan(*inputs.values(), None, state, dout, absolute=a) for a in (False, True))
+    R = scan_roundings(N, S, 0, inputs["z"])
+    out, final = crf.lccrf_state_scan(*inputs.values(), state=state)
+    check(out, want["out"], big["out"], R, "out")
+    check(final, want["final"], big["final"], R, "final")
+    got = crf.lccrf_state_scan_grad(dout, *inputs.values(), state=state)
+    for name in got._fields:
+        more = 2 * D if name in ("dBm", "dCm") else B * N if name in ("dA", "dD", "ddt_bias") else 0
+        check(getattr(got, name), want[name], big[name], R + more, name)
