@@ -375,7 +375,8 @@ hipError_t embed_of(const void* table, int V, int D, int64_t table_row, const in
     // positions a workgroup: its threads' kItems pieces, one position at least
     const int per_block = cpr >= 256 * kItems ? 1 : 256 * kItems / cpr;
     if (!fits((n + per_block - 1) / per_block, 256)) return hipErrorInvalidValue;
-    const auto kernel = past_caches(n * D * static_cast<int64_t>(sizeof(T))) ? embed_kernel<T, SMALL, true> : embed_kernel<T, SMALL, false>;
+    // (rows narrower than a piece go out element by element: through the caches)
+    const auto kernel = past_caches(n * D * static_cast<int64_t>(sizeof(T))) ? embed_kernel<T, SMALL, !SMALL> : embed_kernel<T, SMALL, false>;
     kernel<<<static_cast<unsigned>((n + per_block - 1) / per_block), 256, 0, st>>>(static_cast<const T*>(table), V, D, table_row, ids, n, scale,
                                                                                            static_cast<T*>(out), cpr, per_block);
     return hipGetLastError();
@@ -403,11 +404,11 @@ hipError_t embed_grad_of(AnyRows dout, const int32_t* ids, int B, int N, int V, 
     if (const hipError_t e = ask_lds(reinterpret_cast<const void*>(index_kernel), static_cast<int>(sizeof(int32_t)) * kIndexWaves * (kMaxRange + kKept), asked); e != hipSuccess)
         return e;
     const int64_t table_bytes = static_cast<int64_t>(V) * D * static_cast<int64_t>(sizeof(T));
-    const bool stream = past_caches(table_bytes);
+    const bool stream = past_caches(table_bytes);  // (such a table has four rows a thread: 2^20 pieces are at most 16 MB)
     index_kernel<<<sparse && plan.workgroups < 256 ? 256 : plan.workgroups, kIndexThreads, bytes, st>>>(ids, n, V, plan.range, order, start, sparse ? static_cast<char*>(grad) : nullptr, table_bytes);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const auto rows = sparse ? rows_kernel<T, SMALL, 0, false> : four ? (stream ? rows_kernel<T, SMALL, 4, true> : rows_kernel<T, SMALL, 4, false>)
-                           : (stream ? rows_kernel<T, SMALL, 1, true> : rows_kernel<T, SMALL, 1, false>);
+    const auto rows = sparse ? rows_kernel<T, SMALL, 0, false> : !four ? rows_kernel<T, SMALL, 1, false>
+                      : stream ? rows_kernel<T, SMALL, 4, !SMALL> : rows_kernel<T, SMALL, 4, false>;
     if (piece_blocks + row_blocks) rows<<<static_cast<unsigned>(piece_blocks + row_blocks), 256, 0, st>>>(a, dout.as<T>(), static_cast<T*>(grad), static_cast<int>(piece_blocks));
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (pieces) join_kernel<T, SMALL><<<static_cast<unsigned>((pieces * cpr + 255) / 256), 256, 0, st>>>(a, static_cast<T*>(grad));
