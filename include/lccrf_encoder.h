@@ -50,7 +50,8 @@ int lccrf_embed(const void* table, lccrf_dtype dt, int V, int D, int64_t table_r
  * Its gradient: grad[v] = scale * sum of dout[p] over the positions with ids[p] = v, [V][D], every row
  * written (0 where no position has it).  The positions are sorted by token first, so that every row is
  * summed in a fixed order.  dout: [B][N][D] rows; ids int32 [B * N], B * N <= 2^30.
- * B or N may be 0.
+ * The sums are held in float and rounded once, to dt: a table and its gradient are one type, half of the bytes written
+ * in LCCRF_BF16 (a float gradient of the same positions takes float dout).  B or N may be 0.
  */
 size_t lccrf_embed_grad_workspace_bytes(int64_t n, int V, int D);
 int lccrf_embed_grad(const lccrf_rows* dout, lccrf_dtype dt, const int32_t* ids, int B, int N, int V, int D,

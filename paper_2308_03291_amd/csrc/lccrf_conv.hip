@@ -3,8 +3,8 @@
 // K products an output: the traffic of the input read and the output written once is what bounds all three.  A thread has a
 // 16-byte piece of the channels and walks along a run of positions, its K last inputs in registers, so an input is read
 // once but for the K - 1 in front of every run (which another thread has just read).  Measured, inputs cold: forward B=64 N=512 D=2048
-// bfloat16, 270 MB, 63 us (4.3 TB/s); forward and gradient of B=128 N=128 D=1001 float, ragged, 207 MB, 76 us.  A step of 64 streams with D=2048
-// takes the kernel 3.6 us, its launch and the call more.
+// bfloat16, 270 MB, 61.5 us (4.4 TB/s); forward and gradient of B=128 N=128 D=1001 float, ragged, 207 MB, 74.5 us (padding goes through the gradient's
+// arithmetic like any position).  A step of 64 streams with D=2048 takes the kernel 3.4 us, its launch and the call more.
 #include "lccrf_encoder.h"
 
 namespace lccrf {

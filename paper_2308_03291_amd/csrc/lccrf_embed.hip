@@ -13,8 +13,9 @@
 //      Tokens with more than `piece` positions (in text a few hold a tenth of all) are cut into the pieces of `piece` sorted
 //      positions that they reach into, one partial sum each.
 //   3. join: those partial sums, in order.
-// The traffic of the gradients read and of the table written is what bounds it: 32768 positions of 1024 bfloat16 into 100003 rows, 272 MB, 61 us
-// (index 10.7, rows 46.6, join 5.0); small ones are bound by their three launches (2048 positions of 301 floats, 15.7 us).
+// The traffic of the gradients read and of the table written is what bounds it: 32768 positions of 1024 bfloat16 into 100003 rows, 272 MB, 59 us
+// (index 10.7, rows 46.0, join 4.9); small ones are bound by their three launches (2048 positions of 301 floats, 16 us).  Every workgroup of the
+// index reads all ids: with many positions of narrow rows it costs most (1048576 of 32 floats into 50000 rows 71 us, the rows 28).
 #include "lccrf_encoder.h"
 
 #include <type_traits>

@@ -3,7 +3,7 @@
 // An update of one state is a product, an exponential (two issue slots), a product, two fused multiply-adds: six slots of a
 // SIMD, which with 16 states bound the pass before its traffic does (a channel and position takes 96 slots and some 30 for step and
 // gate, against 8 bytes).  All of it is vector arithmetic: the decays differ by channel and state, so no matrix instruction has the form.
-// Measured (B=64 N=512 D=2048 S=16, bfloat16, gated): 255 us, 2.1 TB/s; 116 vector instructions a channel and position, the vector
+// Measured (B=64 N=512 D=2048 S=16, bfloat16, gated): 256 us, 2.1 TB/s; 116 vector instructions a channel and position, the vector
 // pipes busy 92 % of the time, at the 2.0 GHz that the card keeps under this load.
 // Segments of a sequence run side by side where the batch is small (scan_plan).
 #include "lccrf_state.h"
@@ -296,8 +296,8 @@ __global__ __launch_bounds__(kJoin) void join_segments_kernel(ScanIn in, ScanPla
 
 // ---- one position ---------------------------------------------------------------------------------------------
 // A thread has four states of a channel and `many` streams one after the other, their states in flight together; LQ threads a
-// channel.  The states read and written are what bounds it: 512 streams of D=2048 S=16, 143 MB, 24.6 us (5.8 TB/s: a part of them stays in
-// the memory-side cache); four of D=1024 3.4 us, bound by one pass's latency.
+// channel.  The states read and written are what bounds it: 512 streams of D=2048 S=16, 143 MB, 25.0 us (5.7 TB/s: a part of them stays in
+// the memory-side cache); four of D=1024 3.2 us, bound by one pass's latency.
 template <typename T, int LQ, int MANY, bool WHOLE>
 __global__ __launch_bounds__(256) void step_kernel(ScanIn in, float* __restrict__ state, T* __restrict__ out) {
     const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;

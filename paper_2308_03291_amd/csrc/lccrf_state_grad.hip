@@ -8,7 +8,7 @@
 // The states in front of every eighth position are saved by the forward pass; eight positions are run again from there, their
 // states kept in registers, and then gone through backwards.  27 vector instructions an update with 16 states (counted: 5 forwards, 10
 // backwards, the rest for sums over the channels and what is computed once a channel), two of them exponentials: vector arithmetic
-// bounds it (B=128 N=256 D=1024 S=16, bfloat16, ragged: 345 us, the vector pipes busy 95 % of them).
+// bounds it (B=128 N=256 D=1024 S=16, bfloat16, ragged: 313 us, the vector pipes busy 96 % of them).
 //
 // A wave has 64 channels and up to 8 states: 72 registers of states, three waves a SIMD.  Measured on the whole training step of that
 // batch: 16 states a wave spilled, and left no registers for the next positions' inputs (1290 us against 536 at that time); the

@@ -8,6 +8,9 @@ Activations (``table``, ``x``, ``dt``, ``Bm``, ``Cm``, ``z``, ``dout`` and the c
 bfloat16; weights (``weight``, ``bias``, ``A``, ``D``, ``dt_bias``), their gradients and the scan's state are float32.
 Activations may be views whose rows are dense (half of a projection's output, an expanded row); weights and states are
 contiguous, and so are results.
+
+As everywhere in ``binding``, results carry no history for torch's automatic differentiation, whether inputs require gradients or
+not: a backward pass is the ``_grad`` calls, by hand (``tagger`` has one) or inside a ``torch.autograd.Function``.
 """
 from __future__ import annotations
 
@@ -158,7 +161,9 @@ def lccrf_embed(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, o
 def lccrf_embed_grad(dout: torch.Tensor, ids: torch.Tensor, V: int, *, scale: float = 1.0, out: Optional[torch.Tensor] = None,
                      workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of ``lccrf_embed`` by its table, [V, D] in dout's dtype: every row is scale times the sum, in a fixed order, of the
-    rows of dout [B, N, D] (or [n, D]) whose id (int32 [B, N] or [n]) it is; ids outside [0, V) have none."""
+    rows of dout [B, N, D] (or [n, D]) whose id (int32 [B, N] or [n]) it is; ids outside [0, V) have none.  Summed in float32 and
+    rounded once: the gradient of a bfloat16 table is bfloat16, and where the master copy is float32 (as in ``tagger``) that rounding is the
+    only one it adds."""
     dt, dtype, dev = _first(dout, "dout")
     if dout.dim() == 2:
         dout, ids = dout[None], ids[None]
