@@ -34,7 +34,7 @@ struct GradPlan {
 GradPlan grad_plan(int B, int N, int D, int S, int G) {
     GradPlan p;
     p.state_waves = S <= 8 ? 1 : S <= 16 ? 2 : S <= 32 ? 4 : 8;
-    p.scan = scan_plan(B, N, D, G, false, p.state_waves, 3072, 2);
+    p.scan = scan_plan(B, N, D, G, false, p.state_waves, 3 * 1024, 2);  // three waves a SIMD
     p.tile_waves = p.state_waves >= 4 ? 1 : 4 / p.state_waves;
     while (p.scan.tiles % p.tile_waves) p.tile_waves /= 2;  // no wave without a channel
     p.parts = p.scan.tiles / p.tile_waves;

@@ -62,7 +62,7 @@ def test_the_longest_scan(crf):
     alike(g.ddt[:, inner], (dput * 1.5 + back * -0.5) * 0.5, 1000)  # a difference twelve times smaller than what it is of
     alike(g.dBm[:, inner], dh * step * 1.5, 80)
     alike(g.dCm[:, inner], -0.5 * h, 80)
-    alike(g.dD, -0.5 * 1.5 * MOST, 2 ** 20 + 400)  # a wave adds a segment's positions, 3072 of them are joined
+    alike(g.dD, -0.5 * 1.5 * MOST, 2 ** 20 + 400)  # a wave adds a segment's positions, three waves a SIMD are joined
     alike(g.dA, back * step * MOST, 2 ** 20 + 400)
 
 
