@@ -39,6 +39,9 @@ EXPORTS = (
     "lccrf_embed", "lccrf_embed_grad", "lccrf_embed_grad_workspace_bytes", "lccrf_conv", "lccrf_conv_grad",
     "lccrf_conv_grad_workspace_bytes", "lccrf_conv_step", "lccrf_state_scan", "lccrf_state_scan_saved_bytes",
     "lccrf_state_scan_workspace_bytes", "lccrf_state_scan_grad", "lccrf_state_scan_grad_workspace_bytes", "lccrf_state_step",
+    "lccrf_recurrence", "lccrf_recurrence_saved_bytes", "lccrf_recurrence_workspace_bytes", "lccrf_recurrence_grad",
+    "lccrf_recurrence_grad_workspace_bytes", "lccrf_recurrence_step", "lccrf_group_norm", "lccrf_group_norm_workspace_bytes", "lccrf_group_norm_grad",
+    "lccrf_group_norm_grad_workspace_bytes", "lccrf_distill", "lccrf_distill_grad",
 )
 
 _lib = None
@@ -117,6 +120,7 @@ def load_library() -> ctypes.CDLL:
     lib.lccrf_auto_algo.argtypes = [i, i, i, i]
     lib.lccrf_auto_algo.restype = i
     _encoder.declare(lib)
+    _layers.declare(lib)
     _lib = lib
     return lib
 
@@ -465,3 +469,9 @@ from . import encoder as _encoder  # noqa: E402
 from .encoder import (  # noqa: E402,F401
     lccrf_conv, lccrf_conv_grad, lccrf_conv_step, lccrf_embed, lccrf_embed_grad, lccrf_state_scan, lccrf_state_scan_grad,
     lccrf_state_step, state_scan_saved)
+
+# What a smaller tagger adds to it (include/lccrf_layers.h).
+from . import layers as _layers  # noqa: E402
+from .layers import (  # noqa: E402,F401
+    group_norm_stats, lccrf_distill, lccrf_distill_grad, lccrf_group_norm, lccrf_group_norm_grad, lccrf_recurrence, lccrf_recurrence_grad,
+    lccrf_recurrence_step, recurrence_saved)
