@@ -1,6 +1,8 @@
 // Gated linear recurrence: forward pass and single-token form (lccrf_recur.h says how the work is spread).
 #include "lccrf_recur.h"
 
+#include <type_traits>
+
 namespace lccrf {
 namespace enc {
 namespace {
@@ -17,29 +19,33 @@ struct RecurRun {
     RecurPlan plan;
 };
 
-template <typename T, int V, int P, int W, int MODE, bool GATED>
+template <typename T, int V, int P, int W, int SUB, int MODE, bool GATED>
 __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
+    constexpr int L = 64 / SUB, kRows = SUB * P, kBlock = W * kRows;  // lanes across the tile; positions a wave and a block
     typedef float Pair __attribute__((ext_vector_type(2 * V)));
     typedef Pair AnyPair __attribute__((aligned(4)));
-    __shared__ Pair pairs[W > 1 ? 2 : 1][W][64];
+    typedef float Some __attribute__((ext_vector_type(V)));
+    __shared__ Pair pairs[W > 1 ? 2 : 1][W][L];
+    __shared__ Some states[W > 1 ? 2 : 1][L];  // in front of the block
     const RecurIn& in = r.in;
-    const int lane = threadIdx.x & 63, w = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
-    const unsigned which = blockIdx.x / r.plan.tiles;
-    const int tile = blockIdx.x - which * r.plan.tiles;
-    const int b = which / r.plan.segments, seg = which - b * r.plan.segments;
-    const Lane<V> my(tile, lane, in.D);
+    const int lane = threadIdx.x & 63, cl = lane % L, w = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+    const int sub = lane / L, set = sub * P;
+    const RecurWork work = recur_work(r.plan);
+    const int tile = work.tile, b = static_cast<int>(work.which / r.plan.segments), seg = static_cast<int>(work.which - static_cast<int64_t>(b) * r.plan.segments);
+    if (b >= in.B) return;
+    const Lane<V> my(tile, cl, L, in.D);
     const unsigned bytes = static_cast<unsigned>(my.c) * sizeof(T);
     const int len = length_at(in.lengths, b, in.N), begin = seg * r.plan.seg_len;
     const int stop = in.N - begin < r.plan.seg_len ? in.N : begin + r.plan.seg_len, end = stop < len ? stop : len;
     T* out = static_cast<T*>(r.out) + static_cast<int64_t>(b) * in.N * in.D;
 
     RecurChannel ch[V];
-    float carry[V], total[V];  // the state before the block; kEnds: what of it is the product of the decays
+    float carry[V], total[V];  // the state in front of the first block, later (the last lanes': behind their positions) of the next one; kEnds: this lane's product of decays
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         ch[j] = recur_channel(in, my.c + j);
         carry[j] = seg == 0 && r.state ? r.state[static_cast<int64_t>(b) * in.D + my.c + j] : 0.0f;
-        total[j] = seg == 0 ? 0.0f : 1.0f;
+        total[j] = 1.0f;
     }
     if (!(MODE & kEnds)) {
         const float* e = r.ends + (static_cast<int64_t>(b) * r.plan.segments * in.D + my.c) * 2;
@@ -50,24 +56,33 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
             for (int j = 0; j < V; ++j) carry[j] = fmaf(made[2 * j], carry[j], made[2 * j + 1]);
         }
     }
+    const bool last = w == W - 1 && sub == SUB - 1;
 
     if (begin < end) {
         Bit<T, V> xr[P], fr[P], gr[P], zr[P];
-        const auto fetch = [&](int l0) {
-            take_rows<T, V, P>(fr, in.f, b, l0, len, bytes);
-            take_rows<T, V, P>(gr, in.g, b, l0, len, bytes);
-            take_rows<T, V, P>(xr, in.x, b, l0, len, bytes);
-            if (GATED) take_rows<T, V, P>(zr, in.z, b, l0, len, bytes);
+        const auto fetch = [&](int first) {
+            take_rows<T, V, P, SUB>(fr, in.f, b, first, len, set, bytes);
+            take_rows<T, V, P, SUB>(gr, in.g, b, first, len, set, bytes);
+            take_rows<T, V, P, SUB>(xr, in.x, b, first, len, set, bytes);
+            if (GATED) take_rows<T, V, P, SUB>(zr, in.z, b, first, len, set, bytes);
         };
-        fetch(begin + w * P);
         int buffer = 0;
-        for (int block = begin; block < end; block += W * P) {
-            const int l0 = block + w * P;
-            float a[P][V], put[P][V], h[V];
+        const auto leave = [&](int to) {
+            Some s;
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] = carry[j];
+            if (last) states[to][cl] = s;
+        };
+        if (W > 1) leave(0);
+        const auto run = [&](auto whole, int first) {  // whole: all positions lie before the end, all lanes have channels of their own
+            constexpr bool WHOLE = decltype(whole)::value;
+            const int l0 = first + set;
+            float a[P][V], put[P][V];
+            float(&h)[V] = carry;
             Bit<T, V> z[P];
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                const bool on = l0 + i < end;
+                const bool on = WHOLE || l0 + i < end;
                 float x[V], f[V], g[V];
                 xr[i].get(x);
                 fr[i].get(f);
@@ -77,42 +92,53 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
                 for (int j = 0; j < V; ++j) {
                     const Decay d = decay_of(f[j], ch[j]);
                     a[i][j] = on ? d.a : 1.0f;
-                    put[i][j] = on ? __builtin_amdgcn_sqrtf(d.rest) * sigmoid(g[j] + ch[j].g_bias) * x[j] : 0.0f;
+                    put[i][j] = on ? __builtin_amdgcn_sqrtf(d.rest) * open_gate(g[j], ch[j].g_bias) * x[j] : 0.0f;
                 }
             }
-            fetch(l0 + W * P);
+            fetch(first + kBlock);
             if constexpr (W > 1) {
                 Pair mine;
+                float A[V], E[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    float E = put[0][j];
+                    E[j] = put[0][j];
 #pragma unroll
-                    for (int i = 1; i < P; ++i) E = fmaf(a[i][j], E, put[i][j]);
-                    mine[2 * j] = product_of(a, j);
-                    mine[2 * j + 1] = E;
+                    for (int i = 1; i < P; ++i) E[j] = fmaf(a[i][j], E[j], put[i][j]);
+                    A[j] = product_of(a, j);
+                    if (MODE & kEnds) total[j] = product(total[j], A[j]);
+                    const float own_a = A[j], own_e = E[j];
+                    before_set<SUB, false>(A[j], E[j], sub);
+                    mine[2 * j] = SUB > 1 ? product(own_a, A[j]) : own_a;
+                    mine[2 * j + 1] = SUB > 1 ? fmaf(own_a, E[j], own_e) : own_e;
                 }
-                pairs[buffer][w][lane] = mine;
+                if (SUB == 1 || sub == SUB - 1) pairs[buffer][w][cl] = mine;
                 lds_sync();
+                Pair others[W - 1];
+                const Some from = states[buffer][cl];
 #pragma unroll
-                for (int k = 0; k < W; ++k) {
-                    const Pair other = pairs[buffer][k][lane];
+                for (int k = 0; k < W - 1; ++k) others[k] = pairs[buffer][k][cl];
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        h[j] = k == w ? carry[j] : h[j];
-                        carry[j] = fmaf(other[2 * j], carry[j], other[2 * j + 1]);
-                        if (MODE & kEnds) total[j] = product(total[j], other[2 * j]);
-                    }
+                for (int j = 0; j < V; ++j) h[j] = from[j];
+#pragma unroll
+                for (int k = 0; k < W - 1; ++k) {
+                    if (k == w) break;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) h[j] = fmaf(others[k][2 * j], h[j], others[k][2 * j + 1]);
+                }
+                if (SUB > 1) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) h[j] = fmaf(A[j], h[j], E[j]);
                 }
                 buffer ^= 1;
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) h[j] = carry[j];
             }
             if ((MODE & kSave) && l0 % kRecurSave == 0 && l0 < end)
-                my.give(r.saved + (static_cast<int64_t>(b) * ((in.N + kRecurSave - 1) / kRecurSave) + l0 / kRecurSave) * in.D, h);
+                my.template give<WHOLE>(r.saved + (static_cast<int64_t>(b) * ((in.N + kRecurSave - 1) / kRecurSave) + l0 / kRecurSave) * in.D, h);
             if constexpr ((MODE & kOut) != 0 || W == 1) {
+                // a place for the whole wave and the lane's offset in it
+                T* to = out + static_cast<int64_t>(first) * in.D;
+                const unsigned at = static_cast<unsigned>(set) * static_cast<unsigned>(in.D);
 #pragma unroll
-                for (int i = 0; i < P; ++i) {
+                for (int i = 0; i < P; ++i, to += in.D) {
                     float o[V];
 #pragma unroll
                     for (int j = 0; j < V; ++j) h[j] = fmaf(a[i][j], h[j], put[i][j]);
@@ -122,34 +148,55 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
 #pragma unroll
                         for (int j = 0; j < V; ++j) {
                             o[j] = GATED ? h[j] * silu(zi[j]) : h[j];
-                            o[j] = l0 + i < end ? o[j] : 0.0f;
+                            o[j] = WHOLE || l0 + i < end ? o[j] : 0.0f;
                         }
-                        if (l0 + i < stop) my.give(out + static_cast<int64_t>(l0 + i) * in.D, o);
+                        if (WHOLE || l0 + i < stop) my.template give<WHOLE>(to, o, SUB > 1 ? at : 0u);
                     }
                 }
-                if (W == 1) {
+            } else if (w == W - 1) {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) carry[j] = h[j];
-                }
+                for (int i = 0; i < P; ++i)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) h[j] = fmaf(a[i][j], h[j], put[i][j]);
             }
-        }
+            if (W > 1) leave(buffer);
+        };
+        fetch(begin + w * kRows);
+        int block = begin;
+        if (my.full)
+            for (; block + kBlock <= end; block += kBlock) run(std::true_type{}, block + w * kRows);
+        for (; block < end; block += kBlock) run(std::false_type{}, block + w * kRows);
     }
     if (MODE & kOut) {
         const float zero[V] = {};
-        const int done = begin < end ? begin + (end - begin + W * P - 1) / (W * P) * (W * P) : begin;
-        for (int l = done + w; l < stop; l += W) my.give(out + static_cast<int64_t>(l) * in.D, zero);
+        const int done = begin < end ? begin + (end - begin + kBlock - 1) / kBlock * kBlock : begin;
+        for (int l = done + w * SUB + sub; l < stop; l += W * SUB) my.give(out + static_cast<int64_t>(l) * in.D, zero);
     }
-    if (w) return;
-    if (MODE & kEnds) {
-        float* e = r.ends + ((static_cast<int64_t>(b) * r.plan.segments + seg) * in.D + my.c) * 2;
+    if constexpr ((MODE & kEnds) != 0) {
+        // the product over all lanes of a channel, each with its positions of all blocks (in front of the first segment is the call's own state: nothing else
+        // is taken from there)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int d = L; d < 64; d *= 2) total[j] = product(total[j], __shfl_xor(total[j], d));
+        lds_sync();
+        if (sub == 0) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) pairs[0][w][cl][j] = total[j];
+        }
+        lds_sync();
+        if (!last) return;
         Pair made;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            made[2 * j] = total[j];
+            float all = seg == 0 ? 0.0f : 1.0f;
+#pragma unroll
+            for (int k = 0; k < W; ++k) all = product(all, pairs[0][k][cl][j]);
+            made[2 * j] = all;
             made[2 * j + 1] = carry[j];
         }
-        *reinterpret_cast<AnyPair*>(e) = made;  // (a channel that two lanes have: the same twice)
-    } else if (r.final_state && end == len && (begin < len || seg == 0)) {
+        *reinterpret_cast<AnyPair*>(r.ends + ((static_cast<int64_t>(b) * r.plan.segments + seg) * in.D + my.c) * 2) = made;  // (a channel of two lanes: the same twice)
+    } else if (last && r.final_state && end == len && (begin < len || seg == 0)) {
         my.give(r.final_state + static_cast<int64_t>(b) * in.D, carry);
     }
 }
@@ -179,7 +226,7 @@ __global__ __launch_bounds__(256) void recur_step_kernel(RecurIn in, int cpr, fl
     for (int j = 0; j < W; ++j) {
         const RecurChannel ch = recur_channel(in, c + j);
         const Decay d = decay_of(f[j], ch);
-        h[j] = fmaf(d.a, h[j], __builtin_amdgcn_sqrtf(d.rest) * sigmoid(g[j] + ch.g_bias) * x[j]);
+        h[j] = fmaf(d.a, h[j], __builtin_amdgcn_sqrtf(d.rest) * open_gate(g[j], ch.g_bias) * x[j]);
         o[j] = GATED ? h[j] * silu(z[j]) : h[j];
     }
     Piece<float, W, W == 1>::put(mine, W, h);
@@ -198,42 +245,36 @@ hipError_t recur_step_of(const RecurIn& in, float* state, void* out, hipStream_t
 
 // ---- launches -------------------------------------------------------------------------------------------------
 
-constexpr int kPositions = 8, kWaves = 8;  // a wave's and a workgroup's
-static_assert(kRecurBlock % (kPositions * kWaves) == 0 && kRecurSave % kPositions == 0, "");
+constexpr int kPositions = 4, kWaves = 8, kFewWaves = 4;  // a lane's positions; a workgroup's waves, and where sequences are cut
 
 int channels_a_lane(int D) { return D == 1 ? 1 : 2; }
 
-RecurPlan recur_plan(int B, int N, int D) {
-    RecurPlan p;
-    p.tiles = (D - 1) / (64 * channels_a_lane(D)) + 1;
-    const int64_t groups = static_cast<int64_t>(B) * p.tiles, most = (static_cast<int64_t>(N) + 255) / 256;
-    int64_t segments = groups <= 128 ? 512 / groups : 1;
-    if (segments > most) segments = most;
-    p.seg_len = static_cast<int>(((N + segments - 1) / segments + kRecurBlock - 1) / kRecurBlock * kRecurBlock);
-    p.segments = static_cast<int>((static_cast<int64_t>(N) + p.seg_len - 1) / p.seg_len);
-    return p;
-}
+// Measured, us, wide tiles / narrow / segments (B x N x D, bfloat16, no gate but in the first): 64x512x2048 146 / 165 / 237, 16x1000x1024 64 / 58 / 68, 30x300x300
+// 27 / 22 / 24, 8x256x1024 20 / 16.5 / 19, 4x5000x1024 291 / 117 / 84, 2x10000x256 573 / 170 / 34, 4x16384x514 933 / 291 / 124.
+RecurPlan recur_plan(int B, int N, int D) { return recur_plan_of(B, N, D, 256, 256, 512); }
 
-template <typename T, int V, int W, int MODE>
+template <typename T, int V, int W, int SUB, int MODE>
 hipError_t recur_launch(const RecurRun& r, hipStream_t st) {
     const bool gated = (MODE & kOut) && r.in.z.data;
-    const auto kernel = gated ? recur_kernel<T, V, kPositions, W, MODE, (MODE & kOut) != 0> : recur_kernel<T, V, kPositions, W, MODE, false>;
-    kernel<<<static_cast<unsigned>(static_cast<int64_t>(r.in.B) * r.plan.segments * r.plan.tiles), 64 * W, 0, st>>>(r);
+    const auto kernel = gated ? recur_kernel<T, V, kPositions, W, SUB, MODE, (MODE & kOut) != 0> : recur_kernel<T, V, kPositions, W, SUB, MODE, false>;
+    kernel<<<static_cast<unsigned>(recur_blocks(r.plan, r.in.B)), 64 * W, 0, st>>>(r);
     return hipGetLastError();
 }
-template <typename T, int V, int W>
+template <typename T, int V, int W, int SUB>
 hipError_t recur_of(const RecurRun& r, hipStream_t st) {
-    if constexpr (W > 1) {
-        if (r.plan.segments > 1)
-            if (const hipError_t e = recur_launch<T, V, W, kEnds>(r, st); e != hipSuccess) return e;
-    }
-    if (!r.out) return recur_launch<T, V, W, kSave>(r, st);
-    return r.saved ? recur_launch<T, V, W, kOut | kSave>(r, st) : recur_launch<T, V, W, kOut>(r, st);
+    if constexpr (W == kFewWaves)
+        if (const hipError_t e = recur_launch<T, V, W, SUB, kEnds>(r, st); e != hipSuccess) return e;
+    if (!r.out) return recur_launch<T, V, W, SUB, kSave>(r, st);
+    return r.saved ? recur_launch<T, V, W, SUB, kOut | kSave>(r, st) : recur_launch<T, V, W, SUB, kOut>(r, st);
 }
-template <typename T>
+template <typename T, int V>
 hipError_t recur_by(const RecurRun& r, hipStream_t st) {
-    if (channels_a_lane(r.in.D) == 1) return r.in.N <= kPositions ? recur_of<T, 1, 1>(r, st) : recur_of<T, 1, kWaves>(r, st);
-    return r.in.N <= kPositions ? recur_of<T, 2, 1>(r, st) : recur_of<T, 2, kWaves>(r, st);
+    if (r.plan.segments > 1) return recur_of<T, V, kFewWaves, 1>(r, st);
+    if (r.in.N <= kPositions) return recur_of<T, V, 1, 1>(r, st);
+    if constexpr (V > 1) {
+        if (r.plan.sets > 1) return recur_of<T, V, kWaves, 4>(r, st);
+    }
+    return recur_of<T, V, kWaves, 1>(r, st);
 }
 
 }  // namespace
@@ -246,9 +287,11 @@ size_t recur_workspace(int B, int N, int D) {
 }
 
 hipError_t launch_recur(int dtype, const RecurIn& in, const float* state, void* out, float* final_state, float* saved, void* ws, hipStream_t st) {
-    const RecurRun r{in, state, out, final_state, saved, static_cast<float*>(ws), recur_plan(in.B, in.N, in.D)};
-    if (!fits(static_cast<int64_t>(in.B) * r.plan.segments * r.plan.tiles, 64 * kWaves)) return hipErrorInvalidValue;
-    return dtype ? recur_by<uint16_t>(r, st) : recur_by<float>(r, st);
+    RecurRun r{in, state, out, final_state, saved, static_cast<float*>(ws), recur_plan(in.B, in.N, in.D)};
+    if (!near_rows(in.x) || !near_rows(in.f) || !near_rows(in.g) || !near_rows(in.z)) widen_tiles(r.plan, in.D);
+    if (!fits(recur_blocks(r.plan, in.B), 64 * kWaves)) return hipErrorInvalidValue;
+    if (channels_a_lane(in.D) == 1) return dtype ? recur_by<uint16_t, 1>(r, st) : recur_by<float, 1>(r, st);
+    return dtype ? recur_by<uint16_t, 2>(r, st) : recur_by<float, 2>(r, st);
 }
 
 hipError_t launch_recur_step(int dtype, const RecurIn& in, float* state, void* out, hipStream_t st) {

@@ -8,12 +8,12 @@
 // them, A c + G.  The states in front of every block are saved by the forward pass, so one pass over the inputs is enough.
 #include "lccrf_recur.h"
 
+#include <type_traits>
+
 namespace lccrf {
 namespace enc {
 namespace {
 
-constexpr int P = 4, W = 8;  // positions a wave, waves
-static_assert(P * W == kRecurSave, "a block begins where a state is saved");
 
 struct GradRun {
     RecurIn in;
@@ -25,30 +25,33 @@ struct GradRun {
     RecurPlan plan;
 };
 
-template <typename T, int V, bool GATED, bool ENDS>
+template <typename T, int V, int P, int W, int SUB, bool GATED, bool ENDS>
 __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
-    typedef float Four __attribute__((ext_vector_type(4)));
+    constexpr int L = 64 / SUB, kRows = SUB * P, kBlock = W * kRows;
+    typedef float Three __attribute__((ext_vector_type(4)));
     typedef float Pair __attribute__((ext_vector_type(2 * V)));
     typedef Pair AnyPair __attribute__((aligned(4)));
-    __shared__ Four made[2][W][V][64];  // A, E, G
-    __shared__ float sums[ENDS ? 1 : W][3][V][64];
+    __shared__ Three made[2][W][V][L];  // A, E, G
+    __shared__ float behinds[2][V][L];
+    __shared__ float sums[ENDS ? 1 : W][3][V][L];
     const RecurIn& in = r.in;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned which = blockIdx.x / r.plan.tiles;
-    const int tile = blockIdx.x - which * r.plan.tiles;
-    const int b = which / r.plan.segments, seg = which - b * r.plan.segments;
-    const Lane<V> my(tile, lane, in.D);
+    const int lane = threadIdx.x & 63, cl = lane % L, sub = lane / L, set = sub * P, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const RecurWork work = recur_work(r.plan);
+    const int tile = work.tile, b = static_cast<int>(work.which / r.plan.segments), seg = static_cast<int>(work.which - static_cast<int64_t>(b) * r.plan.segments);
+    if (b >= in.B) return;
+    const Lane<V> my(tile, cl, L, in.D);
     const unsigned bytes = static_cast<unsigned>(my.c) * sizeof(T);
     const int len = length_at(in.lengths, b, in.N), begin = seg * r.plan.seg_len;
     const int stop = in.N - begin < r.plan.seg_len ? in.N : begin + r.plan.seg_len, end = stop < len ? stop : len;
-    const int64_t first = static_cast<int64_t>(b) * in.N;
+    const int64_t first_row = static_cast<int64_t>(b) * in.N;
+    const bool front = w == 0 && sub == 0;
 
     RecurChannel ch[V];
-    float behind[V], total[V], s_log[V], s_f[V], s_g[V];  // the gradient by the state behind the block; sums over this wave's positions
+    float c[V], total[V], s_log[V], s_f[V], s_g[V];  // the gradient behind (the front lanes': the next) block; this lane's product and sums
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         ch[j] = recur_channel(in, my.c + j);
-        behind[j] = s_log[j] = s_f[j] = s_g[j] = 0.0f;
+        c[j] = s_log[j] = s_f[j] = s_g[j] = 0.0f;
         total[j] = 1.0f;
     }
     if (!ENDS) {
@@ -57,11 +60,11 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
         for (int s = r.plan.segments - 1; s > seg; --s) {
             const Pair e = *reinterpret_cast<const AnyPair*>(r.ends + ((base + s) * in.D + my.c) * 2);
 #pragma unroll
-            for (int j = 0; j < V; ++j) behind[j] = fmaf(e[2 * j], behind[j], e[2 * j + 1]);
+            for (int j = 0; j < V; ++j) c[j] = fmaf(e[2 * j], c[j], e[2 * j + 1]);
         }
         const float zero[V] = {};
-        for (int l = (begin < end ? end : begin) + w; l < stop; l += W) {
-            const int64_t at = (first + l) * in.D;
+        for (int l = (begin < end ? end : begin) + w * SUB + sub; l < stop; l += W * SUB) {
+            const int64_t at = (first_row + l) * in.D;
             my.give(static_cast<T*>(r.g.dx) + at, zero);
             my.give(static_cast<T*>(r.g.df) + at, zero);
             my.give(static_cast<T*>(r.g.dg) + at, zero);
@@ -73,25 +76,32 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
         Bit<T, V> xr[P], fr[P], gr[P], zr[P], dr[P];
         Bit<float, V> sr;
         const auto fetch = [&](int block) {
-            const int l0 = block + w * P;
+            const int first = block + w * kRows;
             if (!ENDS) take_bit<float, V>(sr, r.saved + (static_cast<int64_t>(b) * ((in.N + kRecurSave - 1) / kRecurSave) + block / kRecurSave) * in.D, 4u * my.c);
-            take_rows<T, V, P>(fr, in.f, b, l0, len, bytes);
-            take_rows<T, V, P>(dr, r.dout, b, l0, len, bytes);
-            if (GATED) take_rows<T, V, P>(zr, in.z, b, l0, len, bytes);
+            take_rows<T, V, P, SUB>(fr, in.f, b, first, len, set, bytes);
+            take_rows<T, V, P, SUB>(dr, r.dout, b, first, len, set, bytes);
+            if (GATED) take_rows<T, V, P, SUB>(zr, in.z, b, first, len, set, bytes);
             if (!ENDS) {
-                take_rows<T, V, P>(gr, in.g, b, l0, len, bytes);
-                take_rows<T, V, P>(xr, in.x, b, l0, len, bytes);
+                take_rows<T, V, P, SUB>(gr, in.g, b, first, len, set, bytes);
+                take_rows<T, V, P, SUB>(xr, in.x, b, first, len, set, bytes);
             }
         };
-        int block = begin + (end - begin - 1) / (P * W) * (P * W), buffer = 0;
-        fetch(block);
-        for (; block >= begin; block -= P * W) {
-            const int l0 = block + w * P;
+        int buffer = 0;
+        const auto leave = [&](int to) {
+            if (front) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) behinds[to][j][cl] = c[j];
+            }
+        };
+        leave(0);
+        const auto run = [&](auto whole, int block) {  // whole: all positions lie before the end, all lanes have channels of their own
+            constexpr bool WHOLE = decltype(whole)::value;
+            const int first = block + w * kRows, l0 = first + set;
             float a[P][V], m[P][V], rest[P][V], open[P][V], in_gate[P][V], x[P][V], dy[P][V], h[V];
             Bit<T, V> z[P], dout[P];
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                const bool on = l0 + i < end;
+                const bool on = WHOLE || l0 + i < end;
                 float f[V], g[V], zi[V], di[V];
                 fr[i].get(f);
                 dr[i].get(di);
@@ -113,7 +123,7 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
                         open[i][j] = d.open;
                         rest[i][j] = d.rest;
                         m[i][j] = __builtin_amdgcn_sqrtf(d.rest);
-                        in_gate[i][j] = sigmoid(g[j] + ch[j].g_bias);
+                        in_gate[i][j] = open_gate(g[j], ch[j].g_bias);
                         x[i][j] = on ? x[i][j] : 0.0f;
                     }
                 }
@@ -124,39 +134,68 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) h[j] = s[j];
             }
-            fetch(block > begin ? block - P * W : begin);
-            const auto put = [&](int i, int j) { return l0 + i < end ? m[i][j] * in_gate[i][j] * x[i][j] : 0.0f; };
+            fetch(block > begin ? block - kBlock : begin);
+            const auto put = [&](int i, int j) { return WHOLE || l0 + i < end ? m[i][j] * in_gate[i][j] * x[i][j] : 0.0f; };
+            float before_a[V], before_e[V], behind_a[V], behind_g[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 float G = 0.0f, E = 0.0f;
 #pragma unroll
                 for (int i = P - 1; i >= 0; --i) G = a[i][j] * (dy[i][j] + G);
+                const float A = product_of(a, j);
+                if (ENDS) total[j] = product(total[j], A);
+                behind_a[j] = A;
+                behind_g[j] = G;
+                before_set<SUB, true>(behind_a[j], behind_g[j], sub);
                 if (!ENDS) {
 #pragma unroll
                     for (int i = 0; i < P; ++i) E = fmaf(a[i][j], E, put(i, j));
+                    before_a[j] = A;
+                    before_e[j] = E;
+                    before_set<SUB, false>(before_a[j], before_e[j], sub);
                 }
-                made[buffer][w][j][lane] = Four{product_of(a, j), E, G, 0.0f};
+                // a wave's: the last set's way forwards, the first one's backwards
+                if (SUB == 1) {
+                    made[buffer][w][j][cl] = Three{A, E, G, 0.0f};
+                } else {
+                    if (sub == 0) {
+                        made[buffer][w][j][cl][0] = product(A, behind_a[j]);
+                        made[buffer][w][j][cl][2] = fmaf(A, behind_g[j], G);
+                    }
+                    if (!ENDS && sub == SUB - 1) made[buffer][w][j][cl][1] = fmaf(A, before_e[j], E);
+                }
             }
             lds_sync();
-            float c[V];  // the gradient behind this wave's positions
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                Four all[W];
+                Three all[W];
+                c[j] = behinds[buffer][j][cl];
 #pragma unroll
-                for (int k = 0; k < W; ++k) all[k] = made[buffer][k][j][lane];
+                for (int k = 0; k < W; ++k) all[k] = made[buffer][k][j][cl];
 #pragma unroll
-                for (int k = W - 1; k >= 0; --k) {
-                    c[j] = k == w ? behind[j] : c[j];
-                    behind[j] = fmaf(all[k][0], behind[j], all[k][2]);
-                    if (ENDS) total[j] = product(total[j], all[k][0]);
+                for (int k = W - 1; k > 0; --k) {
+                    if (k == w) break;
+                    c[j] = fmaf(all[k][0], c[j], all[k][2]);
                 }
+                if (SUB > 1) c[j] = fmaf(behind_a[j], c[j], behind_g[j]);
                 if (!ENDS) {
 #pragma unroll
-                    for (int k = 0; k < W - 1; ++k) h[j] = k < w ? fmaf(all[k][0], h[j], all[k][1]) : h[j];
+                    for (int k = 0; k < W - 1; ++k) {
+                        if (k == w) break;
+                        h[j] = fmaf(all[k][0], h[j], all[k][1]);
+                    }
+                    if (SUB > 1) h[j] = fmaf(before_a[j], h[j], before_e[j]);
                 }
             }
             buffer ^= 1;
-            if constexpr (!ENDS) {
+            if constexpr (ENDS) {
+                if (w == 0) {
+#pragma unroll
+                    for (int i = P - 1; i >= 0; --i)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) c[j] = a[i][j] * (dy[i][j] + c[j]);
+                }
+            } else {
                 float before[P][V];
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
@@ -166,14 +205,16 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
                         h[j] = fmaf(a[i][j], h[j], put(i, j));
                     }
                 }
+                const unsigned at = SUB > 1 ? static_cast<unsigned>(set) * static_cast<unsigned>(in.D) : 0u;
 #pragma unroll
                 for (int i = P - 1; i >= 0; --i) {
                     float dx[V], df[V], dg[V], dz[V], zi[V], di[V];
+                    const bool on = WHOLE || l0 + i < end;
                     dout[i].get(di);
                     if (GATED) z[i].get(zi);
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        const float dh = dy[i][j] + c[j], u = ch[j].c * open[i][j], ai = a[i][j], gate_in = in_gate[i][j];
+                        const float dh = dy[i][j] + c[j], u = kLn2f * (ch[j].c * open[i][j]), ai = a[i][j], gate_in = in_gate[i][j];
                         // u / m: 0 where 1 - a^2 is (or is too small for its root)
                         const float ratio = rest[i][j] < 1.17549435e-38f ? 0.0f : u * __builtin_amdgcn_rsqf(rest[i][j]);
                         dx[j] = dh * m[i][j] * gate_in;
@@ -185,47 +226,72 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
                             dz[j] = di[j] * fmaf(ai, before[i][j], put(i, j)) * gate * fmaf(zi[j], 1.0f - gate, 1.0f);
                         }
                         c[j] = ai * dh;
-                        const bool on = l0 + i < end;
                         s_log[j] += on ? dlog : 0.0f;
                         s_f[j] += on ? df[j] : 0.0f;
                         s_g[j] += on ? dg[j] : 0.0f;
                     }
-                    if (l0 + i < end) {
-                        const int64_t at = (first + l0 + i) * in.D;
-                        my.give(static_cast<T*>(r.g.dx) + at, dx);
-                        my.give(static_cast<T*>(r.g.df) + at, df);
-                        my.give(static_cast<T*>(r.g.dg) + at, dg);
-                        if (GATED) my.give(static_cast<T*>(r.g.dz) + at, dz);
+                    if (on) {
+                        const int64_t row = (first_row + first + i) * in.D;
+                        my.template give<WHOLE>(static_cast<T*>(r.g.dx) + row, dx, at);
+                        my.template give<WHOLE>(static_cast<T*>(r.g.df) + row, df, at);
+                        my.template give<WHOLE>(static_cast<T*>(r.g.dg) + row, dg, at);
+                        if (GATED) my.template give<WHOLE>(static_cast<T*>(r.g.dz) + row, dz, at);
                     }
                 }
             }
-        }
+            leave(buffer);
+        };
+        int block = begin + (end - begin - 1) / kBlock * kBlock;
+        fetch(block);
+        for (; block >= begin && !(my.full && block + kBlock <= end); block -= kBlock) run(std::false_type{}, block);
+        for (; block >= begin; block -= kBlock) run(std::true_type{}, block);
     }
     if constexpr (ENDS) {
-        if (w) return;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int d = L; d < 64; d *= 2) total[j] = product(total[j], __shfl_xor(total[j], d));
+        lds_sync();
+        if (sub == 0) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) made[0][w][j][cl][0] = total[j];
+        }
+        lds_sync();
+        if (!front) return;
         Pair e;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            e[2 * j] = total[j];
-            e[2 * j + 1] = behind[j];
+            float all = 1.0f;
+#pragma unroll
+            for (int k = 0; k < W; ++k) all = product(all, made[0][k][j][cl][0]);
+            e[2 * j] = all;
+            e[2 * j + 1] = c[j];
         }
         *reinterpret_cast<AnyPair*>(r.ends + ((static_cast<int64_t>(b) * r.plan.segments + seg) * in.D + my.c) * 2) = e;
     } else {
-        if (w == 0 && seg == 0 && r.g.dstate) my.give(r.g.dstate + static_cast<int64_t>(b) * in.D, behind);
+        if (front && seg == 0 && r.g.dstate) my.give(r.g.dstate + static_cast<int64_t>(b) * in.D, c);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            sums[w][0][j][lane] = s_log[j];
-            sums[w][1][j][lane] = s_f[j];
-            sums[w][2][j][lane] = s_g[j];
+#pragma unroll
+            for (int d = L; d < 64; d *= 2) {
+                s_log[j] += __shfl_xor(s_log[j], d);
+                s_f[j] += __shfl_xor(s_f[j], d);
+                s_g[j] += __shfl_xor(s_g[j], d);
+            }
+            if (sub == 0) {
+                sums[w][0][j][cl] = s_log[j];
+                sums[w][1][j][cl] = s_f[j];
+                sums[w][2][j][cl] = s_g[j];
+            }
         }
         lds_sync();
-        if (w >= 3) return;
+        if (w >= 3 || sub) return;
         float s[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            s[j] = sums[0][w][j][lane];
+            s[j] = sums[0][w][j][cl];
 #pragma unroll
-            for (int k = 1; k < W; ++k) s[j] += sums[k][w][j][lane];
+            for (int k = 1; k < W; ++k) s[j] += sums[k][w][j][cl];
         }
         my.give(r.partial + ((static_cast<int64_t>(b) * r.plan.segments + seg) * 3 + w) * in.D, s);
     }
@@ -253,34 +319,39 @@ __global__ __launch_bounds__(1024) void recur_sums_kernel(const float* __restric
     to[ch] = sum;
 }
 
-int channels_a_lane(int D) { return D == 1 ? 1 : 2; }
+constexpr int P = 2, W = 4;  // a lane's positions, a workgroup's waves: 142 registers, three waves a SIMD (four positions: 203, two; the whole training step of
+                             // B=128 N=256 D=1024, bfloat16, ragged, 198 us / 227)
+static_assert(P * W % kRecurSave == 0, "a block begins where a state is saved");
 
-RecurPlan grad_plan(int B, int N, int D) {
-    RecurPlan p;
-    p.tiles = (D - 1) / (64 * channels_a_lane(D)) + 1;
-    const int64_t groups = static_cast<int64_t>(B) * p.tiles, most = (static_cast<int64_t>(N) + 255) / 256;
-    int64_t segments = groups <= 128 ? 256 / groups : 1;
-    if (segments > most) segments = most;
-    p.seg_len = static_cast<int>(((N + segments - 1) / segments + kRecurBlock - 1) / kRecurBlock * kRecurBlock);
-    p.segments = static_cast<int>((static_cast<int64_t>(N) + p.seg_len - 1) / p.seg_len);
-    return p;
-}
+// Measured, us, forward and gradient, wide tiles / narrow / segments (B x N x D, bfloat16): 128x256x1024 ragged 203 / 218 / 258, 64x1024x514 353 / 308 / 277, 16x1000x1024
+// 246 / 173 / 165, 100x200x128 63 / 48 / 59, 30x300x300 102 / 68 / 68, 8x256x1024 72 / 46 / 51, 4x5000x1024 1176 / 646 / 419 (in all of them the
+// forward pass by wide tiles).
+RecurPlan grad_plan(int B, int N, int D) { return recur_plan_of(B, N, D, 768, 1 << 30, 512); }
 
-template <typename T, int V>
+template <typename T, int V, int SUB>
 hipError_t grad_of(const GradRun& r, hipStream_t st) {
-    const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(r.in.B) * r.plan.segments * r.plan.tiles);
+    const unsigned blocks = static_cast<unsigned>(recur_blocks(r.plan, r.in.B));
     const bool gated = r.in.z.data != nullptr;
-    if (r.plan.segments > 1) {
-        const auto ends = gated ? recur_grad_kernel<T, V, true, true> : recur_grad_kernel<T, V, false, true>;
-        ends<<<blocks, 64 * W, 0, st>>>(r);
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if constexpr (SUB == 1) {
+        if (r.plan.segments > 1) {
+            const auto ends = gated ? recur_grad_kernel<T, V, P, W, SUB, true, true> : recur_grad_kernel<T, V, P, W, SUB, false, true>;
+            ends<<<blocks, 64 * W, 0, st>>>(r);
+            if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        }
     }
-    const auto kernel = gated ? recur_grad_kernel<T, V, true, false> : recur_grad_kernel<T, V, false, false>;
+    const auto kernel = gated ? recur_grad_kernel<T, V, P, W, SUB, true, false> : recur_grad_kernel<T, V, P, W, SUB, false, false>;
     kernel<<<blocks, 64 * W, 0, st>>>(r);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     recur_sums_kernel<<<dim3(pieces_of_row(r.in.D, 64), 3), 1024, 0, st>>>(r.partial, static_cast<int64_t>(r.in.B) * r.plan.segments, r.in.D, r.in.decay, r.g.ddecay,
                                                                              r.g.df_bias, r.g.dg_bias);
     return hipGetLastError();
+}
+template <typename T, int V>
+hipError_t grad_by(const GradRun& r, hipStream_t st) {
+    if constexpr (V > 1) {
+        if (r.plan.sets > 1) return grad_of<T, V, 4>(r, st);
+    }
+    return grad_of<T, V, 1>(r, st);
 }
 
 size_t partial_bytes(int B, int segments, int D) { return up256(static_cast<size_t>(B) * segments * 3 * D * 4); }
@@ -296,7 +367,8 @@ size_t recur_grad_workspace(int B, int N, int D, bool with_saved) {
 
 hipError_t launch_recur_grad(int dtype, AnyRows dout, const RecurIn& in, const float* state, const float* saved, const RecurGrads& g, void* ws, hipStream_t st) {
     GradRun r{in, dout, g, saved, nullptr, static_cast<float*>(ws), grad_plan(in.B, in.N, in.D)};
-    if (!fits(static_cast<int64_t>(in.B) * r.plan.segments * r.plan.tiles, 64 * W)) return hipErrorInvalidValue;
+    if (!near_rows(in.x) || !near_rows(in.f) || !near_rows(in.g) || !near_rows(in.z) || !near_rows(dout)) widen_tiles(r.plan, in.D);
+    if (!fits(recur_blocks(r.plan, in.B), 64 * W)) return hipErrorInvalidValue;
     char* more = static_cast<char*>(ws) + partial_bytes(in.B, r.plan.segments, in.D);
     if (r.plan.segments > 1) {
         r.ends = reinterpret_cast<float*>(more);
@@ -307,8 +379,8 @@ hipError_t launch_recur_grad(int dtype, AnyRows dout, const RecurIn& in, const f
         if (const hipError_t e = launch_recur(dtype, in, state, nullptr, nullptr, reinterpret_cast<float*>(more), more + recur_saved_bytes(in.B, in.N, in.D), st); e != hipSuccess)
             return e;
     }
-    if (in.D == 1) return dtype ? grad_of<uint16_t, 1>(r, st) : grad_of<float, 1>(r, st);
-    return dtype ? grad_of<uint16_t, 2>(r, st) : grad_of<float, 2>(r, st);
+    if (in.D == 1) return dtype ? grad_by<uint16_t, 1>(r, st) : grad_by<float, 1>(r, st);
+    return dtype ? grad_by<uint16_t, 2>(r, st) : grad_by<float, 2>(r, st);
 }
 
 }  // namespace enc
