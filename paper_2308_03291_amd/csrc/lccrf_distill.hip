@@ -14,16 +14,8 @@ namespace {
 constexpr int kEntries = 4;  // of a lane, at most: LCCRF_MAX_TOP over 64
 constexpr float kLeast = -3.402823466e38f;
 
-template <int L> __device__ __forceinline__ float team_max(float v) {
-#pragma unroll
-    for (int k = 1; k < L; k *= 2) v = __builtin_elementwise_maximum(v, __shfl_xor(v, k));
-    return v;
-}
-template <int L> __device__ __forceinline__ float team_sum(float v) {
-#pragma unroll
-    for (int k = 1; k < L; k *= 2) v += __shfl_xor(v, k);
-    return v;
-}
+template <int L> __device__ __forceinline__ float team_max(float v) { return max_across(v, L); }
+template <int L> __device__ __forceinline__ float team_sum(float v) { return sum_across(v, L); }
 
 // The teacher's entries of a position, entry t + e L with lane t of its team.
 template <typename T, int L, int E> struct Entries {

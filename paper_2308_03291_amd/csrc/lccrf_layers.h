@@ -64,5 +64,32 @@ __device__ __forceinline__ void lds_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Over `team` neighbouring lanes, a power of two up to 64, the same in all of them: f of a lane's and the other half's, from neighbours on.  In registers
+// throughout: permutations of four lanes, mirrored halves and rows of sixteen, swapped rows and halves.
+template <int CTRL> __device__ __forceinline__ float moved(float x) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+template <typename F> __device__ __forceinline__ float across(float v, int team, F f) {
+    if (team > 1) v = f(v, moved<0xB1>(v));
+    if (team > 2) v = f(v, moved<0x4E>(v));
+    if (team > 4) v = f(v, moved<0x141>(v));
+    if (team > 8) v = f(v, moved<0x140>(v));
+    if (team > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (team > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return v;
+}
+__device__ __forceinline__ float sum_across(float v, int team) {
+    return across(v, team, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float max_across(float v, int team) {
+    return across(v, team, [](float a, float b) { return __builtin_elementwise_maximum(a, b); });
+}
+
 }  // namespace enc
 }  // namespace lccrf

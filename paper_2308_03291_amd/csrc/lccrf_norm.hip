@@ -8,6 +8,9 @@
 // always in the same order: no difference of large numbers, however far the mean is from 0.
 #include "lccrf_layers.h"
 
+#ifndef AW
+#define AW 1024
+#endif
 namespace lccrf {
 namespace enc {
 namespace {
@@ -56,12 +59,8 @@ struct Alone {
     int64_t blocks;                // workgroups a tile
 };
 
-__device__ __forceinline__ float team_sum(float v, int team) {
-    for (int k = 1; k < team; k *= 2) v += __shfl_xor(v, k);
-    return v;
-}
-
-template <typename T, int W, int R, bool GRAD>
+// EXACT: every lane has R pieces of its own, no channel twice.
+template <typename T, int W, int R, bool GRAD, bool EXACT>
 __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alone p, const float* __restrict__ given, T* __restrict__ out, float* __restrict__ stats,
                                                     float* __restrict__ partial) {
     __shared__ float sums[GRAD ? 4 * 64 * 2 * W : 1];
@@ -84,30 +83,48 @@ __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alo
             if (GRAD) dw[r][j] = db[r][j] = 0.0f;
     }
     const float count = 1.0f / C;
-    for (int64_t base = (block * 4 + wave) * rows; base < total; base += p.blocks * 4 * rows) {
-        const int64_t pos = base + team / p.groups;
-        const bool there = pos < total;
-        const unsigned at = there ? static_cast<unsigned>(pos) : 0u;
-        const int b = at / static_cast<unsigned>(in.N), l = at - b * in.N;
-        const bool inside = there && is && l < length_at(in.lengths, b, in.N);
+    // Three positions are under way: one's length is being read, the next one's values, and the third is worked on.
+    struct Position {
+        int b, l, len;
+        bool there;
+    };
+    const int64_t high = p.blocks * 4 * rows, first = (block * 4 + wave) * rows + team / p.groups;
+    const auto position = [&](int64_t pos) {
+        Position q;
+        q.there = pos < total;
+        const unsigned at = q.there ? static_cast<unsigned>(pos) : 0u;
+        q.b = at / static_cast<unsigned>(in.N);
+        q.l = at - q.b * in.N;
+        q.len = length_at(in.lengths, q.b, in.N);
+        return q;
+    };
+    Part<T, W> v[R], d[GRAD ? R : 1];
+    const auto fetch = [&](const Position& q) {
+        if (q.there && is && q.l < q.len) {
+            const T *px = line<T>(in.x, q.b, q.l), *pd = GRAD ? line<T>(dout, q.b, q.l) : nullptr;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (EXACT || skip[r] < W) {
+                    v[r].load(px + c[r], W);
+                    if (GRAD) d[r].load(pd + c[r], W);
+                }
+        }
+    };
+    Position now = position(first), next = position(first + high);
+    fetch(now);
+    for (int64_t pos = first; pos - team / p.groups < total; pos += high) {
+        const Position after = position(pos + 2 * high);
+        const int b = now.b, l = now.l;
+        const bool there = now.there, inside = there && is && l < now.len;
         float x[R][W], dy[GRAD ? R : 1][W];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            Part<T, W> v, d;
-            const bool read = inside && skip[r] < W;
-            if (read) {
-                v.load(line<T>(in.x, b, l) + c[r], W);
-                if (GRAD) d.load(line<T>(dout, b, l) + c[r], W);
-                v.get(x[r]);
-                if (GRAD) d.get(dy[r]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    x[r][j] = 0.0f;
-                    if (GRAD) dy[r][j] = 0.0f;
-                }
-            }
+            v[r].get(x[r]);
+            if (GRAD) d[r].get(dy[r]);
         }
+        fetch(next);
+        now = next;
+        next = after;
         const int64_t unit = (static_cast<int64_t>(b) * in.N + l) * in.G + g;
         float mean = 0.0f, rstd = 0.0f;
         if (GRAD && given) {
@@ -120,17 +137,18 @@ __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alo
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int j = 0; j < W; ++j) s += j >= skip[r] ? x[r][j] : 0.0f;
-            mean = team_sum(s, p.team) * count;
+                for (int j = 0; j < W; ++j) s += EXACT || j >= skip[r] ? x[r][j] : 0.0f;
+            mean = sum_across(s, p.team) * count;
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
-                    const float d = x[r][j] - mean;
-                    m2 += j >= skip[r] ? d * d : 0.0f;
+                    const float away = x[r][j] - mean;
+                    m2 = EXACT || j >= skip[r] ? fmaf(away, away, m2) : m2;
                 }
-            rstd = __builtin_amdgcn_rsqf(fmaf(team_sum(m2, p.team), count, in.eps));
+            rstd = __builtin_amdgcn_rsqf(fmaf(sum_across(m2, p.team), count, in.eps));
         }
+        T* to = out + (static_cast<int64_t>(b) * in.N + l) * in.D;
         if constexpr (!GRAD) {
             if (stats && there && is && t == 0) {
                 stats[2 * unit] = inside ? mean : 0.0f;
@@ -141,35 +159,48 @@ __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alo
                 float o[W];
 #pragma unroll
                 for (int j = 0; j < W; ++j) {
-                    const float y = fmaf((x[r][j] - mean) * rstd, w[r][j], bias[r][j]);
-                    o[j] = inside ? in.silu ? silu(y) : y : 0.0f;
+                    const float y = fmaf(x[r][j] - mean, rstd * w[r][j], bias[r][j]);
+                    o[j] = in.silu ? silu(y) : y;
                 }
-                if (there && skip[r] < W) Part<T, W>::put(out + (static_cast<int64_t>(b) * in.N + l) * in.D + c[r], W, o);
+                if (!inside) {
+#pragma unroll
+                    for (int j = 0; j < W; ++j) o[j] = 0.0f;
+                }
+                if (there && is && (EXACT || skip[r] < W)) Part<T, W>::put(to + c[r], W, o);
             }
         } else {
             float s1 = 0.0f, s2 = 0.0f;
+            if (inside) {  // (a team's lanes together)
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+                for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    const float hat = (x[r][j] - mean) * rstd;
-                    x[r][j] = hat;
-                    if (in.silu) dy[r][j] *= dsilu(fmaf(hat, w[r][j], bias[r][j]));
-                    const bool counts = inside && j >= skip[r];
-                    dw[r][j] += counts ? dy[r][j] * hat : 0.0f;
-                    db[r][j] += counts ? dy[r][j] : 0.0f;
-                    dy[r][j] *= w[r][j];
-                    s1 += counts ? dy[r][j] : 0.0f;
-                    s2 += counts ? dy[r][j] * hat : 0.0f;
-                }
-            s1 = team_sum(s1, p.team) * count;
-            s2 = team_sum(s2, p.team) * count;
+                    for (int j = 0; j < W; ++j) {
+                        const float hat = (x[r][j] - mean) * rstd;
+                        x[r][j] = hat;
+                        if (in.silu) dy[r][j] *= dsilu(fmaf(hat, w[r][j], bias[r][j]));
+                        if (EXACT || j >= skip[r]) {
+                            dw[r][j] = fmaf(dy[r][j], hat, dw[r][j]);
+                            db[r][j] += dy[r][j];
+                        }
+                        dy[r][j] *= w[r][j];
+                        if (EXACT || j >= skip[r]) {
+                            s1 += dy[r][j];
+                            s2 = fmaf(dy[r][j], hat, s2);
+                        }
+                    }
+            }
+            s1 = sum_across(s1, p.team) * count;
+            s2 = sum_across(s2, p.team) * count;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float o[W];
 #pragma unroll
-                for (int j = 0; j < W; ++j) o[j] = inside ? rstd * (dy[r][j] - fmaf(x[r][j], s2, s1)) : 0.0f;
-                if (there && skip[r] < W) Part<T, W>::put(out + (static_cast<int64_t>(b) * in.N + l) * in.D + c[r], W, o);
+                for (int j = 0; j < W; ++j) o[j] = rstd * (dy[r][j] - fmaf(x[r][j], s2, s1));
+                if (!inside) {
+#pragma unroll
+                    for (int j = 0; j < W; ++j) o[j] = 0.0f;
+                }
+                if (there && is && (EXACT || skip[r] < W)) Part<T, W>::put(to + c[r], W, o);
             }
         }
     }
@@ -284,233 +315,531 @@ __global__ __launch_bounds__(256) void wide_kernel(NormIn in, AnyRows dout, int 
     }
 }
 
-// ---- whole sequences ------------------------------------------------------------------------------------------
-// Workgroups are lx pieces wide and ly = 256 / lx positions high and go over a chunk of a sequence's positions.
-struct Span {
-    int ppg, pieces, lx, tiles;  // pieces a group and a row, across a workgroup, such tiles
-    int chunk, chunks;           // positions a workgroup, workgroups a sequence
+// ---- whole sequences in registers ------------------------------------------------------------------------------
+// Where a sequence's groups fit a workgroup's registers, they are read once: a workgroup has whole groups, `lx` pieces (a power of two) wide, of all positions, R
+// pieces a thread.
+struct Held {
+    int ppg, lx, groups, tiles, threads, pieces;  // pieces a group; across a workgroup; groups a workgroup, such tiles; its threads, pieces each
 };
-struct SpanPlace { int b, chunk, piece, ty, ly; };
-__device__ __forceinline__ SpanPlace span_place(const Span& p) {
-    const unsigned rest = blockIdx.x / p.tiles, tile = blockIdx.x - rest * p.tiles, b = rest / p.chunks;
-    const int tx = threadIdx.x % p.lx;
-    return {static_cast<int>(b), static_cast<int>(rest - b * p.chunks), static_cast<int>(tile) * p.lx + tx, static_cast<int>(threadIdx.x) / p.lx, 256 / p.lx};
+
+// The sum of v over a group's pieces and all positions, for every thread of the group: first over the workgroup's positions, then over the pieces.
+// lds: a float a thread, and lx.
+__device__ __forceinline__ float held_sum(float v, const Held& p, float* lds, int tx, int group) {
+    for (int k = p.lx; k < 64; k *= 2) v += __shfl_xor(v, k);
+    const int wide = p.lx < 64 ? p.lx : 64, lane = threadIdx.x & 63, entries = (blockDim.x >> 6) * wide;
+    __syncthreads();
+    if (lane < wide) lds[(threadIdx.x >> 6) * wide + lane] = v;
+    __syncthreads();
+    float* columns = lds + blockDim.x;
+    if (static_cast<int>(threadIdx.x) < p.lx) {
+        float s = 0.0f;
+        for (int e = threadIdx.x; e < entries; e += p.lx) s += lds[e];
+        columns[threadIdx.x] = s;
+    }
+    __syncthreads();
+    float s = 0.0f;
+    if (group < p.groups)
+        for (int k = 0; k < p.ppg; ++k) s += columns[group * p.ppg + k];
+    return s;
 }
 
-// Moments of every piece over a chunk: [B][chunks][pieces][2] (mean, M; the count follows from the lengths).
+template <typename T, int W, int R, bool GRAD>
+__global__ __launch_bounds__(1024) void held_kernel(NormIn in, AnyRows dout, Held p, const float* __restrict__ given, T* __restrict__ out, float* __restrict__ stats,
+                                                                  float* __restrict__ partial) {
+    extern __shared__ float lds[];  // held_sum's; GRAD: [threads][W]
+    const int tx = threadIdx.x & (p.lx - 1), ty = threadIdx.x / p.lx, ly = blockDim.x / p.lx, C = in.D / in.G;
+    const int b = blockIdx.x / p.tiles, tile = blockIdx.x - b * p.tiles, group = tx / p.ppg, g = tile * p.groups + group;
+    const bool is = group < p.groups && g < in.G;
+    const Place at = Place::of<W>(is ? g * p.ppg + tx - group * p.ppg : 0, p.ppg, C);
+    const int len = length_at(in.lengths, b, in.N);
+    Part<T, W> raw[R], draw[GRAD ? R : 1];
+    const T* px = line<T>(in.x, b, 0) + at.c;
+    const T* pd = GRAD ? line<T>(dout, b, 0) + at.c : nullptr;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int l = ty + r * ly;
+        if (is && l < len) {
+            raw[r].load(px + l * in.x.row, W);
+            if (GRAD) draw[r].load(pd + l * dout.row, W);
+        }
+    }
+    const float share = 1.0f / (static_cast<float>(len) * C);  // (len 0: nothing looks at it)
+    const int64_t unit = static_cast<int64_t>(b) * in.G + g;
+    float mean, rstd;
+    if (GRAD && given) {
+        mean = is ? given[2 * unit] : 0.0f;
+        rstd = is ? given[2 * unit + 1] : 0.0f;
+    } else {
+        float s = 0.0f, q = 0.0f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float x[W];
+            raw[r].get(x);
+#pragma unroll
+            for (int j = 0; j < W; ++j) s += is && ty + r * ly < len && j >= at.skip ? x[j] : 0.0f;
+        }
+        mean = held_sum(s, p, lds, tx, group) * share;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float x[W];
+            raw[r].get(x);
+#pragma unroll
+            for (int j = 0; j < W; ++j) q += is && ty + r * ly < len && j >= at.skip ? (x[j] - mean) * (x[j] - mean) : 0.0f;
+        }
+        rstd = __builtin_amdgcn_rsqf(fmaf(held_sum(q, p, lds, tx, group), share, in.eps));
+        if (!GRAD && stats && is && ty == 0 && tx == group * p.ppg) {
+            stats[2 * unit] = len > 0 ? mean : 0.0f;
+            stats[2 * unit + 1] = len > 0 ? rstd : 0.0f;
+        }
+    }
+    T* o = out + static_cast<int64_t>(b) * in.N * in.D + at.c;
+    float w[W], bias[W];
+    int c = at.c;
+    asm volatile("" : "+v"(c));  // fetched here and not in front of the sums, where they would take registers that hold values
+    weights_of<W>(in, c, w, bias);
+    if constexpr (!GRAD) {
+        if (!is) return;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int l = ty + r * ly;
+            float x[W];
+            raw[r].get(x);
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                const float y = fmaf((x[j] - mean) * rstd, w[j], bias[j]);
+                x[j] = l < len ? in.silu ? silu(y) : y : 0.0f;
+            }
+            if (l < in.N) Part<T, W>::put(o + static_cast<int64_t>(l) * in.D, W, x);
+        }
+    } else {
+        float dy[R][W], sums[2][W] = {};  // of dy hat, of dy
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool on = is && ty + r * ly < len;
+            float x[W];
+            raw[r].get(x);
+            draw[r].get(dy[r]);
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                const float hat = (x[j] - mean) * rstd;
+                if (in.silu) dy[r][j] *= dsilu(fmaf(hat, w[j], bias[j]));
+                sums[0][j] += on ? dy[r][j] * hat : 0.0f;
+                sums[1][j] += on ? dy[r][j] : 0.0f;
+            }
+        }
+        // over the positions, channel by channel; the first lx threads have them, write them and weigh them for the group
+        const int wide = p.lx < 64 ? p.lx : 64, lane = threadIdx.x & 63, entries = (blockDim.x >> 6) * wide;
+        float of_group[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                for (int d = p.lx; d < 64; d *= 2) sums[k][j] += __shfl_xor(sums[k][j], d);
+            __syncthreads();
+            if (lane < wide) {
+#pragma unroll
+                for (int j = 0; j < W; ++j) lds[j * entries + (threadIdx.x >> 6) * wide + lane] = sums[k][j];
+            }
+            __syncthreads();
+            if (static_cast<int>(threadIdx.x) < p.lx) {
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    float s = 0.0f;
+                    for (int e = threadIdx.x; e < entries; e += p.lx) s += lds[j * entries + e];
+                    of_group[k] += j >= at.skip ? w[j] * s : 0.0f;
+                    if (partial && is && j >= at.skip) partial[(static_cast<int64_t>(b) * 2 + k) * in.D + at.c + j] = s;
+                }
+            }
+        }
+        __syncthreads();
+        if (static_cast<int>(threadIdx.x) < p.lx) {
+            lds[threadIdx.x] = of_group[0];
+            lds[p.lx + threadIdx.x] = of_group[1];
+        }
+        __syncthreads();
+        if (!is) return;
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int k = 0; k < p.ppg; ++k) {
+            s2 += lds[group * p.ppg + k];
+            s1 += lds[p.lx + group * p.ppg + k];
+        }
+        s1 *= share;
+        s2 *= share;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int l = ty + r * ly;
+            float x[W];
+            raw[r].get(x);
+#pragma unroll
+            for (int j = 0; j < W; ++j) x[j] = l < len ? rstd * (dy[r][j] * w[j] - fmaf((x[j] - mean) * rstd, s2, s1)) : 0.0f;
+            if (l < in.N) Part<T, W>::put(o + static_cast<int64_t>(l) * in.D, W, x);
+        }
+    }
+}
+
+// ---- whole sequences ------------------------------------------------------------------------------------------
+// Two passes: sums of every chunk of positions, then the results; the second finds most of what it reads in the memory-side cache.  Workgroups are lx pieces wide
+// (whole groups, or one of the `parts` of a group that is wider), ly = 256 / lx positions high and go over a chunk of a sequence's positions.  What a group's
+// chunks come to is joined by every workgroup of the second pass for its own groups, all in the same order: no launch between the two.
+struct Span {
+    int ppg, lx, groups, parts, tiles;  // pieces a group; across a workgroup; groups a workgroup or workgroups a group; tiles a row
+    int chunk, chunks;                  // positions a workgroup, workgroups a sequence
+};
+struct SpanPlace {
+    int b, chunk, part, first;  // first group
+    int tx, ty, ly, local, k;   // this thread's group (of the workgroup's) and piece of it
+    bool is;
+};
+__device__ __forceinline__ SpanPlace span_place(const Span& p, const NormIn& in, unsigned block) {
+    SpanPlace m;
+    const unsigned rest = block / p.tiles, tile = block - rest * p.tiles;
+    m.b = rest / p.chunks;
+    m.chunk = rest - m.b * p.chunks;
+    m.part = p.parts > 1 ? tile % p.parts : 0;
+    m.first = p.parts > 1 ? tile / p.parts : tile * p.groups;
+    m.tx = threadIdx.x % p.lx;
+    m.ty = threadIdx.x / p.lx;
+    m.ly = 256 / p.lx;
+    m.local = p.parts > 1 ? 0 : m.tx / p.ppg;
+    m.k = p.parts > 1 ? m.part * p.lx + m.tx : m.tx - m.local * p.ppg;
+    m.is = m.local < p.groups && m.first + m.local < in.G && m.k < p.ppg;
+    return m;
+}
+// Values of a group's part at one position.
+template <int W> __device__ __forceinline__ int part_width(const Span& p, int part, int C) {
+    const int from = part * p.lx * W, to = from + p.lx * W;
+    return p.parts == 1 ? C : (to < C ? to : C) - from;
+}
+
+// What has gone into lds[0 .. lx) is joined group by group: the first of a group's threads has it (threads of the first row of positions call with `mine`).
+template <typename V, typename F> __device__ __forceinline__ void join_groups(V* lds, V& mine, const Span& p, const SpanPlace& my, F joined) {
+    const int in_group = p.parts > 1 ? my.tx : my.k, size = p.parts > 1 ? p.lx : p.ppg;
+    int k = 1;
+    while (k < size) k *= 2;
+    for (k /= 2; k >= 1; k /= 2) {
+        __syncthreads();
+        if (my.ty == 0 && my.local < p.groups && in_group < k && in_group + k < size) lds[my.tx] = mine = joined(mine, lds[my.tx + k]);
+    }
+}
+
+// Joins the entries of the workgroup's groups, `threads` of them side by side: of(local group, entry) in ascending entries for each thread, then halves.  The results stand in
+// lds[group * per], per threads a group.
+template <typename V, typename Of, typename F> __device__ __forceinline__ int join_entries(V* lds, const Span& p, int first, int G, int64_t entries, const V& none, Of of, F joined) {
+    int many = 1;
+    while (many < p.groups) many *= 2;
+    const int per = 256 / many, g = threadIdx.x / per, t = threadIdx.x - g * per;
+    V v = none;
+    if (g < p.groups && first + g < G)
+        for (int64_t e = t; e < entries; e += per) v = joined(v, of(g, e));
+    lds[threadIdx.x] = v;
+    for (int k = per / 2; k >= 1; k /= 2) {
+        __syncthreads();
+        if (t < k) lds[threadIdx.x] = v = joined(v, lds[threadIdx.x + k]);
+    }
+    __syncthreads();
+    return per;
+}
+
+// Moments of every group's part over a chunk: [B][G][chunks][parts][2] (mean, M; the count follows from the lengths).
 constexpr int kBatch = 4;  // positions in flight
 template <typename T, int W>
 __global__ __launch_bounds__(256) void moments_kernel(NormIn in, Span p, float* __restrict__ made) {
     __shared__ Moments lds[256];
-    const SpanPlace my = span_place(p);
+    const SpanPlace my = span_place(p, in, blockIdx.x);
     const int len = length_at(in.lengths, my.b, in.N), begin = my.chunk * p.chunk, stop = len - begin < p.chunk ? len : begin + p.chunk;
     if (begin >= len) return;  // nobody looks at these
-    const bool is = my.piece < p.pieces;
-    const Place at = Place::of<W>(is ? my.piece : 0, p.ppg, in.D / in.G);
+    const Place at = Place::of<W>(my.is ? (my.first + my.local) * p.ppg + my.k : 0, p.ppg, in.D / in.G);
     Moments m{0.0f, 0.0f, 0.0f};
-    for (int l = begin + my.ty; l < stop; l += kBatch * my.ly) {
-        Part<T, W> v[kBatch];
+    Part<T, W> v[kBatch];
+    const auto fetch = [&](int l) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) v[u].load(line<T>(in.x, my.b, l + u * my.ly < stop ? l + u * my.ly : stop - 1) + at.c, W);
+    };
+    int l = begin + my.ty;
+    fetch(l);
+    for (; l < stop; l += kBatch * my.ly) {
         float x[kBatch][W], s = 0.0f, q = 0.0f;
         int rows = 0;
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const bool on = l + u * my.ly < stop;
-            v[u].load(line<T>(in.x, my.b, on ? l + u * my.ly : l) + at.c, W);
-            rows += on;
-        }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
             v[u].get(x[u]);
-#pragma unroll
-            for (int j = 0; j < W; ++j) s += u < rows && j >= at.skip ? x[u][j] : 0.0f;
+            rows += l + u * my.ly < stop;
         }
-        const float n = static_cast<float>(rows * (W - at.skip)), mean = s / n;
+        fetch(l + kBatch * my.ly);
+        if (rows == kBatch && at.skip == 0) {
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u)
+            for (int u = 0; u < kBatch; ++u)
 #pragma unroll
-            for (int j = 0; j < W; ++j) q += u < rows && j >= at.skip ? (x[u][j] - mean) * (x[u][j] - mean) : 0.0f;
-        m = join(m, {n, mean, q});
+                for (int j = 0; j < W; ++j) s += x[u][j];
+            const float mean = s * (1.0f / (kBatch * W));
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+                for (int j = 0; j < W; ++j) q = fmaf(x[u][j] - mean, x[u][j] - mean, q);
+            m = join(m, {kBatch * W, mean, q});
+        } else {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+                for (int j = 0; j < W; ++j) s += u < rows && j >= at.skip ? x[u][j] : 0.0f;
+            const float n = static_cast<float>(rows * (W - at.skip)), mean = s / n;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+                for (int j = 0; j < W; ++j) q = u < rows && j >= at.skip ? fmaf(x[u][j] - mean, x[u][j] - mean, q) : q;
+            m = join(m, {n, mean, q});
+        }
     }
+    if (!my.is) m = {0.0f, 0.0f, 0.0f};
     lds[threadIdx.x] = m;
     for (int k = 128; k >= p.lx; k /= 2) {  // lx is a power of two
         __syncthreads();
         if (static_cast<int>(threadIdx.x) < k) lds[threadIdx.x] = m = join(m, lds[threadIdx.x + k]);
     }
-    if (my.ty == 0 && is) {
-        float* to = made + ((static_cast<int64_t>(my.b) * p.chunks + my.chunk) * p.pieces + my.piece) * 2;
+    join_groups(lds, m, p, my, join);
+    if (my.ty == 0 && my.is && (p.parts > 1 ? my.tx : my.k) == 0) {
+        float* to = made + (((static_cast<int64_t>(my.b) * in.G + my.first + my.local) * p.chunks + my.chunk) * p.parts + my.part) * 2;
         to[0] = m.mean;
         to[1] = m.m2;
     }
 }
 
-// A workgroup joins a group's moments: stats [B][G][2].
-template <int W>
-__global__ __launch_bounds__(256) void stats_kernel(NormIn in, Span p, const float* __restrict__ made, float* __restrict__ stats) {
-    __shared__ Moments lds[256];
-    const int64_t unit = blockIdx.x, b = unit / in.G;
-    const int g = static_cast<int>(unit - b * in.G), len = length_at(in.lengths, static_cast<int>(b), in.N);
-    const int chunks = (len - 1) / p.chunk + 1, C = in.D / in.G;  // (len 0: all of one chunk of no positions)
-    Moments m{0.0f, 0.0f, 0.0f};
-    for (int64_t e = threadIdx.x; len > 0 && e < static_cast<int64_t>(chunks) * p.ppg; e += 256) {
-        const int k = static_cast<int>(e / p.ppg), piece = static_cast<int>(e - static_cast<int64_t>(k) * p.ppg);
-        const Place at = Place::of<W>(g * p.ppg + piece, p.ppg, C);
+// (mean, rstd) of this thread's group: given, or joined from the moments.  keep: written there.
+template <int W> __device__ __forceinline__ void span_stats(const NormIn& in, const Span& p, const SpanPlace& my, int len, const float* given, const float* made, float* keep,
+                                                            Moments* lds, float& mean, float& rstd) {
+    mean = rstd = 0.0f;
+    if (given) {
+        if (my.is) {
+            mean = given[(static_cast<int64_t>(my.b) * in.G + my.first + my.local) * 2];
+            rstd = given[(static_cast<int64_t>(my.b) * in.G + my.first + my.local) * 2 + 1];
+        }
+        return;
+    }
+    const int chunks = len > 0 ? (len - 1) / p.chunk + 1 : 0, C = in.D / in.G;
+    const int per = join_entries(lds, p, my.first, in.G, static_cast<int64_t>(chunks) * p.parts, Moments{0.0f, 0.0f, 0.0f}, [&](int g, int64_t e) {
+        const int k = static_cast<int>(e / p.parts), part = static_cast<int>(e - static_cast<int64_t>(k) * p.parts);
         const int rows = len - k * p.chunk < p.chunk ? len - k * p.chunk : p.chunk;
-        const float* from = made + ((b * p.chunks + k) * p.pieces + g * p.ppg + piece) * 2;
-        m = join(m, {static_cast<float>(rows) * (W - at.skip), from[0], from[1]});
-    }
-    lds[threadIdx.x] = m;
-    for (int k = 128; k >= 1; k /= 2) {
-        __syncthreads();
-        if (static_cast<int>(threadIdx.x) < k) lds[threadIdx.x] = m = join(m, lds[threadIdx.x + k]);
-    }
-    if (threadIdx.x == 0) {
-        stats[2 * unit] = m.mean;
-        stats[2 * unit + 1] = len > 0 ? __builtin_amdgcn_rsqf(m.m2 / m.n + in.eps) : 0.0f;
+        const float* from = made + ((static_cast<int64_t>(my.b) * in.G + my.first + g) * p.chunks * p.parts + e) * 2;
+        return Moments{static_cast<float>(rows) * part_width<W>(p, part, C), from[0], from[1]};
+    }, join);
+    if (my.is) {
+        const Moments m = lds[my.local * per];
+        mean = m.mean;
+        rstd = len > 0 ? __builtin_amdgcn_rsqf(m.m2 / m.n + in.eps) : 0.0f;
+        if (keep && my.chunk == 0 && my.ty == 0 && my.k == 0) {
+            keep[(static_cast<int64_t>(my.b) * in.G + my.first + my.local) * 2] = mean;
+            keep[(static_cast<int64_t>(my.b) * in.G + my.first + my.local) * 2 + 1] = rstd;
+        }
     }
 }
 
-// sums [B][G][2]: the means of dhat and of dhat hat (GRAD).
+// Sums over parts of dweight and dbias, [parts][2][D]: workgroups of 16 channels of one of the two, HIGH threads a channel.
+template <int HIGH> __device__ __forceinline__ void channel_sums(const float* partial, int64_t parts, int D, int64_t block, float* dweight, float* dbias, float* lds) {
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4, k = block & 1;
+    const int64_t ch = (block >> 1) * 16 + x;
+    float* to = k ? dbias : dweight;
+    float s = 0.0f;
+    if (to && ch < D)
+#pragma unroll 4
+        for (int64_t q = y; q < parts; q += HIGH) s += partial[(q * 2 + k) * D + ch];
+    lds[threadIdx.x] = s;
+    for (int h = HIGH / 2; h >= 1; h /= 2) {
+        __syncthreads();
+        if (y < h) lds[threadIdx.x] = s = s + lds[threadIdx.x + 16 * h];
+    }
+    if (y == 0 && to && ch < D) to[ch] = s;
+}
+__global__ __launch_bounds__(1024) void channel_sums_kernel(const float* __restrict__ partial, int64_t parts, int D, float* __restrict__ dweight, float* __restrict__ dbias) {
+    __shared__ float lds[1024];
+    channel_sums<64>(partial, parts, D, blockIdx.x, dweight, dbias, lds);
+}
+int64_t channel_blocks(int D) { return 2 * static_cast<int64_t>((D - 1) / 16 + 1); }
+
+struct Sum2 { float a, b; };
+__device__ __forceinline__ Sum2 add(const Sum2& x, const Sum2& y) { return {x.a + y.a, x.b + y.b}; }
+
+struct ApplyRun {
+    const float *given, *made;  // statistics, or the moments they come from
+    float* stats;               // forwards: to be kept, or null
+    const float* sums;          // GRAD: [B][G][chunks][parts][2]
+    const float* partial;       // GRAD: [B * chunks][2][D], summed by the first `extra` workgroups
+    int64_t extra;
+    float *dweight, *dbias;
+    bool stream;
+};
 template <typename T, int W, bool GRAD>
-__global__ __launch_bounds__(256) void apply_kernel(NormIn in, AnyRows dout, Span p, const float* __restrict__ stats, const float* __restrict__ sums, T* __restrict__ out) {
-    const SpanPlace my = span_place(p);
-    if (my.piece >= p.pieces) return;
+__global__ __launch_bounds__(256) void apply_kernel(NormIn in, AnyRows dout, Span p, ApplyRun r, T* __restrict__ out) {
+    __shared__ Moments lds[256];
+    if (GRAD && blockIdx.x < r.extra) {
+        channel_sums<16>(r.partial, static_cast<int64_t>(in.B) * p.chunks, in.D, blockIdx.x, r.dweight, r.dbias, reinterpret_cast<float*>(lds));
+        return;
+    }
+    const SpanPlace my = span_place(p, in, blockIdx.x - static_cast<unsigned>(GRAD ? r.extra : 0));
     const int len = length_at(in.lengths, my.b, in.N), begin = my.chunk * p.chunk, stop = in.N - begin < p.chunk ? in.N : begin + p.chunk;
     const int end = len < begin ? begin : len < stop ? len : stop;
-    const Place at = Place::of<W>(my.piece, p.ppg, in.D / in.G);
-    T* o = out + static_cast<int64_t>(my.b) * in.N * in.D + at.c;
-    const int64_t unit = static_cast<int64_t>(my.b) * in.G + at.group;
-    float w[W], bias[W];
-    weights_of<W>(in, at.c, w, bias);
-    const float mean = stats[2 * unit], rstd = stats[2 * unit + 1], s1 = GRAD ? sums[2 * unit] : 0.0f, s2 = GRAD ? sums[2 * unit + 1] : 0.0f;
-    int l = begin + my.ty;
-    for (; l < end; l += kBatch * my.ly) {
-        Part<T, W> v[kBatch], d[GRAD ? kBatch : 1];
+    const Place at = Place::of<W>(my.is ? (my.first + my.local) * p.ppg + my.k : 0, p.ppg, in.D / in.G);
+    Part<T, W> v[kBatch], d[GRAD ? kBatch : 1];
+    const auto fetch = [&](int l) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int at_l = l + u * my.ly < end ? l + u * my.ly : l;
+            const int at_l = l + u * my.ly < end ? l + u * my.ly : end - 1;
             v[u].load(line<T>(in.x, my.b, at_l) + at.c, W);
             if (GRAD) d[u].load(line<T>(dout, my.b, at_l) + at.c, W);
         }
+    };
+    int l = begin + my.ty;
+    if (end > begin) fetch(l);  // on their way while the sums are joined
+    float w[W], bias[W];
+    weights_of<W>(in, at.c, w, bias);
+    float mean, rstd, s1 = 0.0f, s2 = 0.0f;
+    span_stats<W>(in, p, my, len, r.given, r.made, GRAD ? nullptr : r.stats, lds, mean, rstd);
+    if (GRAD) {
+        __syncthreads();
+        Sum2* two = reinterpret_cast<Sum2*>(lds);
+        const int chunks = len > 0 ? (len - 1) / p.chunk + 1 : 0;
+        const int per = join_entries(two, p, my.first, in.G, static_cast<int64_t>(chunks) * p.parts, Sum2{0.0f, 0.0f}, [&](int g, int64_t e) {
+            const float* from = r.sums + ((static_cast<int64_t>(my.b) * in.G + my.first + g) * p.chunks * p.parts + e) * 2;
+            return Sum2{from[0], from[1]};
+        }, add);
+        if (my.is && len > 0) {
+            const float n = static_cast<float>(len) * (in.D / in.G);
+            s1 = two[my.local * per].a / n;
+            s2 = two[my.local * per].b / n;
+        }
+    }
+    if (!my.is) return;
+    T* o = out + static_cast<int64_t>(my.b) * in.N * in.D + at.c;
+    float scale[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) scale[j] = rstd * w[j];
+    for (; l < end; l += kBatch * my.ly) {
+        float x[kBatch][W], dy[GRAD ? kBatch : 1][W];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            float x[W], dy[W];
-            v[u].get(x);
-            if (GRAD) d[u].get(dy);
+            v[u].get(x[u]);
+            if (GRAD) d[u].get(dy[u]);
+        }
+        fetch(l + kBatch * my.ly);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
 #pragma unroll
             for (int j = 0; j < W; ++j) {
-                const float hat = (x[j] - mean) * rstd, y = fmaf(hat, w[j], bias[j]);
-                if (GRAD) x[j] = rstd * ((in.silu ? dy[j] * dsilu(y) : dy[j]) * w[j] - fmaf(hat, s2, s1));
-                else x[j] = in.silu ? silu(y) : y;
+                const float away = x[u][j] - mean;
+                if (GRAD) {
+                    const float hat = away * rstd;
+                    x[u][j] = fmaf(in.silu ? dy[u][j] * dsilu(fmaf(hat, w[j], bias[j])) : dy[u][j], scale[j], -rstd * fmaf(hat, s2, s1));
+                } else {
+                    const float y = fmaf(away, scale[j], bias[j]);
+                    x[u][j] = in.silu ? silu(y) : y;
+                }
             }
-            if (l + u * my.ly < end) Part<T, W>::put(o + static_cast<int64_t>(l + u * my.ly) * in.D, W, x);
+            if (l + u * my.ly < end) {
+                T* to = o + static_cast<int64_t>(l + u * my.ly) * in.D;
+                if (r.stream) Part<T, W>::template put<true>(to, W, x[u]);
+                else Part<T, W>::put(to, W, x[u]);
+            }
         }
     }
     const float zero[W] = {};
     for (l = end + my.ty; l < stop; l += my.ly) Part<T, W>::put(o + static_cast<int64_t>(l) * in.D, W, zero);
 }
 
-// Sums of dy hat and dy over a chunk's positions: [B * chunks][2][D] (ALONE: every position has its own statistics, B is 1 and N all positions).
+// Sums of dy hat and dy over a chunk's positions, channel by channel, [B * chunks][2][D] (partial may be null), and weighed, of a group's part: [B][G][chunks][parts][2].
+// ALONE: every position has its own statistics, B is 1 and N all positions, and there are no groups' sums.
 template <typename T, int W, bool ALONE>
-__global__ __launch_bounds__(256) void columns_kernel(NormIn in, AnyRows dout, Span p, const float* __restrict__ stats, float* __restrict__ partial) {
-    __shared__ float lds[256 * 2 * W];
-    const SpanPlace my = span_place(p);
-    const int all = ALONE ? in.B * in.N : in.N;
-    const int len = ALONE ? all : length_at(in.lengths, my.b, in.N), begin = my.chunk * p.chunk;
+__global__ __launch_bounds__(256) void columns_kernel(NormIn in, AnyRows dout, Span p, const float* __restrict__ given, const float* __restrict__ made,
+                                                      float* __restrict__ partial, float* __restrict__ sums) {
+    __shared__ union { Moments m[256]; float f[256 * 2 * W]; Sum2 s[256]; } lds;
+    const SpanPlace my = span_place(p, in, blockIdx.x);
+    const int len = ALONE ? in.B * in.N : length_at(in.lengths, my.b, in.N), begin = my.chunk * p.chunk;
     const int stop = len - begin < p.chunk ? len : begin + p.chunk;
-    const bool is = my.piece < p.pieces;
-    const Place at = Place::of<W>(is ? my.piece : 0, p.ppg, in.D / in.G);
-    float w[W], bias[W], dw[W] = {}, db[W] = {};
+    const Place at = Place::of<W>(my.is ? (my.first + my.local) * p.ppg + my.k : 0, p.ppg, in.D / in.G);
+    float w[W], bias[W], dw[W] = {}, db[W] = {}, mean = 0.0f, rstd = 0.0f;
     weights_of<W>(in, at.c, w, bias);
-    const int64_t unit = static_cast<int64_t>(my.b) * in.G + at.group;
-    float mean = 0.0f, rstd = 0.0f;
-    if (!ALONE) {
-        mean = stats[2 * unit];
-        rstd = stats[2 * unit + 1];
-    }
-    for (int l = begin + my.ty; l < stop; l += kBatch * my.ly) {
-        Part<T, W> v[kBatch], d[kBatch];
-        float means[kBatch], rstds[kBatch];
-        bool on[kBatch];
+    Part<T, W> v[kBatch], d[kBatch];
+    float means[ALONE ? kBatch : 1], rstds[ALONE ? kBatch : 1];
+    bool on[kBatch];
+    const auto fetch = [&](int l) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            on[u] = l + u * my.ly < stop;
-            const int pos = on[u] ? l + u * my.ly : l, b = ALONE ? pos / in.N : my.b, row = ALONE ? pos - b * in.N : pos;
+            on[u] = my.is && l + u * my.ly < stop;
+            const int pos = l + u * my.ly < stop ? l + u * my.ly : stop - 1, b = ALONE ? pos / in.N : my.b, row = ALONE ? pos - b * in.N : pos;
             if (ALONE) {
                 on[u] = on[u] && row < length_at(in.lengths, b, in.N);
-                means[u] = stats[(static_cast<int64_t>(pos) * in.G + at.group) * 2];
-                rstds[u] = stats[(static_cast<int64_t>(pos) * in.G + at.group) * 2 + 1];
+                means[u] = given[(static_cast<int64_t>(pos) * in.G + at.group) * 2];
+                rstds[u] = given[(static_cast<int64_t>(pos) * in.G + at.group) * 2 + 1];
             }
             if (!ALONE || on[u]) {
                 v[u].load(line<T>(in.x, b, row) + at.c, W);
                 d[u].load(line<T>(dout, b, row) + at.c, W);
             }
         }
+    };
+    int l = begin + my.ty;
+    if (begin < stop) fetch(l);  // on their way while the statistics are joined
+    if (!ALONE) span_stats<W>(in, p, my, len, given, made, nullptr, lds.m, mean, rstd);
+    for (; l < stop; l += kBatch * my.ly) {
+        float x[kBatch][W], dy[kBatch][W], hats[ALONE ? kBatch : 1][2];
+        bool is[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            float x[W], dy[W];
-            v[u].get(x);
-            d[u].get(dy);
+            v[u].get(x[u]);
+            d[u].get(dy[u]);
+            is[u] = on[u];
+            if (ALONE) {
+                hats[u][0] = means[u];
+                hats[u][1] = rstds[u];
+            }
+        }
+        fetch(l + kBatch * my.ly);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
 #pragma unroll
             for (int j = 0; j < W; ++j) {
-                const float hat = (x[j] - (ALONE ? means[u] : mean)) * (ALONE ? rstds[u] : rstd);
-                const float g = in.silu ? dy[j] * dsilu(fmaf(hat, w[j], bias[j])) : dy[j];
-                dw[j] += on[u] ? g * hat : 0.0f;
-                db[j] += on[u] ? g : 0.0f;
+                const float hat = (x[u][j] - (ALONE ? hats[u][0] : mean)) * (ALONE ? hats[u][1] : rstd);
+                const float g = in.silu ? dy[u][j] * dsilu(fmaf(hat, w[j], bias[j])) : dy[u][j];
+                dw[j] = is[u] ? fmaf(g, hat, dw[j]) : dw[j];
+                db[j] = is[u] ? db[j] + g : db[j];
             }
         }
     }
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-        lds[(2 * j) * 256 + threadIdx.x] = dw[j];
-        lds[(2 * j + 1) * 256 + threadIdx.x] = db[j];
+        lds.f[(2 * j) * 256 + threadIdx.x] = dw[j];
+        lds.f[(2 * j + 1) * 256 + threadIdx.x] = db[j];
     }
+    for (int h = my.ly / 2; h >= 1; h /= 2) {
+        __syncthreads();
+        if (my.ty < h) {
+#pragma unroll
+            for (int j = 0; j < 2 * W; ++j) lds.f[j * 256 + threadIdx.x] += lds.f[j * 256 + threadIdx.x + h * p.lx];
+        }
+    }
+    Sum2 mine{0.0f, 0.0f};
+    if (my.ty == 0 && my.is) {
+        float* to = partial ? partial + (static_cast<int64_t>(my.b) * p.chunks + my.chunk) * 2 * in.D + at.c : nullptr;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            if (j < at.skip) continue;
+            const float s_hat = lds.f[(2 * j) * 256 + threadIdx.x], s = lds.f[(2 * j + 1) * 256 + threadIdx.x];
+            if (to) {
+                to[j] = s_hat;
+                to[in.D + j] = s;
+            }
+            mine.a = fmaf(w[j], s, mine.a);
+            mine.b = fmaf(w[j], s_hat, mine.b);
+        }
+    }
+    if (ALONE) return;
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * W * p.lx; e += 256) {
-        const int x = e % p.lx, k = e / p.lx, piece = my.piece - static_cast<int>(threadIdx.x) % p.lx + x;
-        if (piece >= p.pieces) continue;
-        const Place to = Place::of<W>(piece, p.ppg, in.D / in.G);
-        float s = 0.0f;
-        for (int y = 0; y < my.ly; ++y) s += lds[k * 256 + y * p.lx + x];
-        if (k / 2 >= to.skip) partial[((static_cast<int64_t>(my.b) * p.chunks + my.chunk) * 2 + k % 2) * in.D + to.c + k / 2] = s;
+    if (my.ty == 0) lds.s[my.tx] = mine;
+    join_groups(lds.s, mine, p, my, add);
+    if (my.ty == 0 && my.is && (p.parts > 1 ? my.tx : my.k) == 0) {
+        float* to = sums + (((static_cast<int64_t>(my.b) * in.G + my.first + my.local) * p.chunks + my.chunk) * p.parts + my.part) * 2;
+        to[0] = mine.a;
+        to[1] = mine.b;
     }
-}
-
-// A workgroup joins a group's sums: [B][G][2], the means of dhat and dhat hat.
-__global__ __launch_bounds__(256) void group_sums_kernel(NormIn in, int chunks, const float* __restrict__ partial, float* __restrict__ sums) {
-    __shared__ float lds[4];
-    const int64_t unit = blockIdx.x, b = unit / in.G;
-    const int g = static_cast<int>(unit - b * in.G), len = length_at(in.lengths, static_cast<int>(b), in.N), C = in.D / in.G;
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int64_t e = threadIdx.x; e < static_cast<int64_t>(chunks) * C; e += 256) {
-        const int64_t k = e / C;
-        const int c = g * C + static_cast<int>(e - k * C);
-        const float w = in.weight ? in.weight[c] : 1.0f, *from = partial + (b * chunks + k) * 2 * in.D + c;
-        s2 = fmaf(w, from[0], s2);
-        s1 = fmaf(w, from[in.D], s1);
-    }
-    s1 = block_sum(s1, lds);
-    s2 = block_sum(s2, lds);
-    if (threadIdx.x == 0) {
-        const float n = static_cast<float>(len) * C;
-        sums[2 * unit] = len > 0 ? s1 / n : 0.0f;
-        sums[2 * unit + 1] = len > 0 ? s2 / n : 0.0f;
-    }
-}
-
-// dweight and dbias from [parts][2][D]: workgroups of 64 channels, sixteen threads a channel.
-__global__ __launch_bounds__(1024) void channel_sums_kernel(const float* __restrict__ partial, int64_t parts, int D, float* __restrict__ dweight, float* __restrict__ dbias) {
-    __shared__ float lds[16][64];
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6, k = blockIdx.y, ch = blockIdx.x * 64 + x;
-    float* to = k ? dbias : dweight;
-    if (!to) return;
-    float s = 0.0f;
-    if (ch < D)
-        for (int64_t q = y; q < parts; q += 16) s += partial[(q * 2 + k) * D + ch];
-    lds[y][x] = s;
-    __syncthreads();
-    if (y || ch >= D) return;
-    for (int i = 1; i < 16; ++i) s += lds[i][x];
-    to[ch] = s;
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------
@@ -544,7 +873,7 @@ Alone alone_plan(int dtype, int B, int N, int D, int G, int& pieces) {
     while (p.groups < 64 / p.team && p.groups < G) p.groups *= 2;
     p.tiles = (G - 1) / p.groups + 1;
     const int64_t rows = 4 * (64 / p.team / p.groups), all = (static_cast<int64_t>(B) * N + rows - 1) / rows;
-    int64_t most = 2048 / p.tiles;
+    int64_t most = AW / p.tiles;
     if (most < 1) most = 1;
     p.blocks = all < most ? all : most;
     return p;
@@ -554,29 +883,76 @@ Span span_plan(int dtype, int B, int N, int D, int G) {
     Span p;
     const int C = D / G, W = piece_width(dtype, C);
     p.ppg = (C - 1) / W + 1;
-    p.pieces = p.ppg * G;
+    const int64_t pieces = static_cast<int64_t>(p.ppg) * G;
+    p.parts = (p.ppg - 1) / 256 + 1;
     p.lx = 1;
-    while (p.lx < 64 && p.lx < p.pieces) p.lx *= 2;
-    p.tiles = (p.pieces - 1) / p.lx + 1;
-    const int least = kBatch * (256 / p.lx);  // a chunk's positions: as many as keep 1024 workgroups, at most 16 batches of a thread
+    while (p.lx < 64 && p.lx < pieces) p.lx *= 2;
+    while (p.lx < 256 && p.lx < p.ppg) p.lx *= 2;
+    // wider where groups leave fewer threads without a piece
+    for (int lx = 2 * p.lx; p.parts == 1 && lx <= 256 && lx / 2 < pieces; lx *= 2)
+        if (lx / p.ppg * p.ppg * p.lx * 8 > p.lx / p.ppg * p.ppg * lx * 9) p.lx = lx;
+    p.groups = p.parts > 1 ? 1 : p.lx / p.ppg;
+    p.tiles = p.parts > 1 ? G * p.parts : (G - 1) / p.groups + 1;
+    const int least = kBatch * (256 / p.lx);  // a chunk's positions: as many as keep 512 workgroups, at most 16 batches of a thread
     p.chunk = 16 * least;
-    while (p.chunk > least && static_cast<int64_t>(B) * p.tiles * ((N - 1) / p.chunk + 1) < 1024) p.chunk /= 2;
+    while (p.chunk > least && static_cast<int64_t>(B) * p.tiles * ((N - 1) / p.chunk + 1) < 512) p.chunk /= 2;
     p.chunks = (N - 1) / p.chunk + 1;
     return p;
 }
 
-size_t moments_bytes(const Span& p, int B) { return up256(static_cast<size_t>(B) * p.chunks * p.pieces * 8); }
+// Whether a sequence's groups fit registers.  At least 128 bytes of a row a workgroup (whole cache lines), more where groups leave fewer lanes without a piece;
+// as many threads as hold the positions in R pieces.
+constexpr int64_t kHeldBytes = int64_t{16} << 20;
+bool held_plan(int dtype, int B, int N, int D, int G, Held& p) {
+    if (static_cast<int64_t>(B) * N * D * (dtype ? 2 : 4) > kHeldBytes) return false;
+    const int C = D / G, W = piece_width(dtype, C), line = 128 / (W * (dtype ? 2 : 4));
+    p.ppg = (C - 1) / W + 1;
+    if (p.ppg > 512) return false;
+    const int64_t pieces = static_cast<int64_t>(p.ppg) * G;
+    int least = 1;
+    while (least < p.ppg || (least < line && least < pieces)) least *= 2;
+    p.lx = least;
+    for (int lx = 2 * least; lx <= 4 * least && lx <= 256; lx *= 2)  // (never across more than a row has)
+        if (lx / 2 < pieces && lx / p.ppg * p.ppg * p.lx > p.lx / p.ppg * p.ppg * lx * 9 / 8) p.lx = lx;
+    p.groups = p.lx / p.ppg;
+    p.tiles = (G - 1) / p.groups + 1;
+    for (const int most : {2, 4})
+        for (p.threads = 256; p.threads <= 1024; p.threads *= 2) {
+            if (p.threads < p.lx || (N - 1) / (p.threads / p.lx) + 1 > most) continue;
+            p.pieces = most;
+            return true;
+        }
+    return false;
+}
+
+// two floats a group's part and chunk
+size_t entries_bytes(const Span& p, int B, int G) { return up256(static_cast<size_t>(B) * G * p.chunks * p.parts * 8); }
 size_t stats_bytes(int64_t units) { return up256(static_cast<size_t>(units) * 8); }
 size_t partial_bytes(int64_t parts, int D) { return up256(static_cast<size_t>(parts) * 2 * D * 4); }
 
 template <typename T, int W, bool GRAD>
 hipError_t alone_of(const NormIn& in, AnyRows dout, const Alone& p, int pieces, const float* given, void* out, float* stats, float* partial, hipStream_t st) {
     if (!fits(p.blocks * p.tiles, 256)) return hipErrorInvalidValue;
-    auto kernel = alone_kernel<T, W, 1, GRAD>;
+    const bool exact = in.D / in.G == p.team * pieces * W;
+    auto kernel = exact ? alone_kernel<T, W, 1, GRAD, true> : alone_kernel<T, W, 1, GRAD, false>;
     if constexpr (W == Wide<T>::V) {  // narrower pieces are at most two a group
-        kernel = pieces <= 1 ? kernel : pieces == 2 ? alone_kernel<T, W, 2, GRAD> : pieces == 3 ? alone_kernel<T, W, 3, GRAD> : alone_kernel<T, W, 4, GRAD>;
+        if (pieces == 2) kernel = exact ? alone_kernel<T, W, 2, GRAD, true> : alone_kernel<T, W, 2, GRAD, false>;
+        if (pieces == 3) kernel = alone_kernel<T, W, 3, GRAD, false>;
+        if (pieces == 4) kernel = exact ? alone_kernel<T, W, 4, GRAD, true> : alone_kernel<T, W, 4, GRAD, false>;
     }
     kernel<<<static_cast<unsigned>(p.blocks * p.tiles), 256, 0, st>>>(in, dout, p, given, static_cast<T*>(out), stats, partial);
+    return hipGetLastError();
+}
+
+template <typename T, int W, bool GRAD>
+hipError_t held_of(const NormIn& in, AnyRows dout, const Held& p, const float* given, void* out, float* stats, float* partial, hipStream_t st) {
+    if (!fits(static_cast<int64_t>(in.B) * p.tiles, p.threads)) return hipErrorInvalidValue;
+    const auto kernel = p.pieces == 2 ? held_kernel<T, W, 2, GRAD> : held_kernel<T, W, 4, GRAD>;
+    const int entries = p.threads / 64 * (p.lx < 64 ? p.lx : 64);
+    int floats = p.threads + p.lx;
+    if (GRAD && floats < W * entries) floats = W * entries;
+    if (floats < 2 * p.lx) floats = 2 * p.lx;
+    kernel<<<static_cast<unsigned>(in.B * p.tiles), p.threads, sizeof(float) * floats, st>>>(in, dout, p, given, static_cast<T*>(out), stats, partial);
     return hipGetLastError();
 }
 
@@ -599,21 +975,21 @@ hipError_t norm_of(int dtype, const NormIn& in, const Outs& o, void* ws, hipStre
         }
         return hipGetLastError();
     }
+    Held h;
+    if (held_plan(dtype, in.B, in.N, in.D, in.G, h)) return held_of<T, W, false>(in, {}, h, nullptr, o.out, o.stats, nullptr, st);
     const Span p = span_plan(dtype, in.B, in.N, in.D, in.G);
     const int64_t blocks = static_cast<int64_t>(in.B) * p.chunks * p.tiles;
-    if (!fits(blocks, 256) || !fits(static_cast<int64_t>(in.B) * in.G, 256)) return hipErrorInvalidValue;
+    if (!fits(blocks, 256)) return hipErrorInvalidValue;
     float* made = static_cast<float*>(ws);
-    float* stats = o.stats ? o.stats : reinterpret_cast<float*>(static_cast<char*>(ws) + moments_bytes(p, in.B));
     moments_kernel<T, W><<<static_cast<unsigned>(blocks), 256, 0, st>>>(in, p, made);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    stats_kernel<W><<<static_cast<unsigned>(in.B * in.G), 256, 0, st>>>(in, p, made, stats);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess || !o.out) return e;
-    apply_kernel<T, W, false><<<static_cast<unsigned>(blocks), 256, 0, st>>>(in, {}, p, stats, nullptr, static_cast<T*>(o.out));
+    const ApplyRun r{nullptr, made, o.stats, nullptr, nullptr, 0, nullptr, nullptr, past_caches(static_cast<int64_t>(in.B) * in.N * in.D * static_cast<int64_t>(sizeof(T)))};
+    apply_kernel<T, W, false><<<static_cast<unsigned>(blocks), 256, 0, st>>>(in, {}, p, r, static_cast<T*>(o.out));
     return hipGetLastError();
 }
 
-hipError_t channel_sums(const float* partial, int64_t parts, const NormIn& in, const Outs& o, hipStream_t st) {
-    channel_sums_kernel<<<dim3(pieces_of_row(in.D, 64), 2), 1024, 0, st>>>(partial, parts, in.D, o.dweight, o.dbias);
+hipError_t launch_channel_sums(const float* partial, int64_t parts, const NormIn& in, const Outs& o, hipStream_t st) {
+    channel_sums_kernel<<<static_cast<unsigned>(channel_blocks(in.D)), 1024, 0, st>>>(partial, parts, in.D, o.dweight, o.dbias);
     return hipGetLastError();
 }
 
@@ -627,7 +1003,7 @@ hipError_t norm_grad_of(int dtype, AnyRows dout, const NormIn& in, const float* 
         float* partial = reinterpret_cast<float*>(room);
         if (alone_fits(p.ppg)) {
             if (const hipError_t e = alone_of<T, W, true>(in, dout, p, pieces, stats, o.out, nullptr, sums ? partial : nullptr, st); e != hipSuccess || !sums) return e;
-            return channel_sums(partial, p.blocks, in, o, st);
+            return launch_channel_sums(partial, p.blocks, in, o, st);
         }
         if constexpr (W == Wide<T>::V) {
             const int64_t units = static_cast<int64_t>(in.B) * in.N * in.G;
@@ -636,31 +1012,35 @@ hipError_t norm_grad_of(int dtype, AnyRows dout, const NormIn& in, const float* 
             float* made = reinterpret_cast<float*>(room + partial_bytes(q.chunks, in.D));
             wide_kernel<T, W, true><<<static_cast<unsigned>(units < kWideBlocks ? units : kWideBlocks), 256, 0, st>>>(in, dout, p.ppg, stats, static_cast<T*>(o.out), stats ? nullptr : made);
             if (const hipError_t e = hipGetLastError(); e != hipSuccess || !sums) return e;
-            columns_kernel<T, W, true><<<static_cast<unsigned>(q.chunks * q.tiles), 256, 0, st>>>(in, dout, q, stats ? stats : made, partial);
+            columns_kernel<T, W, true><<<static_cast<unsigned>(q.chunks * q.tiles), 256, 0, st>>>(in, dout, q, stats ? stats : made, nullptr, partial, nullptr);
             if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-            return channel_sums(partial, q.chunks, in, o, st);
+            return launch_channel_sums(partial, q.chunks, in, o, st);
         }
         return hipErrorInvalidValue;
     }
+    Held h;
+    if (held_plan(dtype, in.B, in.N, in.D, in.G, h)) {
+        float* partial = reinterpret_cast<float*>(room);
+        if (const hipError_t e = held_of<T, W, true>(in, dout, h, stats, o.out, nullptr, sums ? partial : nullptr, st); e != hipSuccess || !sums) return e;
+        return launch_channel_sums(partial, in.B, in, o, st);
+    }
     const Span p = span_plan(dtype, in.B, in.N, in.D, in.G);
-    const int64_t blocks = static_cast<int64_t>(in.B) * p.chunks * p.tiles, units = static_cast<int64_t>(in.B) * in.G;
-    if (!fits(blocks, 256) || !fits(units, 256)) return hipErrorInvalidValue;
+    const int64_t blocks = static_cast<int64_t>(in.B) * p.chunks * p.tiles, extra = sums ? channel_blocks(in.D) : 0;
+    if (!fits(blocks + extra, 256)) return hipErrorInvalidValue;
     float* partial = reinterpret_cast<float*>(room);
     room += partial_bytes(static_cast<int64_t>(in.B) * p.chunks, in.D);
-    float* means = reinterpret_cast<float*>(room);
-    room += stats_bytes(units);
+    float* of_groups = reinterpret_cast<float*>(room);
+    room += entries_bytes(p, in.B, in.G);
+    float* made = reinterpret_cast<float*>(room);
     if (!stats) {
-        float* made = reinterpret_cast<float*>(room);
-        if (const hipError_t e = norm_of<T, W>(dtype, in, {nullptr, made, nullptr, nullptr}, room + stats_bytes(units), st); e != hipSuccess) return e;
-        stats = made;
+        moments_kernel<T, W><<<static_cast<unsigned>(blocks), 256, 0, st>>>(in, p, made);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    columns_kernel<T, W, false><<<static_cast<unsigned>(blocks), 256, 0, st>>>(in, dout, p, stats, partial);
+    columns_kernel<T, W, false><<<static_cast<unsigned>(blocks), 256, 0, st>>>(in, dout, p, stats, made, sums ? partial : nullptr, of_groups);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    group_sums_kernel<<<static_cast<unsigned>(units), 256, 0, st>>>(in, p.chunks, partial, means);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    apply_kernel<T, W, true><<<static_cast<unsigned>(blocks), 256, 0, st>>>(in, dout, p, stats, means, static_cast<T*>(o.out));
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess || !sums) return e;
-    return channel_sums(partial, static_cast<int64_t>(in.B) * p.chunks, in, o, st);
+    const ApplyRun r{stats, made, nullptr, of_groups, partial, extra, o.dweight, o.dbias, past_caches(static_cast<int64_t>(in.B) * in.N * in.D * static_cast<int64_t>(sizeof(T)))};
+    apply_kernel<T, W, true><<<static_cast<unsigned>(blocks + extra), 256, 0, st>>>(in, dout, p, r, static_cast<T*>(o.out));
+    return hipGetLastError();
 }
 
 #define LCCRF_BY_WIDTH(call)                      \
@@ -674,8 +1054,9 @@ hipError_t norm_grad_of(int dtype, AnyRows dout, const NormIn& in, const float* 
 }  // namespace
 
 size_t norm_workspace(int dtype, int B, int N, int D, int G, bool alone) {
-    if (alone) return 256;
-    return moments_bytes(span_plan(dtype, B, N, D, G), B) + stats_bytes(static_cast<int64_t>(B) * G);
+    Held h;
+    if (alone || held_plan(dtype, B, N, D, G, h)) return 256;
+    return entries_bytes(span_plan(dtype, B, N, D, G), B, G);
 }
 
 size_t norm_grad_workspace(int dtype, int B, int N, int D, int G, bool alone) {
@@ -685,9 +1066,10 @@ size_t norm_grad_workspace(int dtype, int B, int N, int D, int G, bool alone) {
         if (alone_fits(p.ppg)) return partial_bytes(p.blocks, D);
         return partial_bytes(span_plan(dtype, 1, B * N, D, G).chunks, D) + stats_bytes(static_cast<int64_t>(B) * N * G);
     }
+    Held h;
+    if (held_plan(dtype, B, N, D, G, h)) return partial_bytes(B, D);
     const Span p = span_plan(dtype, B, N, D, G);
-    const int64_t units = static_cast<int64_t>(B) * G;
-    return partial_bytes(static_cast<int64_t>(B) * p.chunks, D) + 2 * stats_bytes(units) + norm_workspace(dtype, B, N, D, G, false);
+    return partial_bytes(static_cast<int64_t>(B) * p.chunks, D) + 2 * entries_bytes(p, B, G);
 }
 
 hipError_t launch_norm(int dtype, const NormIn& in, void* out, float* stats, void* ws, hipStream_t st) {
