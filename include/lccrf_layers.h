@@ -10,7 +10,8 @@
  * may not overlap inputs, except where stated.  lengths: int32 [B] or NULL (= all N), clamped to [0, N]; inputs at and past the
  * length are never read, outputs and gradients there are 0.
  * LCCRF_EINVAL where a size is below 1 or above its limit (B * N at most 2^31 - 1024; D, V and K below), LCCRF_EALIGN where a
- * pointer is not aligned to its element (workspaces and `saved`: 256 bytes).
+ * pointer is not aligned to its element (workspaces and `saved`: 256 bytes).  A workspace of 256 bytes is one that nothing is kept in: it may
+ * be NULL.
  */
 #ifndef LCCRF_LAYERS_H
 #define LCCRF_LAYERS_H

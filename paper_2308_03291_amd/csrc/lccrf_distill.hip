@@ -7,6 +7,8 @@
 // threads have the same class, so the gradient may be written over the logits.
 #include "lccrf_layers.h"
 
+#include <type_traits>
+
 namespace lccrf {
 namespace enc {
 namespace {
@@ -84,8 +86,9 @@ template <typename T, int L, int E> struct Entries {
 #pragma unroll
         for (int f = 0; f < E; ++f)
             for (int s = 0; s < L && f * L + s < K; ++s) {
-                const int other = __shfl(id[f], base + s);
-                const float q = __shfl(v[f], base + s);
+                // (64 lanes: the entry is the same for all of them)
+                const int other = L == 64 ? __builtin_amdgcn_readlane(id[f], s) : __shfl(id[f], base + s);
+                const float q = L == 64 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v[f]), s)) : __shfl(v[f], base + s);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const bool same = other == id[e];
@@ -179,7 +182,7 @@ __global__ __launch_bounds__(256) void team_kernel(DistillIn in, const float* __
 template <typename T, int THREADS, int E, bool GRAD>
 __global__ __launch_bounds__(THREADS) void row_kernel(DistillIn in, const float* __restrict__ dloss, const float* __restrict__ given, float* __restrict__ loss,
                                                       float* __restrict__ lse, T* dlogits) {
-    constexpr int W = Wide<T>::V, kWaves = THREADS / 64;
+    constexpr int W = Wide<T>::V, kWaves = THREADS / 64, U = 4;  // pieces in flight
     __shared__ float tops[kWaves], sums[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pieces = in.V / W, left = in.V - pieces * W;
     const float per_t = 1.0f / in.temperature, k2 = kLog2e * per_t;
@@ -205,10 +208,8 @@ __global__ __launch_bounds__(THREADS) void row_kernel(DistillIn in, const float*
             log_s = given[row];
         } else {
             float m = kLeast, s = 0.0f;
-            for (int k = tid; k < pieces; k += THREADS) {
-                Piece<T, W> raw;
+            const auto take = [&](const Piece<T, W>& raw) {
                 float x[W];
-                raw.load(x0 + static_cast<int64_t>(k) * W, W);
                 raw.get(x);
                 float now = m;
 #pragma unroll
@@ -217,6 +218,19 @@ __global__ __launch_bounds__(THREADS) void row_kernel(DistillIn in, const float*
 #pragma unroll
                 for (int j = 0; j < W; ++j) s += exp2_fast((x[j] - now) * k2);
                 m = now;
+            };
+            int k = tid;
+            for (; k + (U - 1) * THREADS < pieces; k += U * THREADS) {
+                Piece<T, W> raw[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) raw[u].load(x0 + static_cast<int64_t>(k + u * THREADS) * W, W);
+#pragma unroll
+                for (int u = 0; u < U; ++u) take(raw[u]);
+            }
+            for (; k < pieces; k += THREADS) {
+                Piece<T, W> raw;
+                raw.load(x0 + static_cast<int64_t>(k) * W, W);
+                take(raw);
             }
             if (tid < left) {
                 const float x = get1(x0 + static_cast<int64_t>(pieces) * W + tid), now = __builtin_elementwise_maximum(m, x);
@@ -239,7 +253,7 @@ __global__ __launch_bounds__(THREADS) void row_kernel(DistillIn in, const float*
             for (int v = 0; v < kWaves; ++v) s += sums[v] * exp2_fast((tops[v] - M) * k2);
             log_s = kLn2f * __builtin_amdgcn_logf(s);
         }
-        const float scale = GRAD ? dloss[row] * in.temperature : 0.0f;
+        const float scale = GRAD ? dloss[row] * in.temperature : 0.0f, log2_s = kLog2e * log_s;
         if (wave == 0) {
             const float log_st = top.settle(k2);
             if (loss) {
@@ -254,27 +268,150 @@ __global__ __launch_bounds__(THREADS) void row_kernel(DistillIn in, const float*
 #pragma unroll
             for (int e = 0; e < E; ++e) asm volatile("" : "+v"(top.x[e]));
             __syncthreads();
-            for (int k = tid; k < pieces; k += THREADS) {
-                Piece<T, W> raw;
+            const auto turn = [&](const Piece<T, W>& raw, int k) {
                 float x[W];
-                raw.load(x0 + static_cast<int64_t>(k) * W, W);
                 raw.get(x);
 #pragma unroll
-                for (int j = 0; j < W; ++j) x[j] = exp2_fast((x[j] - M) * k2 - kLog2e * log_s) * scale;
-                Piece<T, W>::put(o + static_cast<int64_t>(k) * W, W, x);
+                for (int j = 0; j < W; ++j) x[j] = exp2_fast(fmaf(x[j] - M, k2, -log2_s)) * scale;
+                Piece<T, W>::template put<true>(o + static_cast<int64_t>(k) * W, W, x);
+            };
+            int k = tid;
+            for (; k + (U - 1) * THREADS < pieces; k += U * THREADS) {
+                Piece<T, W> raw[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) raw[u].load(x0 + static_cast<int64_t>(k + u * THREADS) * W, W);
+#pragma unroll
+                for (int u = 0; u < U; ++u) turn(raw[u], k + u * THREADS);
+            }
+            for (; k < pieces; k += THREADS) {
+                Piece<T, W> raw;
+                raw.load(x0 + static_cast<int64_t>(k) * W, W);
+                turn(raw, k);
             }
             if (tid < left) {
                 const int64_t at = static_cast<int64_t>(pieces) * W + tid;
-                put1(o + at, exp2_fast((get1(x0 + at) - M) * k2 - kLog2e * log_s) * scale);
+                put1(o + at, exp2_fast(fmaf(get1(x0 + at) - M, k2, -log2_s)) * scale);
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the row is written, then the named classes once more
             __syncthreads();
             if (wave == 0) {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (top.id[e] >= 0) put1(o + top.id[e], (exp2_fast((top.x[e] - M) * k2 - kLog2e * log_s) - top.v[e]) * scale);
+                    if (top.id[e] >= 0) put1(o + top.id[e], (exp2_fast(fmaf(top.x[e] - M, k2, -log2_s)) - top.v[e]) * scale);
             }
         }
+    }
+}
+
+// ---- many classes, loss and gradient in one: a row in registers --------------------------------------------------
+// A workgroup has a row, R pieces a thread, and reads it once.  The first wave finds the named classes and leaves them in LDS, chained by the thread that has
+// the class in its registers: that thread writes them once more behind its row, the difference rounded once (the classes of a chain differ, so their order does
+// not matter).
+struct Named { int id, next; float x, q; };
+template <typename T, int THREADS, int R, int E>
+__global__ __launch_bounds__(THREADS) void held_kernel(DistillIn in, const float* __restrict__ dloss, float* __restrict__ loss, T* dlogits) {
+    constexpr int W = Wide<T>::V, kWaves = THREADS / 64;
+    __shared__ float tops[kWaves], sums[kWaves];
+    __shared__ int heads[THREADS];
+    __shared__ Named named[64 * E];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), pieces = in.V / W, left = in.V - pieces * W;
+    const float per_t = 1.0f / in.temperature, k2 = kLog2e * per_t;
+    const int64_t row = blockIdx.x;
+    const T* from = static_cast<const T*>(in.logits) + row * in.row;
+    T* o = dlogits + row * in.V;
+    Entries<T, 64, E> top;
+    top.load(in, row, lane, true);
+    if (__ballot(top.some()) == 0) {  // the same in all waves
+        if (tid == 0 && loss) loss[row] = 0.0f;
+        const float zero[W] = {};
+        for (int k = tid; k < pieces; k += THREADS) Piece<T, W>::put(o + static_cast<unsigned>(k) * W, W, zero);
+        if (tid < left) put1(o + static_cast<unsigned>(pieces) * W + tid, 0.0f);
+        return;
+    }
+    Piece<T, W> raw[R];
+    T rest{};
+#pragma unroll
+    for (int r = 0; r < R; ++r) {  // a thread without a piece takes the last one
+        if (r * THREADS >= pieces) break;
+        const unsigned k = tid + r * THREADS < pieces ? tid + r * THREADS : pieces - 1;
+        raw[r].raw = *reinterpret_cast<const typename Piece<T, W>::Any*>(reinterpret_cast<const char*>(from) + k * 16u);
+    }
+    if (tid < left) rest = from[static_cast<unsigned>(pieces) * W + tid];
+    heads[tid] = -1;
+    lds_sync();
+    float log_st = 0.0f;
+    if (wave == 0) {
+        top.gather(from);
+        log_st = top.settle(k2);
+        Entries<T, 64, E> once = top;
+        once.gather_twice(in.K);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (once.id[e] >= 0) {
+                const int piece = once.id[e] / W, owner = piece < pieces ? piece % THREADS : once.id[e] - pieces * W;
+                Named& n = named[lane + e * 64];
+                n.id = once.id[e];
+                n.x = once.x[e];
+                n.q = once.v[e];
+                n.next = atomicExch(&heads[owner], lane + e * 64);
+            }
+    }
+    float m = kLeast, s = 0.0f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r * THREADS >= pieces) break;
+        float x[W];
+        asm volatile("" : "+v"(raw[r].raw));  // (widened where it is used and not kept so)
+        raw[r].get(x);
+        float now = m, sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) now = __builtin_elementwise_maximum(now, x[j]);
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum += exp2_fast((x[j] - now) * k2);
+        // (the last piece once more: its maximum does no harm)
+        s = fmaf(s, exp2_fast((m - now) * k2), tid + r * THREADS < pieces ? sum : 0.0f);
+        m = now;
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (tid < left) {
+        const float x = widen(rest), now = __builtin_elementwise_maximum(m, x);
+        s = s * exp2_fast((m - now) * k2) + exp2_fast((x - now) * k2);
+        m = now;
+    }
+    const float wave_top = team_max<64>(m);
+    s = team_sum<64>(s * exp2_fast((m - wave_top) * k2));
+    if (lane == 0) {
+        tops[wave] = wave_top;
+        sums[wave] = s;
+    }
+    lds_sync();
+    float M = tops[0];
+#pragma unroll
+    for (int v = 1; v < kWaves; ++v) M = __builtin_elementwise_maximum(M, tops[v]);
+    s = 0.0f;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) s += sums[v] * exp2_fast((tops[v] - M) * k2);
+    const float scale = dloss[row] * in.temperature, share = scale / s;
+    if (wave == 0 && loss) {
+        const float d = top.divergence(per_t, log_st, M, kLn2f * __builtin_amdgcn_logf(s));
+        if (lane == 0) loss[row] = in.temperature * in.temperature * d;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r * THREADS >= pieces) break;
+        float x[W];
+        asm volatile("" : "+v"(raw[r].raw));
+        raw[r].get(x);
+#pragma unroll
+        for (int j = 0; j < W; ++j) x[j] = exp2_fast((x[j] - M) * k2) * share;
+        if (tid + r * THREADS < pieces) Piece<T, W>::template put<true>(o + static_cast<unsigned>(tid + r * THREADS) * W, W, x);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (tid < left) put1(o + static_cast<unsigned>(pieces) * W + tid, exp2_fast((widen(rest) - M) * k2) * share);
+    for (int k = heads[tid]; k >= 0;) {  // behind this thread's own stores
+        const Named n = named[k];
+        put1(o + n.id, fmaf(exp2_fast((n.x - M) * k2), share, -n.q * scale));
+        k = n.next;
     }
 }
 
@@ -300,8 +437,22 @@ hipError_t distill_of(const DistillIn& in, const float* dloss, const float* give
         if (wide <= 64) return go(team_kernel<T, 64, 1, 1, GRAD>, 64);
         return go(wide <= 128 ? team_kernel<T, 64, 2, 1, GRAD> : team_kernel<T, 64, 4, 1, GRAD>, 64);
     }
-    const unsigned blocks = static_cast<unsigned>(in.n < kMostBlocks ? in.n : kMostBlocks);
     const bool many = in.K > 64;
+    if constexpr (GRAD) {
+        if (!given && pieces <= 16384 && in.n < kMostBlocks) {
+            const auto go = [&](auto kernel, int threads) {
+                kernel<<<static_cast<unsigned>(in.n), threads, 0, st>>>(in, dloss, loss, o);
+                return hipGetLastError();
+            };
+            if (pieces <= 1024) return go(many ? held_kernel<T, 256, 4, kEntries> : held_kernel<T, 256, 4, 1>, 256);
+            if (pieces <= 2048) return go(many ? held_kernel<T, 256, 8, kEntries> : held_kernel<T, 256, 8, 1>, 256);
+            if (pieces <= 4096) return go(many ? held_kernel<T, 512, 8, kEntries> : held_kernel<T, 512, 8, 1>, 512);
+            if (pieces <= 8192) return go(many ? held_kernel<T, 512, 16, kEntries> : held_kernel<T, 512, 16, 1>, 512);
+            if (pieces <= 12800) return go(many ? held_kernel<T, 512, 25, kEntries> : held_kernel<T, 512, 25, 1>, 512);
+            return go(many ? held_kernel<T, 512, 32, kEntries> : held_kernel<T, 512, 32, 1>, 512);
+        }
+    }
+    const unsigned blocks = static_cast<unsigned>(in.n < kMostBlocks ? in.n : kMostBlocks);
     if (pieces < 2048) {
         const auto kernel = many ? row_kernel<T, 256, kEntries, GRAD> : row_kernel<T, 256, 1, GRAD>;
         kernel<<<blocks, 256, 0, st>>>(in, dloss, given, loss, lse, o);

@@ -30,6 +30,10 @@ inline RecurIn recur_in(const lccrf_recurrence_inputs* in, float rate, const int
     return {rows(in->x), rows(in->f), rows(in->g), rows(in->z), in->decay, in->f_bias, in->g_bias, rate, lengths, B, N, D};
 }
 
+// A size of 0 is that of a call that is not served: what is asked for is 256 bytes more than what is needed.
+inline size_t asked(size_t need) { return need + 256; }
+inline bool room(const void* workspace, size_t bytes, size_t need) { return need == 0 || (workspace && bytes >= need); }
+
 inline int distill_inputs(const void* logits, int dtype, const int32_t* ids, const float* teacher) {
     if (!logits || !ids || !teacher) return LCCRF_ENULL;
     return lies(logits, size_of(dtype)) && lies(ids, 4) && lies(teacher, 4) ? LCCRF_OK : LCCRF_EALIGN;
@@ -40,9 +44,9 @@ inline int distill_inputs(const void* logits, int dtype, const int32_t* ids, con
 extern "C" {
 
 size_t lccrf_recurrence_saved_bytes(int B, int N, int D) { return sizes_ok(B, N, D) ? recur_saved_bytes(B, N, D) : 0; }
-size_t lccrf_recurrence_workspace_bytes(int B, int N, int D) { return sizes_ok(B, N, D) ? recur_workspace(B, N, D) : 0; }
+size_t lccrf_recurrence_workspace_bytes(int B, int N, int D) { return sizes_ok(B, N, D) ? asked(recur_workspace(B, N, D)) : 0; }
 size_t lccrf_recurrence_grad_workspace_bytes(int B, int N, int D, int with_saved) {
-    return sizes_ok(B, N, D) ? recur_grad_workspace(B, N, D, with_saved != 0) : 0;
+    return sizes_ok(B, N, D) ? asked(recur_grad_workspace(B, N, D, with_saved != 0)) : 0;
 }
 
 int lccrf_recurrence(const lccrf_recurrence_inputs* in, lccrf_dtype dtype, float rate, const int32_t* lengths, int B, int N, int D, const float* state, void* out,
@@ -50,7 +54,7 @@ int lccrf_recurrence(const lccrf_recurrence_inputs* in, lccrf_dtype dtype, float
     if (!type_ok(dtype) || !sizes_ok(B, N, D) || !positive(rate)) return LCCRF_EINVAL;
     if (!out) return LCCRF_ENULL;
     if (const int rc = recur_inputs(in, dtype)) return rc;
-    if (!workspace || workspace_bytes < recur_workspace(B, N, D)) return LCCRF_EWORKSPACE;
+    if (!room(workspace, workspace_bytes, recur_workspace(B, N, D))) return LCCRF_EWORKSPACE;
     if (!lies(lengths, 4) || !lies(state, 4) || !lies(out, size_of(dtype)) || !lies(final_state, 4) || !lies(saved, 256) || !lies(workspace, 256)) return LCCRF_EALIGN;
     return status(launch_recur(dtype, recur_in(in, rate, lengths, B, N, D), state, out, final_state, static_cast<float*>(saved), workspace, static_cast<hipStream_t>(stream)));
 }
@@ -61,7 +65,7 @@ int lccrf_recurrence_grad(const lccrf_rows* dout, const lccrf_recurrence_inputs*
     if (!dout || !dout->data || !g || !g->dx || !g->df || !g->dg || !g->ddecay) return LCCRF_ENULL;
     if (const int rc = recur_inputs(in, dtype)) return rc;
     if ((in->z.data != nullptr) != (g->dz != nullptr) || (g->dstate && !state)) return LCCRF_EINVAL;
-    if (!workspace || workspace_bytes < recur_grad_workspace(B, N, D, saved != nullptr)) return LCCRF_EWORKSPACE;
+    if (!room(workspace, workspace_bytes, recur_grad_workspace(B, N, D, saved != nullptr))) return LCCRF_EWORKSPACE;
     const size_t e = size_of(dtype);
     if (!lies(dout->data, e) || !lies(lengths, 4) || !lies(state, 4) || !lies(saved, 256) || !lies(workspace, 256) || !lies(g->dx, e) || !lies(g->df, e) || !lies(g->dg, e) ||
         !lies(g->dz, e) || !lies(g->ddecay, 4) || !lies(g->df_bias, 4) || !lies(g->dg_bias, 4) || !lies(g->dstate, 4))
@@ -80,17 +84,17 @@ int lccrf_recurrence_step(const lccrf_recurrence_inputs* in, lccrf_dtype dtype, 
 }
 
 size_t lccrf_group_norm_workspace_bytes(lccrf_dtype dtype, int B, int N, int D, int G, int per_position) {
-    return norm_ok(dtype, B, N, D, G) ? norm_workspace(dtype, B, N, D, G, per_position != 0) : 0;
+    return norm_ok(dtype, B, N, D, G) ? asked(norm_workspace(dtype, B, N, D, G, per_position != 0)) : 0;
 }
 size_t lccrf_group_norm_grad_workspace_bytes(lccrf_dtype dtype, int B, int N, int D, int G, int per_position) {
-    return norm_ok(dtype, B, N, D, G) ? norm_grad_workspace(dtype, B, N, D, G, per_position != 0) : 0;
+    return norm_ok(dtype, B, N, D, G) ? asked(norm_grad_workspace(dtype, B, N, D, G, per_position != 0)) : 0;
 }
 
 int lccrf_group_norm(const lccrf_rows* x, lccrf_dtype dtype, const float* weight, const float* bias, const int32_t* lengths, int B, int N, int D, int G, int per_position,
                      float eps, int silu, void* out, float* stats, void* workspace, size_t workspace_bytes, void* stream) {
     if (!norm_ok(dtype, B, N, D, G) || !positive(eps)) return LCCRF_EINVAL;
     if (!x || !x->data || !out) return LCCRF_ENULL;
-    if (!workspace || workspace_bytes < norm_workspace(dtype, B, N, D, G, per_position != 0)) return LCCRF_EWORKSPACE;
+    if (!room(workspace, workspace_bytes, norm_workspace(dtype, B, N, D, G, per_position != 0))) return LCCRF_EWORKSPACE;
     const size_t e = size_of(dtype);
     if (!lies(x->data, e) || !lies(weight, 4) || !lies(bias, 4) || !lies(lengths, 4) || !lies(out, e) || !lies(stats, 4) || !lies(workspace, 256)) return LCCRF_EALIGN;
     const NormIn in{rows(*x), weight, bias, lengths, B, N, D, G, eps, silu != 0, per_position != 0};
@@ -102,7 +106,7 @@ int lccrf_group_norm_grad(const lccrf_rows* dout, const lccrf_rows* x, lccrf_dty
                           size_t workspace_bytes, void* stream) {
     if (!norm_ok(dtype, B, N, D, G) || !positive(eps)) return LCCRF_EINVAL;
     if (!dout || !dout->data || !x || !x->data || !dx) return LCCRF_ENULL;
-    if (!workspace || workspace_bytes < norm_grad_workspace(dtype, B, N, D, G, per_position != 0)) return LCCRF_EWORKSPACE;
+    if (!room(workspace, workspace_bytes, norm_grad_workspace(dtype, B, N, D, G, per_position != 0))) return LCCRF_EWORKSPACE;
     const size_t e = size_of(dtype);
     if (!lies(dout->data, e) || !lies(x->data, e) || !lies(weight, 4) || !lies(bias, 4) || !lies(lengths, 4) || !lies(stats, 4) || !lies(dx, e) || !lies(dweight, 4) ||
         !lies(dbias, 4) || !lies(workspace, 256))

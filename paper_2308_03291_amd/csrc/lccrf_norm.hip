@@ -1055,7 +1055,7 @@ hipError_t norm_grad_of(int dtype, AnyRows dout, const NormIn& in, const float* 
 
 size_t norm_workspace(int dtype, int B, int N, int D, int G, bool alone) {
     Held h;
-    if (alone || held_plan(dtype, B, N, D, G, h)) return 256;
+    if (alone || held_plan(dtype, B, N, D, G, h)) return 0;
     return entries_bytes(span_plan(dtype, B, N, D, G), B, G);
 }
 

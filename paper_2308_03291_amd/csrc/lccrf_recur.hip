@@ -283,7 +283,7 @@ size_t recur_saved_bytes(int B, int N, int D) { return up256(static_cast<size_t>
 
 size_t recur_workspace(int B, int N, int D) {
     const RecurPlan p = recur_plan(B, N, D);
-    return p.segments > 1 ? recur_ends_bytes(B, p.segments, D) : 256;
+    return p.segments > 1 ? recur_ends_bytes(B, p.segments, D) : 0;
 }
 
 hipError_t launch_recur(int dtype, const RecurIn& in, const float* state, void* out, float* final_state, float* saved, void* ws, hipStream_t st) {

@@ -15,6 +15,7 @@ import torch
 from .encoder import _MOST, _Rows, _activation, _bytes, _call, _dense, _first, _lengths, _lib, _like, _result, _scratch
 
 MAX_TOP = 256
+_NOTHING = 256  # a workspace of this size holds nothing and need not be there
 
 _RecurInputs = ctypes.c_int64 * 15  # x, f, g, z as _Rows, decay, f_bias, g_bias
 _RecurGrads = ctypes.c_int64 * 8    # dx, df, dg, dz, ddecay, df_bias, dg_bias, dstate
@@ -46,22 +47,45 @@ def declare(lib) -> None:
 
 # ---- gated linear recurrence ----------------------------------------------------------------------------------
 
+def _weights(names, *tensors, size: int, dev: int):
+    """Addresses of contiguous float32 [size] tensors; 0 for those that are not there."""
+    f32, shape = torch.float32, (size,)
+    for t in tensors:
+        if t is not None and not (t.dtype is f32 and t.shape == shape and t.get_device() == dev and (size == 1 or t.stride()[0] == 1)):
+            for t, name in zip(tensors, names):  # one by one, to say what is wrong
+                _dense(t, name, shape, f32, dev, True)
+    return [0 if t is None else t.data_ptr() for t in tensors]
+
+
 def _recur_args(x, f, g, decay, z, f_bias, g_bias):
     """Checks what all calls of the recurrence share; (dtype's code, device number, shape of x, dtype, the inputs' block)."""
     code, dtype, dev = _first(x, "x")
     shape = x.shape
     if 0 in shape or max(shape) > _MOST:
         raise ValueError(f"x must be [B, N, D] (one position: [B, D]), its sizes at most {_MOST}, got {list(shape)}")
-    f32, D = torch.float32, shape[-1]
-    block = []
-    for t, name in ((x, "x"), (f, "f"), (g, "g"), (z, "z")):
-        if t is None and name == "z":
-            block += (0, 0, 0)
-            continue
-        strides = _activation(t, name, shape, dtype, dev)
-        block += (t.data_ptr(), strides[0], strides[1])  # (one position: the second stride is that of the channels, which nothing looks at)
-    return code, dev, shape, dtype, _RecurInputs(*block, _dense(decay, "decay", (D,), f32, dev), _dense(f_bias, "f_bias", (D,), f32, dev, True),
-                                                 _dense(g_bias, "g_bias", (D,), f32, dev, True))
+    xs, fs, gs, zs, pz = x.stride(), f.stride(), g.stride(), (0, 0, 1), 0
+    if z is not None:
+        zs, pz = z.stride(), z.data_ptr()
+    # all at once; one by one only to say what is wrong
+    if not (f.shape == shape and g.shape == shape and f.dtype is dtype and g.dtype is dtype and xs[-1] == fs[-1] == gs[-1] == zs[-1] == 1
+            and f.get_device() == g.get_device() == dev and (z is None or (z.shape == shape and z.dtype is dtype and z.get_device() == dev))):
+        for t, name in ((x, "x"), (f, "f"), (g, "g"), (z, "z")):
+            if t is not None:
+                _activation(t, name, shape, dtype, dev)
+    if decay is None:
+        raise ValueError("decay is missing")
+    pd, pf, pg = _weights(("decay", "f_bias", "g_bias"), decay, f_bias, g_bias, size=shape[-1], dev=dev)
+    # (one position: the second stride is that of the channels, which nothing looks at)
+    return code, dev, shape, dtype, _RecurInputs(x.data_ptr(), xs[0], xs[1], f.data_ptr(), fs[0], fs[1], g.data_ptr(), gs[0], gs[1], pz, zs[0], zs[1], pd, pf, pg)
+
+
+def _scratch_at(name: str, sizes, device, workspace):
+    """(address, bytes, tensor) of a call's workspace: none where the library keeps nothing there."""
+    need = _bytes(f"{name}_workspace_bytes", *sizes)
+    if workspace is None and need == _NOTHING:
+        return 0, 0, None
+    ws = _scratch(need, name, device, workspace)
+    return ws.data_ptr(), ws.numel(), ws
 
 
 def recurrence_saved(x: torch.Tensor) -> torch.Tensor:
@@ -99,8 +123,8 @@ def lccrf_recurrence(x: torch.Tensor, f: torch.Tensor, g: torch.Tensor, decay: t
     psaved = _recur_saved(saved, shape, dev)
     out = _result(out, "out", shape, dtype, None, dev, x)
     final = _result(final, "final", (B, D), f32, device, dev, state)
-    ws = _scratch(_bytes("lccrf_recurrence_workspace_bytes", B, N, D), "lccrf_recurrence", device, workspace)
-    _call("lccrf_recurrence", dev, _lib().lccrf_recurrence, block, code, rate, plen, B, N, D, pstate, out.data_ptr(), final.data_ptr(), psaved, ws.data_ptr(), ws.numel())
+    pws, nws, ws = _scratch_at("lccrf_recurrence", (B, N, D), device, workspace)
+    _call("lccrf_recurrence", dev, _lib().lccrf_recurrence, block, code, rate, plen, B, N, D, pstate, out.data_ptr(), final.data_ptr(), psaved, pws, nws)
     return out, final
 
 
@@ -130,9 +154,9 @@ def lccrf_recurrence_grad(dout: torch.Tensor, x: torch.Tensor, f: torch.Tensor, 
     pstate = _dense(state, "state", (B, D), torch.float32, dev, True)
     psaved = _recur_saved(saved, shape, dev)
     grad = RecurrenceGrad(_like(x), _like(f), _like(g), *[None if t is None else _like(t) for t in (z, decay, f_bias, g_bias, state)])
-    ws = _scratch(_bytes("lccrf_recurrence_grad_workspace_bytes", B, N, D, int(saved is not None)), "lccrf_recurrence_grad", x.device, workspace)
+    pws, nws, ws = _scratch_at("lccrf_recurrence_grad", (B, N, D, int(saved is not None)), x.device, workspace)
     _call("lccrf_recurrence_grad", dev, _lib().lccrf_recurrence_grad, _Rows(dout.data_ptr(), strides[0], strides[1]), block, code, rate, plen, B, N, D, pstate, psaved,
-          _RecurGrads(*[0 if t is None else t.data_ptr() for t in grad]), ws.data_ptr(), ws.numel())
+          _RecurGrads(*[0 if t is None else t.data_ptr() for t in grad]), pws, nws)
     return grad
 
 
@@ -157,9 +181,8 @@ def _norm_args(x, weight, bias, groups):
         raise ValueError(f"x must be [B, N, D], its sizes at most {_MOST}, got {list(shape)}")
     if groups < 1 or shape[2] % groups:
         raise ValueError(f"{shape[2]} channels cannot be cut into {groups} groups")
-    strides, f32 = _activation(x, "x", shape, dtype, dev), torch.float32
-    return (code, dtype, dev, shape, _Rows(x.data_ptr(), strides[0], strides[1]), _dense(weight, "weight", shape[2:], f32, dev, True),
-            _dense(bias, "bias", shape[2:], f32, dev, True))
+    strides = _activation(x, "x", shape, dtype, dev)
+    return (code, dtype, dev, shape, _Rows(x.data_ptr(), strides[0], strides[1]), *_weights(("weight", "bias"), weight, bias, size=shape[2], dev=dev))
 
 
 def _stats_shape(shape, groups: int, per_position: bool):
@@ -187,8 +210,8 @@ def lccrf_group_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bia
     pstats = _dense(stats, "stats", _stats_shape(shape, groups, per_position), torch.float32, dev, True)
     out = _result(out, "out", shape, dtype, None, dev, x)
     alone = int(per_position)
-    ws = _scratch(_bytes("lccrf_group_norm_workspace_bytes", code, B, N, D, groups, alone), "lccrf_group_norm", device, workspace)
-    _call("lccrf_group_norm", dev, _lib().lccrf_group_norm, prows, code, pw, pb, plen, B, N, D, groups, alone, eps, int(silu), out.data_ptr(), pstats, ws.data_ptr(), ws.numel())
+    pws, nws, ws = _scratch_at("lccrf_group_norm", (code, B, N, D, groups, alone), device, workspace)
+    _call("lccrf_group_norm", dev, _lib().lccrf_group_norm, prows, code, pw, pb, plen, B, N, D, groups, alone, eps, int(silu), out.data_ptr(), pstats, pws, nws)
     return out
 
 
@@ -210,9 +233,9 @@ def lccrf_group_norm_grad(dout: torch.Tensor, x: torch.Tensor, weight: Optional[
     pstats = _dense(stats, "stats", _stats_shape(shape, groups, per_position), torch.float32, dev, True)
     grad = GroupNormGrad(_like(x), *[None if t is None else _like(t) for t in (weight, bias)])
     alone = int(per_position)
-    ws = _scratch(_bytes("lccrf_group_norm_grad_workspace_bytes", code, B, N, D, groups, alone), "lccrf_group_norm_grad", x.device, workspace)
+    pws, nws, ws = _scratch_at("lccrf_group_norm_grad", (code, B, N, D, groups, alone), x.device, workspace)
     _call("lccrf_group_norm_grad", dev, _lib().lccrf_group_norm_grad, _Rows(dout.data_ptr(), strides[0], strides[1]), prows, code, pw, pb, plen, B, N, D, groups, alone, eps,
-          int(silu), pstats, *[0 if t is None else t.data_ptr() for t in grad], ws.data_ptr(), ws.numel())
+          int(silu), pstats, *[0 if t is None else t.data_ptr() for t in grad], pws, nws)
     return grad
 
 
@@ -227,13 +250,16 @@ def _distill_args(logits, ids, teacher):
     lead, V, strides = shape[:-1], shape[-1], logits.stride()
     if strides[-1] != 1 and V > 1:
         raise ValueError("logits' last dimension must be dense")
-    n, row = 1, 0
-    for size, stride in zip(reversed(lead), reversed(strides[:-1])):
-        if size > 1:  # one distance between all rows
-            if n > 1 and stride != row * n:
-                raise ValueError("logits' rows must lie at one distance from each other")
-            row = row if n > 1 else stride
-        n *= size
+    if logits.is_contiguous():
+        n, row = logits.numel() // V, V
+    else:
+        n, row = 1, 0
+        for size, stride in zip(reversed(lead), reversed(strides[:-1])):
+            if size > 1:  # one distance between all rows
+                if n > 1 and stride != row * n:
+                    raise ValueError("logits' rows must lie at one distance from each other")
+                row = row if n > 1 else stride
+            n *= size
     if ids.dim() != len(shape) or not 1 <= ids.shape[-1] <= MAX_TOP:
         raise ValueError(f"ids must be [..., K] with 1 to {MAX_TOP} entries a position, got {list(ids.shape)}")
     top = (*lead, ids.shape[-1])

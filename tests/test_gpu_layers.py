@@ -343,7 +343,7 @@ def test_distill(crf, t, kind, n, V, K):
         with_loss = torch.full_like(loss, float("nan"))
         dlogits = crf.lccrf_distill_grad(dloss, logits, ids, teacher, temperature=temperature, loss=with_loss)
         check(dlogits, want["dlogits"], "dlogits")
-        assert torch.equal(loss, with_loss)
+        check(with_loss, want["loss"], "loss with the gradient")  # (summed in another order than by itself)
         check(crf.lccrf_distill_grad(dloss, logits, ids, teacher, temperature=temperature, lse=lse), given["dlogits"], "dlogits of lse")
         over = logits.clone().contiguous()
         assert torch.equal(crf.lccrf_distill_grad(dloss, over, ids, teacher, temperature=temperature, out=over), dlogits), "over the logits"
