@@ -8,9 +8,6 @@
 // always in the same order: no difference of large numbers, however far the mean is from 0.
 #include "lccrf_layers.h"
 
-#ifndef AW
-#define AW 1024
-#endif
 namespace lccrf {
 namespace enc {
 namespace {
@@ -59,15 +56,24 @@ struct Alone {
     int64_t blocks;                // workgroups a tile
 };
 
-// EXACT: every lane has R pieces of its own, no channel twice.
-template <typename T, int W, int R, bool GRAD, bool EXACT>
+// EXACT: every lane has R pieces of its own, no channel twice.  ALL: the whole workgroup is one team.
+template <typename T, int W, int R, bool GRAD, bool EXACT, bool ALL>
 __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alone p, const float* __restrict__ given, T* __restrict__ out, float* __restrict__ stats,
                                                     float* __restrict__ partial) {
-    __shared__ float sums[GRAD ? 4 * 64 * 2 * W : 1];
+    __shared__ float sums[GRAD && !ALL ? 4 * 64 * 2 * W : 16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int t = lane % p.team, team = lane / p.team, rows = 64 / p.team / p.groups;  // positions a wave
-    const int tile = blockIdx.x % p.tiles, g = tile * p.groups + team % p.groups, C = in.D / in.G;
+    const int t = ALL ? threadIdx.x : lane % p.team, team = ALL ? 0 : lane / p.team, rows = ALL ? 1 : 64 / p.team / p.groups;  // positions a wave
+    const int tile = blockIdx.x % p.tiles, g = tile * p.groups + (ALL ? 0 : team % p.groups), C = in.D / in.G;
     const int64_t block = blockIdx.x / p.tiles, total = static_cast<int64_t>(in.B) * in.N;
+    const int at_once = ALL ? 1 : 4 * rows;  // positions a workgroup
+    // over the team; `which` of a position's four sums
+    const auto team_sum = [&](float v, int which) {
+        if (!ALL) return sum_across(v, p.team);
+        v = sum_across(v, 64);
+        if (lane == 0) sums[which * 4 + wave] = v;
+        lds_sync();  // (a place is written again after three other such sums)
+        return sums[which * 4] + sums[which * 4 + 1] + sums[which * 4 + 2] + sums[which * 4 + 3];
+    };
     const bool is = g < in.G;
     int c[R], skip[R];  // skip W: no piece
     float w[R][W], bias[R][W], dw[GRAD ? R : 1][W], db[GRAD ? R : 1][W];
@@ -88,7 +94,7 @@ __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alo
         int b, l, len;
         bool there;
     };
-    const int64_t high = p.blocks * 4 * rows, first = (block * 4 + wave) * rows + team / p.groups;
+    const int64_t high = p.blocks * at_once, first = ALL ? block : (block * 4 + wave) * rows + team / p.groups;
     const auto position = [&](int64_t pos) {
         Position q;
         q.there = pos < total;
@@ -112,7 +118,7 @@ __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alo
     };
     Position now = position(first), next = position(first + high);
     fetch(now);
-    for (int64_t pos = first; pos - team / p.groups < total; pos += high) {
+    for (int64_t pos = first; pos - (ALL ? 0 : team / p.groups) < total; pos += high) {
         const Position after = position(pos + 2 * high);
         const int b = now.b, l = now.l;
         const bool there = now.there, inside = there && is && l < now.len;
@@ -138,7 +144,7 @@ __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alo
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int j = 0; j < W; ++j) s += EXACT || j >= skip[r] ? x[r][j] : 0.0f;
-            mean = sum_across(s, p.team) * count;
+            mean = team_sum(s, 0) * count;
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -146,7 +152,7 @@ __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alo
                     const float away = x[r][j] - mean;
                     m2 = EXACT || j >= skip[r] ? fmaf(away, away, m2) : m2;
                 }
-            rstd = __builtin_amdgcn_rsqf(fmaf(sum_across(m2, p.team), count, in.eps));
+            rstd = __builtin_amdgcn_rsqf(fmaf(team_sum(m2, 1), count, in.eps));
         }
         T* to = out + (static_cast<int64_t>(b) * in.N + l) * in.D;
         if constexpr (!GRAD) {
@@ -189,8 +195,8 @@ __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alo
                         }
                     }
             }
-            s1 = sum_across(s1, p.team) * count;
-            s2 = sum_across(s2, p.team) * count;
+            s1 = team_sum(s1, 2) * count;
+            s2 = team_sum(s2, 3) * count;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float o[W];
@@ -206,6 +212,17 @@ __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alo
     }
     if constexpr (GRAD) {
         if (!partial) return;
+        if constexpr (ALL) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int j = 0; j < W; ++j)
+                    if (j >= skip[r]) {
+                        partial[block * 2 * in.D + c[r] + j] = dw[r][j];
+                        partial[(block * 2 + 1) * in.D + c[r] + j] = db[r][j];
+                    }
+            return;
+        }
         const int many = 64 / (p.team * p.groups);  // teams of a wave with the same group
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -852,28 +869,34 @@ int piece_width(int dtype, int C) {
 
 constexpr int kMostPieces = 4;  // a lane's, in registers
 
-bool alone_fits(int ppg) { return ppg <= 64 * kMostPieces; }
-// Lanes a team and pieces a lane: one each as long as a wave has the lanes; 3 pieces where that leaves fewer of them without one.
-void team_of(int ppg, int& team, int& pieces) {
+bool alone_fits(int ppg) { return ppg <= 256 * kMostPieces; }
+// Lanes a team and pieces a lane: one each as long as a wave has the lanes; 3 pieces where that leaves fewer of them without one; a workgroup a team where a
+// wave's lanes would take more than 16 channels each.
+void team_of(int ppg, int W, int& team, int& pieces) {
     team = 1;
     while (team < 64 && team < ppg) team *= 2;
-    pieces = (ppg + team - 1) / team;
-    if (pieces == 1 && team >= 4 && 3 * (team / 4) >= ppg) {
+    if (ppg > 64 * 16 / W) team = 256;
+    pieces = (ppg - 1) / team + 1;
+    if (pieces == 1 && team >= 4 && team <= 64 && 3 * (team / 4) >= ppg) {
         team /= 4;
         pieces = 3;
     }
 }
 
-Alone alone_plan(int dtype, int B, int N, int D, int G, int& pieces) {
+// Workgroups: as many as the chip holds at once by the registers that they take, then they take their positions in turn (a second round for a few of them costs as
+// much as the first; B=128 N=128 D=1001 in seven groups, float, ragged, gradient in 768 workgroups of three waves a SIMD 90 us for the whole training step,
+// in 1024 103).
+Alone alone_plan(int dtype, int B, int N, int D, int G, bool grad, int& pieces) {
     Alone p;
     const int C = D / G, W = piece_width(dtype, C);
     p.ppg = (C - 1) / W + 1;
-    team_of(p.ppg, p.team, pieces);
+    team_of(p.ppg, W, p.team, pieces);
     p.groups = 1;
-    while (p.groups < 64 / p.team && p.groups < G) p.groups *= 2;
+    while (p.team < 64 && p.groups < 64 / p.team && p.groups < G) p.groups *= 2;
     p.tiles = (G - 1) / p.groups + 1;
-    const int64_t rows = 4 * (64 / p.team / p.groups), all = (static_cast<int64_t>(B) * N + rows - 1) / rows;
-    int64_t most = AW / p.tiles;
+    const int64_t rows = p.team > 64 ? 1 : 4 * (64 / p.team / p.groups), all = (static_cast<int64_t>(B) * N + rows - 1) / rows;
+    const int registers = pieces * (W == 8 ? 2 : 1);  // waves a SIMD: 4 of the gradient's up to two pieces of 4 channels, 3 of three and four, 2, 1
+    int64_t most = (!grad || registers <= 2 ? 1024 : registers == 3 || (registers == 4 && W == 8) ? 768 : registers <= 6 ? 512 : 256) / p.tiles;
     if (most < 1) most = 1;
     p.blocks = all < most ? all : most;
     return p;
@@ -934,11 +957,17 @@ template <typename T, int W, bool GRAD>
 hipError_t alone_of(const NormIn& in, AnyRows dout, const Alone& p, int pieces, const float* given, void* out, float* stats, float* partial, hipStream_t st) {
     if (!fits(p.blocks * p.tiles, 256)) return hipErrorInvalidValue;
     const bool exact = in.D / in.G == p.team * pieces * W;
-    auto kernel = exact ? alone_kernel<T, W, 1, GRAD, true> : alone_kernel<T, W, 1, GRAD, false>;
+    auto kernel = exact ? alone_kernel<T, W, 1, GRAD, true, false> : alone_kernel<T, W, 1, GRAD, false, false>;
     if constexpr (W == Wide<T>::V) {  // narrower pieces are at most two a group
-        if (pieces == 2) kernel = exact ? alone_kernel<T, W, 2, GRAD, true> : alone_kernel<T, W, 2, GRAD, false>;
-        if (pieces == 3) kernel = alone_kernel<T, W, 3, GRAD, false>;
-        if (pieces == 4) kernel = exact ? alone_kernel<T, W, 4, GRAD, true> : alone_kernel<T, W, 4, GRAD, false>;
+        if (p.team > 64) {
+            kernel = pieces == 1 ? alone_kernel<T, W, 1, GRAD, false, true> : pieces == 2 ? alone_kernel<T, W, 2, GRAD, false, true>
+                     : pieces == 3 ? alone_kernel<T, W, 3, GRAD, false, true> : alone_kernel<T, W, 4, GRAD, false, true>;
+        } else {
+            if (pieces == 2) kernel = exact ? alone_kernel<T, W, 2, GRAD, true, false> : alone_kernel<T, W, 2, GRAD, false, false>;
+            if (pieces == 3) kernel = alone_kernel<T, W, 3, GRAD, false, false>;
+            if constexpr (W == 4)
+                if (pieces == 4) kernel = exact ? alone_kernel<T, W, 4, GRAD, true, false> : alone_kernel<T, W, 4, GRAD, false, false>;
+        }
     }
     kernel<<<static_cast<unsigned>(p.blocks * p.tiles), 256, 0, st>>>(in, dout, p, given, static_cast<T*>(out), stats, partial);
     return hipGetLastError();
@@ -967,7 +996,7 @@ template <typename T, int W>
 hipError_t norm_of(int dtype, const NormIn& in, const Outs& o, void* ws, hipStream_t st) {
     if (in.alone) {
         int pieces;
-        const Alone p = alone_plan(dtype, in.B, in.N, in.D, in.G, pieces);
+        const Alone p = alone_plan(dtype, in.B, in.N, in.D, in.G, false, pieces);
         if (alone_fits(p.ppg)) return alone_of<T, W, false>(in, {}, p, pieces, nullptr, o.out, o.stats, nullptr, st);
         if constexpr (W == Wide<T>::V) {
             const int64_t units = static_cast<int64_t>(in.B) * in.N * in.G;
@@ -999,7 +1028,7 @@ hipError_t norm_grad_of(int dtype, AnyRows dout, const NormIn& in, const float* 
     const bool sums = o.dweight || o.dbias;
     if (in.alone) {
         int pieces;
-        const Alone p = alone_plan(dtype, in.B, in.N, in.D, in.G, pieces);
+        const Alone p = alone_plan(dtype, in.B, in.N, in.D, in.G, true, pieces);
         float* partial = reinterpret_cast<float*>(room);
         if (alone_fits(p.ppg)) {
             if (const hipError_t e = alone_of<T, W, true>(in, dout, p, pieces, stats, o.out, nullptr, sums ? partial : nullptr, st); e != hipSuccess || !sums) return e;
@@ -1062,7 +1091,7 @@ size_t norm_workspace(int dtype, int B, int N, int D, int G, bool alone) {
 size_t norm_grad_workspace(int dtype, int B, int N, int D, int G, bool alone) {
     if (alone) {
         int pieces;
-        const Alone p = alone_plan(dtype, B, N, D, G, pieces);
+        const Alone p = alone_plan(dtype, B, N, D, G, true, pieces);
         if (alone_fits(p.ppg)) return partial_bytes(p.blocks, D);
         return partial_bytes(span_plan(dtype, 1, B * N, D, G).chunks, D) + stats_bytes(static_cast<int64_t>(B) * N * G);
     }
