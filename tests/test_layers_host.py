@@ -1,0 +1,216 @@
+"""The layers of include/lccrf_layers.h without a GPU: what their entry points refuse, what they ask for, and the 64-bit reference of the GPU
+tests against automatic differentiation and differences."""
+import ctypes
+import math
+import os
+
+import pytest
+import torch
+
+import layers_reference as ref
+from paper_2308_03291_amd import binding, layers
+from paper_2308_03291_amd.encoder import _Rows
+
+EINVAL, ENULL, EWS, EALIGN = -1, -2, -3, -4
+FAKE = 4096  # an aligned "pointer" that is never dereferenced on these paths
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(binding.LIB_PATH):
+        from paper_2308_03291_amd import build_ext
+        build_ext.build()
+    return binding.load_library()
+
+
+def rows(data=FAKE):
+    return ctypes.byref(_Rows(data or 0, 8, 8))
+
+
+def inputs(x=FAKE, f=FAKE, g=FAKE, z=None, decay=FAKE, f_bias=FAKE, g_bias=FAKE):
+    return ctypes.byref(layers._RecurInputs(*[v for p in (x, f, g, z) for v in (p or 0, 8, 8)], decay or 0, f_bias or 0, g_bias or 0))
+
+
+def test_recurrence_refuses(lib):
+    assert lib.lccrf_recurrence_saved_bytes(3, 17, 64) == 3 * 3 * 64 * 4  # the states in front of every eighth position
+    assert lib.lccrf_recurrence_workspace_bytes(2, 4, 8) == 256
+    long = lib.lccrf_recurrence_workspace_bytes(1, 100000, 8)
+    assert long > 256 and long % 256 == 0
+    for size in (lib.lccrf_recurrence_saved_bytes, lib.lccrf_recurrence_workspace_bytes, lambda *a: lib.lccrf_recurrence_grad_workspace_bytes(*a, 0)):
+        assert [size(0, 4, 8), size(2, 0, 8), size(2, 4, 0), size(2, 4, (1 << 22) + 1), size(1 << 16, 1 << 16, 8)] == [0] * 5
+
+    def call(block=None, dt=0, rate=8.0, lengths=None, B=2, N=4, D=8, state=FAKE, out=FAKE, fin=FAKE, saved=None, ws=None, n=0):
+        return lib.lccrf_recurrence(block or inputs(), dt, rate, lengths, B, N, D, state, out, fin, saved, ws, n, None)
+
+    assert [call(dt=2), call(B=0), call(N=0), call(D=0), call(D=(1 << 22) + 1), call(B=1 << 16, N=1 << 16)] == [EINVAL] * 6
+    assert [call(rate=r) for r in (0.0, -1.0, INF, NAN)] == [EINVAL] * 4
+    assert [call(out=None), call(inputs(x=None)), call(inputs(f=None)), call(inputs(g=None)), call(inputs(decay=None))] == [ENULL] * 5
+    assert lib.lccrf_recurrence(None, 0, 8.0, None, 2, 4, 8, FAKE, FAKE, FAKE, None, None, 0, None) == ENULL
+    assert [call(N=100000, B=1), call(N=100000, B=1, ws=FAKE, n=long - 257)] == [EWS] * 2
+    assert [call(saved=FAKE + 64), call(ws=FAKE + 8), call(lengths=FAKE + 2), call(state=FAKE + 2), call(out=FAKE + 2), call(fin=FAKE + 1), call(inputs(x=FAKE + 2)),
+            call(inputs(z=FAKE + 2)), call(inputs(f_bias=FAKE + 1))] == [EALIGN] * 9
+    big, small = (lib.lccrf_recurrence_grad_workspace_bytes(2, 40, 8, k) for k in (0, 1))
+    assert big > small > 256
+
+    def grad(block=None, dout=rows(), rate=1.0, state=FAKE, saved=FAKE, ws=FAKE, n=small, D=8, **other):
+        values = {k: FAKE for k in ("dx", "df", "dg", "dz", "ddecay", "df_bias", "dg_bias", "dstate")} | {"dz": None} | other
+        return lib.lccrf_recurrence_grad(dout, block or inputs(), 0, rate, None, 2, 40, D, state, saved, layers._RecurGrads(*[v or 0 for v in values.values()]), ws, n, None)
+
+    assert [grad(dz=FAKE), grad(inputs(z=FAKE)), grad(state=None), grad(rate=0.0), grad(D=0)] == [EINVAL] * 5
+    assert [grad(dout=None), grad(dout=rows(None)), grad(dx=None), grad(df=None), grad(dg=None), grad(ddecay=None), grad(inputs(g=None))] == [ENULL] * 7
+    assert [grad(ws=None), grad(n=small - 257), grad(saved=None)] == [EWS] * 3
+    assert [grad(dx=FAKE + 2), grad(ddecay=FAKE + 2), grad(saved=FAKE + 64), grad(ws=FAKE + 16), grad(dout=rows(FAKE + 1)), grad(dstate=FAKE + 2)] == [EALIGN] * 6
+
+    def step(block=None, rate=8.0, B=2, D=8, state=FAKE, out=FAKE):
+        return lib.lccrf_recurrence_step(block or inputs(), 0, rate, B, D, state, out, None)
+
+    assert [step(B=0), step(D=0), step(rate=NAN)] == [EINVAL] * 3
+    assert [step(state=None), step(out=None), step(inputs(x=None))] == [ENULL] * 3
+    assert [step(state=FAKE + 2), step(out=FAKE + 2), step(inputs(g=FAKE + 2))] == [EALIGN] * 3
+
+
+def test_group_norm_refuses(lib):
+    for alone in (0, 1):
+        assert lib.lccrf_group_norm_workspace_bytes(0, 2, 4, 8, 2, alone) == 256
+        for size in (lib.lccrf_group_norm_workspace_bytes, lib.lccrf_group_norm_grad_workspace_bytes):
+            assert [size(2, 2, 4, 8, 2, alone), size(0, 0, 4, 8, 2, alone), size(0, 2, 4, 8, 3, alone), size(0, 2, 4, 8, 0, alone), size(0, 2, 4, 8, 16, alone),
+                    size(0, 1 << 16, 1 << 16, 8, 1, alone)] == [0] * 6
+    need = lib.lccrf_group_norm_workspace_bytes(0, 64, 512, 1024, 32, 0)
+    assert need > 256 and need % 256 == 0
+
+    def call(x=rows(), dt=0, w=FAKE, b=FAKE, B=2, N=4, D=8, G=2, eps=1e-5, out=FAKE, stats=None, ws=None, n=0):
+        return lib.lccrf_group_norm(x, dt, w, b, None, B, N, D, G, 0, eps, 1, out, stats, ws, n, None)
+
+    assert [call(dt=3), call(B=0), call(N=0), call(D=0), call(G=0), call(G=3)] == [EINVAL] * 6
+    assert [call(eps=e) for e in (0.0, -1e-5, INF, NAN)] == [EINVAL] * 4
+    assert [call(x=None), call(x=rows(None)), call(out=None)] == [ENULL] * 3
+    assert [call(B=64, N=512, D=1024, G=32), call(B=64, N=512, D=1024, G=32, ws=FAKE, n=need - 257)] == [EWS] * 2
+    assert [call(x=rows(FAKE + 1)), call(w=FAKE + 2), call(b=FAKE + 1), call(out=FAKE + 2), call(stats=FAKE + 2), call(ws=FAKE + 4)] == [EALIGN] * 6
+    need = lib.lccrf_group_norm_grad_workspace_bytes(1, 2, 4, 8, 2, 1)
+    assert need > 256
+
+    def grad(dout=rows(), x=rows(), eps=1e-5, stats=None, dx=FAKE, dw=FAKE, ws=FAKE, n=need, G=2):
+        return lib.lccrf_group_norm_grad(dout, x, 1, FAKE, FAKE, None, 2, 4, 8, G, 1, eps, 1, stats, dx, dw, FAKE, ws, n, None)
+
+    assert [grad(G=5), grad(eps=0.0)] == [EINVAL] * 2
+    assert [grad(dout=None), grad(dout=rows(None)), grad(x=None), grad(dx=None)] == [ENULL] * 4
+    assert [grad(ws=None), grad(n=need - 257)] == [EWS] * 2
+    assert [grad(dx=FAKE + 1), grad(dw=FAKE + 2), grad(stats=FAKE + 1), grad(ws=FAKE + 8), grad(dout=rows(FAKE + 1))] == [EALIGN] * 5
+
+
+def test_distill_refuses(lib):
+    def call(logits=FAKE, dt=0, ids=FAKE, teacher=FAKE, n=4, V=10, K=3, t=1.0, loss=FAKE, lse=FAKE):
+        return lib.lccrf_distill(logits, 10, dt, ids, teacher, n, V, K, t, loss, lse, None)
+
+    assert [call(dt=2), call(n=-1), call(n=1 << 31), call(V=0), call(V=(1 << 30) + 1), call(K=0), call(K=257)] == [EINVAL] * 7
+    assert [call(t=t) for t in (0.0, -1.0, INF, NAN)] == [EINVAL] * 4
+    assert [call(logits=None), call(ids=None), call(teacher=None), call(loss=None), call(lse=None)] == [ENULL] * 5
+    assert [call(logits=FAKE + 2), call(ids=FAKE + 2), call(teacher=FAKE + 1), call(loss=FAKE + 2), call(lse=FAKE + 2)] == [EALIGN] * 5
+    assert call(n=0, logits=None, ids=None, teacher=None) == 0  # nothing to do, nothing enqueued
+
+    def grad(dloss=FAKE, logits=2 * FAKE, row=10, ids=FAKE, teacher=FAKE, n=4, V=10, K=3, t=1.0, lse=None, loss=None, out=3 * FAKE):
+        return lib.lccrf_distill_grad(dloss, logits, row, 0, ids, teacher, n, V, K, t, lse, loss, out, None)
+
+    assert [grad(V=0), grad(K=257), grad(t=INF), grad(out=2 * FAKE, row=11)] == [EINVAL] * 4
+    assert [grad(dloss=None), grad(logits=None), grad(ids=None), grad(teacher=None), grad(out=None)] == [ENULL] * 5
+    assert [grad(dloss=FAKE + 2), grad(lse=FAKE + 2), grad(loss=FAKE + 1), grad(out=FAKE + 2)] == [EALIGN] * 4
+
+
+def test_binding_refuses():
+    t = torch.zeros
+    i32 = torch.int32
+    for call in (lambda: binding.lccrf_recurrence(t(2, 3, 8), t(2, 3, 8), t(2, 3, 8), t(8)), lambda: binding.lccrf_recurrence(t(2, 8), t(2, 8), t(2, 8), t(8)),
+                 lambda: binding.lccrf_recurrence(t(2, 0, 8), t(2, 0, 8), t(2, 0, 8), t(8)), lambda: binding.recurrence_saved(t(2, 3)),
+                 lambda: binding.lccrf_recurrence_grad(t(2, 3, 8), t(2, 3, 8), t(2, 3, 8), t(2, 3, 8), t(8)), lambda: binding.lccrf_recurrence_step(t(2, 8), t(2, 8), t(2, 8), t(8), None, None, None, t(2, 8)),
+                 lambda: binding.lccrf_recurrence_step(t(2, 3, 8), t(2, 3, 8), t(2, 3, 8), t(8), None, None, None, t(2, 8)),
+                 lambda: binding.lccrf_group_norm(t(2, 3, 8), groups=2), lambda: binding.lccrf_group_norm(t(2, 8), groups=2), lambda: binding.lccrf_group_norm_grad(t(2, 3, 8), t(2, 3, 8), groups=3),
+                 lambda: binding.group_norm_stats(t(2, 8), 2), lambda: binding.group_norm_stats(t(2, 3, 8), 0),
+                 lambda: binding.lccrf_distill(t(2, 8), t(2, 3, dtype=i32), t(2, 3)), lambda: binding.lccrf_distill(t(8), t(3, dtype=i32), t(3)),
+                 lambda: binding.lccrf_distill(t(2, 8, dtype=torch.float16), t(2, 3, dtype=i32), t(2, 3)), lambda: binding.lccrf_distill_grad(t(2), t(2, 8), t(2, 3, dtype=i32), t(2, 3))):
+        with pytest.raises(ValueError):
+            call()
+
+
+# ---- the reference --------------------------------------------------------------------------------------------
+
+def _leaf(*shape, g):
+    return torch.randn(*shape, generator=g, dtype=torch.float64).requires_grad_(True)
+
+
+def test_reference_of_the_recurrence_is_its_own_derivative():
+    g = torch.Generator().manual_seed(1)
+    B, N, D = 3, 7, 5
+    x, f, gate, z = (_leaf(B, N, D, g=g) for _ in range(4))
+    lam, fb, gb, st = _leaf(D, g=g), _leaf(D, g=g), _leaf(D, g=g), _leaf(B, D, g=g)
+    lens, dout = torch.tensor([7, 0, 4]), torch.randn(B, N, D, generator=g, dtype=torch.float64)
+    u = -3.0 * torch.nn.functional.softplus(lam) * torch.sigmoid(f + fb)
+    h, loss = st, 0.0
+    for l in range(N):
+        alive = (lens > l)[:, None]
+        h = torch.where(alive, torch.exp(u[:, l]) * h + torch.sqrt(1 - torch.exp(2 * u[:, l])) * torch.sigmoid(gate[:, l] + gb) * x[:, l], h)
+        loss = loss + (torch.where(alive, h * torch.nn.functional.silu(z[:, l]), 0.0) * dout[:, l]).sum()
+    want = torch.autograd.grad(loss, (x, f, gate, z, lam, fb, gb, st))
+    got = ref.recurrence(x, f, gate, lam, z, fb, gb, lens, 3.0, st, dout)
+    for name, t in zip(("dx", "df", "dg", "dz", "ddecay", "df_bias", "dg_bias", "dstate"), want):
+        assert torch.allclose(got[name][0], t, rtol=1e-11, atol=1e-12), name
+        assert (got[name][1] >= 0).all()
+    assert torch.allclose(got["final"][0], h) and torch.allclose((got["out"][0] * dout).sum(), loss, rtol=1e-12)
+
+
+def test_reference_of_the_recurrence_by_differences():
+    g = torch.Generator().manual_seed(2)
+    r = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)  # noqa: E731
+    B, N, D = 2, 6, 3
+    args = {"x": r(B, N, D), "f": r(B, N, D), "g": r(B, N, D), "decay": r(D), "z": r(B, N, D), "f_bias": r(D), "g_bias": r(D), "lengths": torch.tensor([6, 3]), "rate": 8.0,
+            "state": r(B, D)}
+    dout = r(B, N, D)
+    got = ref.recurrence(**args, dout=dout)
+    for k, name in {"x": "dx", "f": "df", "g": "dg", "decay": "ddecay", "z": "dz", "f_bias": "df_bias", "g_bias": "dg_bias", "state": "dstate"}.items():
+        v = r(*args[k].shape)
+        loss = lambda s: (ref.recurrence(**(args | {k: args[k] + s * 1e-5 * v}))["out"][0] * dout).sum()  # noqa: E731
+        difference, formula = float((loss(1) - loss(-1)) / 2e-5), float((got[name][0] * v).sum())
+        assert abs(difference - formula) <= 1e-8 * (1 + abs(formula)) + 1e-7, name
+
+
+@pytest.mark.parametrize("alone", (False, True))
+@pytest.mark.parametrize("act", (False, True))
+def test_reference_of_the_group_norm_is_its_own_derivative(alone, act):
+    g = torch.Generator().manual_seed(3)
+    B, N, D, G = 3, 5, 8, 2
+    x, w, b = _leaf(B, N, D, g=g), _leaf(D, g=g), _leaf(D, g=g)
+    lens, dout = torch.tensor([5, 0, 2]), torch.randn(B, N, D, generator=g, dtype=torch.float64)
+    loss = 0.0
+    for i, n in enumerate(lens.tolist()):
+        for part in ([slice(l, l + 1) for l in range(n)] if alone else [slice(0, n)] if n else []):
+            v = x[i, part].view(-1, G, D // G)
+            over = (0, 2)
+            hat = (v - v.mean(over, keepdim=True)) / torch.sqrt(v.var(over, unbiased=False, keepdim=True) + 1e-3)
+            y = hat.reshape(-1, D) * w + b
+            loss = loss + ((torch.nn.functional.silu(y) if act else y) * dout[i, part]).sum()
+    want = torch.autograd.grad(loss, (x, w, b))
+    got = ref.group_norm(x, w, b, lens, G, 1e-3, act, alone, dout)
+    for name, t in zip(("dx", "dweight", "dbias"), want):
+        assert torch.allclose(got[name][0], t, rtol=1e-10, atol=1e-11), name
+    assert torch.allclose((got["out"][0] * dout).sum(), loss, rtol=1e-12)
+
+
+def test_reference_of_the_distillation_is_its_own_derivative():
+    g = torch.Generator().manual_seed(4)
+    n, V, K, t = 5, 7, 4, 2.5
+    x = _leaf(n, V, g=g)
+    ids = torch.randint(-3, V + 2, (n, K), generator=g)
+    ids[0] = torch.tensor([2, 2, 5, -1])  # a class twice
+    ids[3] = -1
+    v = torch.randn(n, K, generator=g, dtype=torch.float64)
+    v[1, 2] = -math.inf
+    dloss, loss = torch.randn(n, generator=g, dtype=torch.float64), 0.0
+    for i in range(n):
+        keep = (ids[i] >= 0) & (ids[i] < V) & (v[i] > -math.inf)
+        if keep.any():
+            q = torch.softmax(v[i][keep] / t, 0)
+            logp = torch.log_softmax(x[i] / t, 0)[ids[i][keep]]
+            loss = loss + dloss[i] * t * t * (q * (torch.log(q) - logp)).sum()
+    got = ref.distill(x, ids, v, t, dloss)
+    assert torch.allclose(got["dlogits"][0], torch.autograd.grad(loss, x)[0], rtol=1e-11, atol=1e-12)
+    assert torch.allclose((got["loss"][0] * dloss).sum(), loss, rtol=1e-12) and float(got["loss"][0][3]) == 0.0

@@ -1,0 +1,127 @@
+"""What the entry points of include/lccrf_layers.h launch, without a GPU: a stand-in for the HIP runtime (launch_recorder.cpp) writes launches
+down and lets the one fail that a test names.  Pointers are made up; the host code looks at none of them."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+LIB = os.path.join(os.path.dirname(HERE), "paper_2308_03291_amd", "liblccrf.so")
+OK, EINVAL, ELAUNCH = 0, -1, -5
+
+PROGRAM = r'''
+import ctypes, json, sys
+recorder = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
+lib = ctypes.CDLL(sys.argv[2])
+i, i64, f, vp, sz = ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t
+P, BIG = 4096, 1 << 62
+def by(*v):
+    return ctypes.byref((i64 * len(v))(*v))
+def rows(row=8):
+    return by(P, 8, row)
+def inputs(z=0, row=8):
+    return by(*[v for p in (P, P, P, z) for v in (p, 8, row)], P, P, P)
+def recur(B, N, D, saved=0, dt=0, row=8):
+    return lib.lccrf_recurrence(inputs(0, row), i(dt), f(8.0), None, i(B), i(N), i(D), None, vp(P), vp(P), vp(saved or None), vp(P), sz(BIG), None)
+def recur_grad(B, N, D, saved=0, dt=0, row=8):
+    return lib.lccrf_recurrence_grad(rows(row), inputs(0, row), i(dt), f(8.0), None, i(B), i(N), i(D), None, vp(saved or None), by(P, P, P, 0, P, P, P, 0), vp(P), sz(BIG), None)
+def recur_step(B, D, dt=0):
+    return lib.lccrf_recurrence_step(inputs(P), i(dt), f(8.0), i(B), i(D), vp(P), vp(P), None)
+def norm(B, N, D, G, alone, dt=0):
+    return lib.lccrf_group_norm(rows(), i(dt), vp(P), vp(P), None, i(B), i(N), i(D), i(G), i(alone), f(1e-5), i(1), vp(P), None, vp(P), sz(BIG), None)
+def norm_grad(B, N, D, G, alone, dt=0, stats=0):
+    return lib.lccrf_group_norm_grad(rows(), rows(), i(dt), vp(P), vp(P), None, i(B), i(N), i(D), i(G), i(alone), f(1e-5), i(1), vp(stats or None), vp(P), vp(P), vp(P), vp(P), sz(BIG), None)
+def distill(n, V, K, dt=0):
+    return lib.lccrf_distill(vp(P), i64(V), i(dt), vp(P), vp(P), i64(n), i(V), i(K), f(1.0), vp(P), vp(P), None)
+def distill_grad(n, V, K, dt=0, lse=0):
+    return lib.lccrf_distill_grad(vp(P), vp(P), i64(V), i(dt), vp(P), vp(P), i64(n), i(V), i(K), f(1.0), vp(lse or None), None, vp(2 * P), None)
+def size(name, *a):
+    fn = getattr(lib, name)
+    fn.restype = sz
+    return fn(*[i(v) for v in a])
+answers = []
+for call, launch in json.load(sys.stdin):
+    recorder.recorder_reset(launch, 0)
+    rc = globals()[call[0]](*call[1:])
+    made = []
+    for k in range(recorder.recorder_count()):
+        six = (ctypes.c_uint32 * 6)()
+        recorder.recorder_get(k, six)
+        made.append(list(six))
+    answers.append([rc, made])
+print(json.dumps(answers))
+'''
+
+
+@pytest.fixture(scope="module")
+def ask(tmp_path_factory):
+    """ask([(call, arguments ...), ...], launch): (status, launches) of every call."""
+    if not os.path.exists(LIB):
+        from paper_2308_03291_amd import build_ext
+        build_ext.build()
+    recorder = str(tmp_path_factory.mktemp("recorder") / "librecorder.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-o", recorder, os.path.join(HERE, "launch_recorder.cpp")], check=True)
+
+    def run(calls, launch=-1):
+        out = subprocess.run([sys.executable, "-c", PROGRAM, recorder, LIB], input=json.dumps([[list(c), launch] for c in calls]), capture_output=True, text=True, timeout=60)
+        assert out.returncode == 0, out.stderr
+        return [(rc, made) for rc, made in json.loads(out.stdout)]
+
+    return run
+
+
+SEVERAL = [("recur", 2, 5000, 30), ("recur", 1, 3000, 1), ("recur", 2, 5000, 30, 4096), ("recur_grad", 2, 5000, 30), ("recur_grad", 2, 5000, 30, 4096), ("recur_grad", 64, 20, 300, 4096),
+           ("norm", 64, 512, 1024, 32, 0), ("norm_grad", 64, 512, 1024, 32, 0), ("norm_grad", 64, 512, 1024, 32, 0, 1, 4096), ("norm_grad", 2, 9, 24, 3, 0), ("norm_grad", 2, 9, 24, 3, 1),
+           ("norm_grad", 2, 9, 40000, 2, 1), ("norm", 2, 5000, 40000, 1, 0)]
+SINGLE = [("recur", 2, 1, 30), ("recur", 2, 40, 30), ("recur_step", 3, 5), ("norm", 2, 9, 24, 3, 0), ("norm", 2, 9, 24, 3, 1), ("norm", 2, 9, 40000, 2, 1), ("distill", 5, 9, 3), ("distill", 5, 90000, 100),
+          ("distill_grad", 5, 9, 3), ("distill_grad", 5, 3000, 3), ("distill_grad", 5, 90000, 100), ("distill_grad", 5, 9000, 3, 1, 4096)]
+
+
+def test_a_launch_that_fails_is_reported(ask):
+    """Whichever it is; and nothing goes out behind it."""
+    for call in SEVERAL + SINGLE:
+        (rc, made), = ask([call])
+        assert rc == OK and (len(made) > 1) == (call in SEVERAL), (call, rc, made)
+        for k in range(len(made)):
+            (rc, got), = ask([call], launch=k)
+            assert rc == ELAUNCH, f"{call}: launch {k} of {len(made)} failed, status {rc}"
+            assert len(got) == k + 1, f"{call}: {len(got) - k - 1} launches behind the one that failed"
+
+
+def test_rows_far_apart_take_wide_tiles(ask):
+    """Narrow tiles reach their rows by 32-bit offsets: rows further apart go by wide tiles, in fewer workgroups, of the same workspace."""
+    for call in (("recur", 8, 100, 600), ("recur_grad", 8, 100, 600, 4096)):
+        (_, near), (_, far), (_, back) = ask([call, (*call, *[0] * (5 - len(call)), 0, 1 << 24), (*call, *[0] * (5 - len(call)), 0, -600)])
+        assert near[0][0] > far[0][0] == back[0][0]
+
+
+MOST = 2 ** 31 - 1024  # positions of a call
+
+
+def test_sizes_at_their_limits(ask):
+    """Every launch has a grid that the runtime takes (the stand-in refuses the others), or the call is refused before anything goes out."""
+    big = [("recur", 1, MOST, 1), ("recur", MOST, 1, 1), ("recur", 1, 1, 1 << 22), ("recur", 1, MOST, 1 << 22), ("recur", MOST // 64, 64, 3), ("recur_grad", 1, MOST, 1, 4096), ("recur_grad", MOST, 1, 1, 4096),
+           ("recur_grad", 1, 1, 1 << 22), ("recur_grad", 1, MOST, 130), ("recur_step", MOST, 1), ("recur_step", 1, 1 << 22, 1)]
+    for alone in (0, 1):
+        for shape in ((1, MOST, 1, 1), (MOST, 1, 1, 1), (1, 1, 1 << 22, 1), (1, 1, 1 << 22, 1 << 22), (1, 1, (1 << 22) - 2, 2), (1, MOST, 24, 3), (MOST // 7, 7, 64, 64), (1, MOST, 1 << 22, 1 << 11)):
+            big += [("norm", *shape, alone), ("norm_grad", *shape, alone), ("norm", *shape, alone, 1), ("norm_grad", *shape, alone, 1, 4096)]
+    big += [(name, n, V, K, dt) for name in ("distill", "distill_grad") for n, V in ((2 ** 31 - 1, 1), (2 ** 31 - 1, 130), (1, 1 << 30), (2 ** 31 - 1, 5000), (2 ** 31 - 1, 1 << 30)) for K in (1, 256) for dt in (0, 1)]
+    for call, (rc, made) in zip(big, ask(big)):
+        assert (rc == OK and made and all(v[0] * v[3] < 2 ** 32 and v[1] == v[2] == v[4] == v[5] == 1 or v[1] == 3 for v in made)) or (rc == EINVAL and made == []), (call, rc, made)
+    for call in (("recur", 1, MOST + 1, 1), ("recur", 1, 4, (1 << 22) + 1), ("norm", 1, MOST + 1, 1, 1, 0), ("distill", 1 << 31, 5, 1)):
+        (rc, made), = ask([call])
+        assert rc == EINVAL and made == [], call
+
+
+def test_workspaces_hold_what_is_asked_for(ask):
+    """What the launches of a call spread over comes from the same plan as its workspace: sizes are whole lines and grow with what they hold."""
+    def size(*c):
+        (rc, _), = ask([("size", *c)])
+        return rc
+    for B, N, D in ((1, 100000, 514), (4, 16384, 514), (1, MOST, 1), (2, 700, 64)):
+        assert size("lccrf_recurrence_workspace_bytes", B, N, D) % 256 == 0 and size("lccrf_recurrence_saved_bytes", B, N, D) >= B * -(-N // 8) * D * 4
+        with_saved, alone = (size("lccrf_recurrence_grad_workspace_bytes", B, N, D, k) for k in (1, 0))
+        forward = size("lccrf_recurrence_workspace_bytes", B, N, D) - 256
+        assert alone == with_saved + size("lccrf_recurrence_saved_bytes", B, N, D) + forward
