@@ -14,7 +14,20 @@ namespace {
 
 // ---- pieces ---------------------------------------------------------------------------------------------------
 
-template <typename T, int W> using Part = Piece<T, W, W == 1>;
+// (again: of registers that hold the piece for several passes, widened in each where it is used and not kept so.)
+template <typename T, int W> struct Part : Piece<T, W, W == 1> {
+    __device__ __forceinline__ void again(float (&o)[W]) {
+        if constexpr (W > 1) {
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(W * sizeof(T) / 4); ++i) {
+                uint32_t v = this->raw[i];
+                asm volatile("" : "+v"(v));
+                this->raw[i] = v;
+            }
+        }
+        this->get(o);
+    }
+};
 
 struct Place {
     int c, group, skip;  // first channel; its group; how many of the channels the piece before has too
@@ -26,7 +39,7 @@ struct Place {
 
 __device__ __forceinline__ float dsilu(float y) {
     const float s = sigmoid(y);
-    return s * fmaf(y, 1.0f - s, 1.0f);
+    return fmaf(s, fmaf(-y, s, y), s);  // s (1 + y (1 - s))
 }
 
 struct Moments { float n, mean, m2; };
@@ -334,7 +347,8 @@ __global__ __launch_bounds__(256) void wide_kernel(NormIn in, AnyRows dout, int 
 
 // ---- whole sequences in registers ------------------------------------------------------------------------------
 // Where a sequence's groups fit a workgroup's registers, they are read once: a workgroup has whole groups, `lx` pieces (a power of two) wide, of all positions, R
-// pieces a thread.
+// pieces a thread.  kRun tiles side by side run on one XCD, one after another: where a tile is half a cache line wide the line is then fetched from memory once.
+constexpr int kRun = 2;
 struct Held {
     int ppg, lx, groups, tiles, threads, pieces;  // pieces a group; across a workgroup; groups a workgroup, such tiles; its threads, pieces each
 };
@@ -361,23 +375,33 @@ __device__ __forceinline__ float held_sum(float v, const Held& p, float* lds, in
 }
 
 template <typename T, int W, int R, bool GRAD>
-__global__ __launch_bounds__(1024) void held_kernel(NormIn in, AnyRows dout, Held p, const float* __restrict__ given, T* __restrict__ out, float* __restrict__ stats,
+__global__ __launch_bounds__(R > 4 ? 512 : 1024) void held_kernel(NormIn in, AnyRows dout, Held p, const float* __restrict__ given, T* __restrict__ out, float* __restrict__ stats,
                                                                   float* __restrict__ partial) {
     extern __shared__ float lds[];  // held_sum's; GRAD: [threads][W]
     const int tx = threadIdx.x & (p.lx - 1), ty = threadIdx.x / p.lx, ly = blockDim.x / p.lx, C = in.D / in.G;
-    const int b = blockIdx.x / p.tiles, tile = blockIdx.x - b * p.tiles, group = tx / p.ppg, g = tile * p.groups + group;
+    const unsigned rest = blockIdx.x / 8, work = (rest / kRun * 8 + blockIdx.x % 8) * kRun + rest % kRun;
+    if (work >= static_cast<unsigned>(in.B) * p.tiles) return;
+    const int b = work / p.tiles, tile = work - b * p.tiles, group = tx / p.ppg, g = tile * p.groups + group;
     const bool is = group < p.groups && g < in.G;
     const Place at = Place::of<W>(is ? g * p.ppg + tx - group * p.ppg : 0, p.ppg, C);
     const int len = length_at(in.lengths, b, in.N);
+    const bool exact = at.skip == 0;
     Part<T, W> raw[R], draw[GRAD ? R : 1];
-    const T* px = line<T>(in.x, b, 0) + at.c;
-    const T* pd = GRAD ? line<T>(dout, b, 0) + at.c : nullptr;
+    {
+        const T* px = line<T>(in.x, b, 0) + at.c;
+        const T* pd = GRAD ? line<T>(dout, b, 0) + at.c : nullptr;
+        const int64_t x_step = ly * in.x.row, d_step = ly * dout.row;
+        px += ty * in.x.row;
+        if (GRAD) pd += ty * dout.row;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int l = ty + r * ly;
-        if (is && l < len) {
-            raw[r].load(px + l * in.x.row, W);
-            if (GRAD) draw[r].load(pd + l * dout.row, W);
+        for (int r = 0; r < R; ++r) {
+            if (r * ly >= len) break;
+            if (is && ty + r * ly < len) {
+                raw[r].load(px, W);
+                if (GRAD) draw[r].load(pd, W);
+            }
+            px += x_step;
+            pd += d_step;
         }
     }
     const float share = 1.0f / (static_cast<float>(len) * C);  // (len 0: nothing looks at it)
@@ -390,18 +414,26 @@ __global__ __launch_bounds__(1024) void held_kernel(NormIn in, AnyRows dout, Hel
         float s = 0.0f, q = 0.0f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
+            if (r * ly >= len) break;
             float x[W];
-            raw[r].get(x);
+            raw[r].again(x);
+            if (is && ty + r * ly < len) {
 #pragma unroll
-            for (int j = 0; j < W; ++j) s += is && ty + r * ly < len && j >= at.skip ? x[j] : 0.0f;
+                for (int j = 0; j < W; ++j) s += exact || j >= at.skip ? x[j] : 0.0f;
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
         mean = held_sum(s, p, lds, tx, group) * share;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
+            if (r * ly >= len) break;
             float x[W];
-            raw[r].get(x);
+            raw[r].again(x);
+            if (is && ty + r * ly < len) {
 #pragma unroll
-            for (int j = 0; j < W; ++j) q += is && ty + r * ly < len && j >= at.skip ? (x[j] - mean) * (x[j] - mean) : 0.0f;
+                for (int j = 0; j < W; ++j) q = exact || j >= at.skip ? fmaf(x[j] - mean, x[j] - mean, q) : q;
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
         rstd = __builtin_amdgcn_rsqf(fmaf(held_sum(q, p, lds, tx, group), share, in.eps));
         if (!GRAD && stats && is && ty == 0 && tx == group * p.ppg) {
@@ -409,40 +441,53 @@ __global__ __launch_bounds__(1024) void held_kernel(NormIn in, AnyRows dout, Hel
             stats[2 * unit + 1] = len > 0 ? rstd : 0.0f;
         }
     }
-    T* o = out + static_cast<int64_t>(b) * in.N * in.D + at.c;
+    T* o = out + (static_cast<int64_t>(b) * in.N + ty) * in.D + at.c;
+    const int64_t o_step = static_cast<int64_t>(ly) * in.D;
     float w[W], bias[W];
     int c = at.c;
     asm volatile("" : "+v"(c));  // fetched here and not in front of the sums, where they would take registers that hold values
     weights_of<W>(in, c, w, bias);
+    const float zero[W] = {};
     if constexpr (!GRAD) {
         if (!is) return;
 #pragma unroll
+        for (int j = 0; j < W; ++j) w[j] *= rstd;
+#pragma unroll
         for (int r = 0; r < R; ++r) {
+            if (r * ly >= in.N) break;
             const int l = ty + r * ly;
             float x[W];
-            raw[r].get(x);
+            raw[r].again(x);
+            if (l < len) {
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                const float y = fmaf((x[j] - mean) * rstd, w[j], bias[j]);
-                x[j] = l < len ? in.silu ? silu(y) : y : 0.0f;
+                for (int j = 0; j < W; ++j) {
+                    const float y = fmaf(x[j] - mean, w[j], bias[j]);
+                    x[j] = in.silu ? silu(y) : y;
+                }
+                Part<T, W>::put(o, W, x);
+            } else if (l < in.N) {
+                Part<T, W>::put(o, W, zero);
             }
-            if (l < in.N) Part<T, W>::put(o + static_cast<int64_t>(l) * in.D, W, x);
+            o += o_step;
+            __builtin_amdgcn_sched_barrier(0);
         }
     } else {
-        float dy[R][W], sums[2][W] = {};  // of dy hat, of dy
+        float sums[2][W] = {};  // of dy hat, of dy
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const bool on = is && ty + r * ly < len;
-            float x[W];
-            raw[r].get(x);
-            draw[r].get(dy[r]);
+            if (r * ly >= len) break;
+            float x[W], dy[W];
+            raw[r].again(x);
+            draw[r].again(dy);
+            if (is && ty + r * ly < len) {
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                const float hat = (x[j] - mean) * rstd;
-                if (in.silu) dy[r][j] *= dsilu(fmaf(hat, w[j], bias[j]));
-                sums[0][j] += on ? dy[r][j] * hat : 0.0f;
-                sums[1][j] += on ? dy[r][j] : 0.0f;
+                for (int j = 0; j < W; ++j) {
+                    const float hat = (x[j] - mean) * rstd, d = in.silu ? dy[j] * dsilu(fmaf(hat, w[j], bias[j])) : dy[j];
+                    sums[0][j] = fmaf(d, hat, sums[0][j]);
+                    sums[1][j] += d;
+                }
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
         // over the positions, channel by channel; the first lx threads have them, write them and weigh them for the group
         const int wide = p.lx < 64 ? p.lx : 64, lane = threadIdx.x & 63, entries = (blockDim.x >> 6) * wide;
@@ -480,16 +525,27 @@ __global__ __launch_bounds__(1024) void held_kernel(NormIn in, AnyRows dout, Hel
             s2 += lds[group * p.ppg + k];
             s1 += lds[p.lx + group * p.ppg + k];
         }
-        s1 *= share;
-        s2 *= share;
+        s1 *= -share * rstd;
+        s2 *= -share * rstd;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
+            if (r * ly >= in.N) break;
             const int l = ty + r * ly;
-            float x[W];
-            raw[r].get(x);
+            float x[W], dy[W];
+            raw[r].again(x);
+            draw[r].again(dy);
+            if (l < len) {
 #pragma unroll
-            for (int j = 0; j < W; ++j) x[j] = l < len ? rstd * (dy[r][j] * w[j] - fmaf((x[j] - mean) * rstd, s2, s1)) : 0.0f;
-            if (l < in.N) Part<T, W>::put(o + static_cast<int64_t>(l) * in.D, W, x);
+                for (int j = 0; j < W; ++j) {
+                    const float hat = (x[j] - mean) * rstd, d = in.silu ? dy[j] * dsilu(fmaf(hat, w[j], bias[j])) : dy[j];
+                    x[j] = fmaf(d, rstd * w[j], fmaf(hat, s2, s1));
+                }
+                Part<T, W>::put(o, W, x);
+            } else if (l < in.N) {
+                Part<T, W>::put(o, W, zero);
+            }
+            o += o_step;
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
@@ -923,12 +979,13 @@ Span span_plan(int dtype, int B, int N, int D, int G) {
     return p;
 }
 
-// Whether a sequence's groups fit registers.  At least 128 bytes of a row a workgroup (whole cache lines), more where groups leave fewer lanes without a piece;
-// as many threads as hold the positions in R pieces.
+// Whether a sequence's groups fit registers.  At least 64 bytes of a row a workgroup, more where groups leave fewer lanes without a piece; as many threads as hold
+// the positions in R pieces.  (64 x 512 x 1024 in 32 groups, bf16: 28.7 - 30.7 us with 64 bytes and kRun 2, 30.8 with 128 and 1, 133 with 64 and 1.)  Over
+// kHeldBytes threads hold eight pieces in one go: fewer and larger workgroups.
 constexpr int64_t kHeldBytes = int64_t{16} << 20;
 bool held_plan(int dtype, int B, int N, int D, int G, Held& p) {
-    if (static_cast<int64_t>(B) * N * D * (dtype ? 2 : 4) > kHeldBytes) return false;
-    const int C = D / G, W = piece_width(dtype, C), line = 128 / (W * (dtype ? 2 : 4));
+    const bool large = static_cast<int64_t>(B) * N * D * (dtype ? 2 : 4) > kHeldBytes;
+    const int C = D / G, W = piece_width(dtype, C), line = 64 / (W * (dtype ? 2 : 4));
     p.ppg = (C - 1) / W + 1;
     if (p.ppg > 512) return false;
     const int64_t pieces = static_cast<int64_t>(p.ppg) * G;
@@ -939,9 +996,10 @@ bool held_plan(int dtype, int B, int N, int D, int G, Held& p) {
         if (lx / 2 < pieces && lx / p.ppg * p.ppg * p.lx > p.lx / p.ppg * p.ppg * lx * 9 / 8) p.lx = lx;
     p.groups = p.lx / p.ppg;
     p.tiles = (G - 1) / p.groups + 1;
-    for (const int most : {2, 4})
-        for (p.threads = 256; p.threads <= 1024; p.threads *= 2) {
+    for (const int most : {2, 4, 8})
+        for (p.threads = 256; p.threads <= (most > 4 ? 512 : 1024); p.threads *= 2) {
             if (p.threads < p.lx || (N - 1) / (p.threads / p.lx) + 1 > most) continue;
+            if (large && most < 8) continue;
             p.pieces = most;
             return true;
         }
@@ -975,13 +1033,14 @@ hipError_t alone_of(const NormIn& in, AnyRows dout, const Alone& p, int pieces, 
 
 template <typename T, int W, bool GRAD>
 hipError_t held_of(const NormIn& in, AnyRows dout, const Held& p, const float* given, void* out, float* stats, float* partial, hipStream_t st) {
-    if (!fits(static_cast<int64_t>(in.B) * p.tiles, p.threads)) return hipErrorInvalidValue;
-    const auto kernel = p.pieces == 2 ? held_kernel<T, W, 2, GRAD> : held_kernel<T, W, 4, GRAD>;
+    const int64_t blocks = (static_cast<int64_t>(in.B) * p.tiles + 8 * kRun - 1) / (8 * kRun) * (8 * kRun);
+    if (!fits(blocks, p.threads)) return hipErrorInvalidValue;
+    const auto kernel = p.pieces == 2 ? held_kernel<T, W, 2, GRAD> : p.pieces == 4 ? held_kernel<T, W, 4, GRAD> : held_kernel<T, W, 8, GRAD>;
     const int entries = p.threads / 64 * (p.lx < 64 ? p.lx : 64);
     int floats = p.threads + p.lx;
     if (GRAD && floats < W * entries) floats = W * entries;
     if (floats < 2 * p.lx) floats = 2 * p.lx;
-    kernel<<<static_cast<unsigned>(in.B * p.tiles), p.threads, sizeof(float) * floats, st>>>(in, dout, p, given, static_cast<T*>(out), stats, partial);
+    kernel<<<static_cast<unsigned>(blocks), p.threads, sizeof(float) * floats, st>>>(in, dout, p, given, static_cast<T*>(out), stats, partial);
     return hipGetLastError();
 }
 

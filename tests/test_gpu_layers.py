@@ -278,6 +278,13 @@ def test_group_norm_long(crf):
     check_norm(crf, generator(6), 2, 5000, 33, 3, torch.float32, "ragged", False, True, True, strided, "long")
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("B,N,D,G", [(70, 130, 520, 65), (46, 201, 1001, 7), (1100, 9, 1000, 25), (9, 1023, 1024, 16)])
+def test_group_norm_of_many_sequences(crf, t, B, N, D, G):
+    """What caches do not hold: eight pieces a thread, or two passes."""
+    check_norm(crf, generator(7 * B + N), B, N, D, G, t, "ragged", False, True, True, normal, "many")
+
+
 @pytest.mark.parametrize("alone", (False, True))
 def test_group_norm_of_equal_values(crf, alone):
     """No spread: the activation of the bias, and no gradient but the bias's."""

@@ -76,7 +76,7 @@ def test_group_norm_refuses(lib):
         for size in (lib.lccrf_group_norm_workspace_bytes, lib.lccrf_group_norm_grad_workspace_bytes):
             assert [size(2, 2, 4, 8, 2, alone), size(0, 0, 4, 8, 2, alone), size(0, 2, 4, 8, 3, alone), size(0, 2, 4, 8, 0, alone), size(0, 2, 4, 8, 16, alone),
                     size(0, 1 << 16, 1 << 16, 8, 1, alone)] == [0] * 6
-    need = lib.lccrf_group_norm_workspace_bytes(0, 64, 512, 1024, 32, 0)
+    need = lib.lccrf_group_norm_workspace_bytes(0, 8, 5000, 1024, 32, 0)
     assert need > 256 and need % 256 == 0
 
     def call(x=rows(), dt=0, w=FAKE, b=FAKE, B=2, N=4, D=8, G=2, eps=1e-5, out=FAKE, stats=None, ws=None, n=0):
@@ -85,7 +85,7 @@ def test_group_norm_refuses(lib):
     assert [call(dt=3), call(B=0), call(N=0), call(D=0), call(G=0), call(G=3)] == [EINVAL] * 6
     assert [call(eps=e) for e in (0.0, -1e-5, INF, NAN)] == [EINVAL] * 4
     assert [call(x=None), call(x=rows(None)), call(out=None)] == [ENULL] * 3
-    assert [call(B=64, N=512, D=1024, G=32), call(B=64, N=512, D=1024, G=32, ws=FAKE, n=need - 257)] == [EWS] * 2
+    assert [call(B=8, N=5000, D=1024, G=32), call(B=8, N=5000, D=1024, G=32, ws=FAKE, n=need - 257)] == [EWS] * 2
     assert [call(x=rows(FAKE + 1)), call(w=FAKE + 2), call(b=FAKE + 1), call(out=FAKE + 2), call(stats=FAKE + 2), call(ws=FAKE + 4)] == [EALIGN] * 6
     need = lib.lccrf_group_norm_grad_workspace_bytes(1, 2, 4, 8, 2, 1)
     assert need > 256

@@ -73,9 +73,9 @@ def ask(tmp_path_factory):
 
 
 SEVERAL = [("recur", 2, 5000, 30), ("recur", 1, 3000, 1), ("recur", 2, 5000, 30, 4096), ("recur_grad", 2, 5000, 30), ("recur_grad", 2, 5000, 30, 4096), ("recur_grad", 64, 20, 300, 4096),
-           ("norm", 64, 512, 1024, 32, 0), ("norm_grad", 64, 512, 1024, 32, 0), ("norm_grad", 64, 512, 1024, 32, 0, 1, 4096), ("norm_grad", 2, 9, 24, 3, 0), ("norm_grad", 2, 9, 24, 3, 1),
+           ("norm", 8, 5000, 1024, 32, 0), ("norm_grad", 8, 5000, 1024, 32, 0), ("norm_grad", 8, 5000, 1024, 32, 0, 1, 4096), ("norm_grad", 64, 512, 1024, 32, 0), ("norm_grad", 2, 9, 24, 3, 0), ("norm_grad", 2, 9, 24, 3, 1),
            ("norm_grad", 2, 9, 40000, 2, 1), ("norm", 2, 5000, 40000, 1, 0)]
-SINGLE = [("recur", 2, 1, 30), ("recur", 2, 40, 30), ("recur_step", 3, 5), ("norm", 2, 9, 24, 3, 0), ("norm", 2, 9, 24, 3, 1), ("norm", 2, 9, 40000, 2, 1), ("distill", 5, 9, 3), ("distill", 5, 90000, 100),
+SINGLE = [("recur", 2, 1, 30), ("recur", 2, 40, 30), ("recur_step", 3, 5), ("norm", 2, 9, 24, 3, 0), ("norm", 2, 9, 24, 3, 1), ("norm", 2, 9, 40000, 2, 1), ("norm", 64, 512, 1024, 32, 0), ("distill", 5, 9, 3), ("distill", 5, 90000, 100),
           ("distill_grad", 5, 9, 3), ("distill_grad", 5, 3000, 3), ("distill_grad", 5, 90000, 100), ("distill_grad", 5, 9000, 3, 1, 4096)]
 
 
