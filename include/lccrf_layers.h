@@ -30,7 +30,7 @@ extern "C" {
  *   x, f, g, z [B][N][D] rows; decay [D], f_bias and g_bias [D] or NULL (= 0); state and final [B][D] float (state NULL: 0;
  *   final NULL: not wanted; final may be state itself).  rate is positive and finite, D at most 2^22.
  * saved: NULL, or lccrf_recurrence_saved_bytes of device memory that takes what the gradient would otherwise compute again (the
- * states in front of every thirty-second position; its layout is the library's own).
+ * states in front of every eighth position; its layout is the library's own).
  */
 typedef struct {
     lccrf_rows x, f, g, z;

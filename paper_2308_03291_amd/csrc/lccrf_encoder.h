@@ -18,6 +18,11 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Rounded once, to nearest even (one instruction on gfx950).
 __device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x)); }
+__device__ __forceinline__ uint32_t to_bf16_pair(float low, float high) {  // both by one instruction
+    typedef float Floats __attribute__((ext_vector_type(2)));
+    typedef __bf16 Halves __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(Floats{low, high}, Halves));
+}
 __device__ __forceinline__ float from_bf16(uint16_t h) { return __uint_as_float(static_cast<uint32_t>(h) << 16); }
 
 __device__ __forceinline__ float get1(const float* p) { return *p; }
@@ -59,7 +64,7 @@ template <typename T, int W, bool SMALL = false> struct Piece {
             for (int i = 0; i < W; ++i) v[i] = __float_as_uint(o[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < W / 2; ++i) v[i] = to_bf16(o[2 * i]) | static_cast<uint32_t>(to_bf16(o[2 * i + 1])) << 16;
+            for (int i = 0; i < W / 2; ++i) v[i] = to_bf16_pair(o[2 * i], o[2 * i + 1]);
         }
         if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<Any*>(p));
         else *reinterpret_cast<Any*>(p) = v;

@@ -6,8 +6,7 @@
 // of its positions - what they turn a state h into, A h + E; those of a wave are joined by shuffles, those of the waves through LDS: after one barrier every
 // wave folds the pairs of the waves in front of it onto the state before the block, and every lane runs its own positions again from there, with the
 // a and b that it has kept in registers; the last one leaves the state behind the block in LDS.  So every input is read once and its gates
-// are computed once.  Narrow tiles (SUB 4 and 8) are for few sequences, where wide ones would be fewer workgroups than the chip has room for, and
-// for widths that wide tiles cover badly.
+// are computed once.  Narrow tiles (SUB 4) are for few sequences, where wide ones would be fewer workgroups than the chip has room for.
 #pragma once
 
 #include "lccrf_layers.h"
@@ -18,8 +17,9 @@ namespace enc {
 constexpr int kRecurSave = 8;   // positions between two saved states
 constexpr int kRecurBlock = 64;  // segments are multiples of it
 
+constexpr int kWideTile = 128, kNarrowTile = 32;  // channels
 struct RecurPlan {
-    int sets;  // SUB, 1 or 4
+    bool narrow;
     int tiles, segments, seg_len;
     bool near;  // tiles of the same positions on one XCD
 };
@@ -28,15 +28,12 @@ struct RecurPlan {
 // other and share the cache lines on their borders (where a row is no whole number of lines, most of them): eight sequences' segments side by side, all tiles
 // of each on one XCD.
 constexpr int kXcds = 8;
-struct RecurWork { int64_t which; int tile; };
+struct RecurWork { int b, seg, tile; };  // (in scalar registers, though divided for in vector ones)
 __device__ __forceinline__ RecurWork recur_work(const RecurPlan& p) {
-    const unsigned tiles = p.tiles;
-    if (!p.near) {
-        const unsigned which = blockIdx.x / tiles;
-        return {which, static_cast<int>(blockIdx.x - which * tiles)};
-    }
-    const unsigned rest = blockIdx.x / kXcds, eight = rest / tiles;
-    return {static_cast<int64_t>(eight) * kXcds + blockIdx.x % kXcds, static_cast<int>(rest - eight * tiles)};
+    const unsigned tiles = p.tiles, segments = p.segments, rest = p.near ? blockIdx.x / kXcds : blockIdx.x, group = rest / tiles;
+    const unsigned which = p.near ? group * kXcds + blockIdx.x % kXcds : group, b = which / segments;
+    return {__builtin_amdgcn_readfirstlane(static_cast<int>(b)), __builtin_amdgcn_readfirstlane(static_cast<int>(which - b * segments)),
+            __builtin_amdgcn_readfirstlane(static_cast<int>(rest - group * tiles))};
 }
 inline int64_t recur_blocks(const RecurPlan& p, int B) {
     const int64_t all = static_cast<int64_t>(B) * p.segments;
@@ -47,19 +44,19 @@ inline int64_t recur_blocks(const RecurPlan& p, int B) {
 // over all segments makes what each turns a state into, and the segments side by side fold those in front of them.  (How many of which: with the launches.)
 inline RecurPlan recur_plan_of(int B, int N, int D, int many, int narrow, int longest) {
     RecurPlan p;
-    const int wide = D == 1 ? 64 : 128;
-    p.sets = 1;
-    p.tiles = (D - 1) / wide + 1;
+    p.narrow = false;
+    p.tiles = (D - 1) / (D == 1 ? 64 : kWideTile) + 1;
     const int64_t groups = static_cast<int64_t>(B) * p.tiles;
     int64_t segments = 1;
-    if (groups < many && D > 1) {
-        const int64_t tiles = (D - 1) / 32 + 1;
-        if (N <= longest || B * tiles >= narrow) {
-            p.sets = 4;
+    if (groups < many) {
+        const int64_t tiles = (D - 1) / kNarrowTile + 1;
+        if (D > 1 && (N <= longest || B * tiles >= narrow)) {
+            p.narrow = true;
             p.tiles = static_cast<int>(tiles);
+        } else {
+            segments = 2048 / groups;
         }
     }
-    if (groups < many && p.sets == 1) segments = 2048 / groups;
     const int64_t most = (static_cast<int64_t>(N) + kRecurBlock - 1) / kRecurBlock;
     if (segments > most) segments = most;
     if (segments < 1) segments = 1;
@@ -87,9 +84,11 @@ template <int V> struct Lane {
         own = left >= V ? V : left > 0 ? left : 0;
         full = (tile + 1) * lanes * V <= D;
     }
-    // (`at`: this lane's row, so many elements behind the wave's)
+    // (`at`: this lane's row, so many elements behind the wave's.)  The offset is added by the store itself, not to every output's address ahead of a loop.
     template <bool WHOLE = false, typename T> __device__ __forceinline__ void give(T* row, const float (&v)[V], unsigned at = 0) const {
-        T* p = reinterpret_cast<T*>(reinterpret_cast<char*>(row) + (at + static_cast<unsigned>(c)) * static_cast<unsigned>(sizeof(T)));
+        unsigned bytes = (at + static_cast<unsigned>(c)) * static_cast<unsigned>(sizeof(T));
+        asm volatile("" : "+v"(bytes));
+        T* p = reinterpret_cast<T*>(reinterpret_cast<char*>(row) + bytes);
         if (WHOLE || own == V) {
             Bit<T, V>::put(p, V, v);
         } else {
@@ -107,9 +106,10 @@ template <typename T, int V> __device__ __forceinline__ void take_bit(Bit<T, V>&
 // P rows, from `first` on for the wave's first set of lanes and P further for each of the next; of those at or past the end the last one before it
 // (len > 0) takes the place.  A lane's place is a scalar address and a 32-bit offset: `set` is P times its number of set, `step` the bytes from a row to
 // the next (near_rows below), `bytes` its channels'.
-template <typename T, int V, int P, int SUB> __device__ __forceinline__ void take_rows(Bit<T, V> (&v)[P], const AnyRows& r, int b, int first, int len, int set, unsigned bytes) {
+template <typename T, int V, int P, int SUB, bool WHOLE = false>
+__device__ __forceinline__ void take_rows(Bit<T, V> (&v)[P], const AnyRows& r, int b, int first, int len, int set, unsigned bytes) {
     const unsigned step = static_cast<unsigned>(r.row) * sizeof(T);
-    if (first + P * SUB <= len) {
+    if (WHOLE || first + P * SUB <= len) {
         const T* p = row_of<T>(r, b, first);
         const unsigned at = SUB > 1 ? set * step + bytes : bytes;
 #pragma unroll
@@ -127,8 +127,8 @@ template <typename T, int V, int P, int SUB> __device__ __forceinline__ void tak
 // Rows of a wave no further apart than its 32-bit offsets reach; with others, tiles are wide.
 inline bool near_rows(const AnyRows& r) { return r.row >= 0 && r.row < (1 << 24); }
 inline void widen_tiles(RecurPlan& p, int D) {
-    if (p.sets > 1) p.tiles = (D - 1) / 128 + 1;
-    p.sets = 1;
+    if (p.narrow) p.tiles = (D - 1) / kWideTile + 1;
+    p.narrow = false;
 }
 
 // A channel's constants, times log2(e) where they go into a power of two: c = -rate log(1 + exp(decay)).
@@ -139,21 +139,20 @@ __device__ __forceinline__ RecurChannel recur_channel(const RecurIn& in, int d) 
 // s(v + bias), bias times -log2(e).
 __device__ __forceinline__ float open_gate(float v, float bias) { return __builtin_amdgcn_rcpf(1.0f + exp2_fast(fmaf(v, -kLog2e, bias))); }
 
-// a = exp(u) = exp2(t), t = c open; rest = 1 - a^2.  For small u, a^2 has lost what 1 - a^2 is made of: from 2 u > -1/4 on the series of
-// 1 - exp(2 u) instead, in t (off by less than 2^-24 of it); below that 1 - a a loses no more than two bits.
+// a = exp(u) = exp2(t), t = c open; rest = 1 - a^2.  For small u, a^2 has lost what 1 - a^2 is made of: from 2 u > -1/4 on
+// a polynomial instead, t q(t), q of degree 4 through (1 - exp(2 u)) / t at Chebyshev's points (with its rounded coefficients off by at most 2^-26 of it); below that
+// 1 - a a loses no more than two bits.
 struct Decay { float open, t, a, rest; };
 __device__ __forceinline__ Decay decay_of(float f, const RecurChannel& ch) {
-    constexpr double k = 2.0 * 0.693147180559945309417;
     Decay d;
     d.open = open_gate(f, ch.f_bias);
     d.t = ch.c * d.open;
     d.a = exp2_fast(d.t);
-    float q = static_cast<float>(-k * k * k * k * k * k / 720.0);
-    q = fmaf(q, d.t, static_cast<float>(-k * k * k * k * k / 120.0));
-    q = fmaf(q, d.t, static_cast<float>(-k * k * k * k / 24.0));
-    q = fmaf(q, d.t, static_cast<float>(-k * k * k / 6.0));
-    q = fmaf(q, d.t, static_cast<float>(-k * k / 2.0));
-    q = fmaf(q, d.t, static_cast<float>(-k));
+    float q = -0.0384703129529953f;
+    q = fmaf(q, d.t, -0.15323998034000397f);
+    q = fmaf(q, d.t, -0.44399136304855347f);
+    q = fmaf(q, d.t, -0.9609050750732422f);
+    q = fmaf(q, d.t, -1.3862943649291992f);
     d.rest = d.t > -0.18033688f ? q * d.t : fmaf(-d.a, d.a, 1.0f);
     return d;
 }

@@ -31,10 +31,9 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
     const int lane = threadIdx.x & 63, cl = lane % L, w = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const int sub = lane / L, set = sub * P;
     const RecurWork work = recur_work(r.plan);
-    const int tile = work.tile, b = static_cast<int>(work.which / r.plan.segments), seg = static_cast<int>(work.which - static_cast<int64_t>(b) * r.plan.segments);
+    const int b = work.b, seg = work.seg;
     if (b >= in.B) return;
-    const Lane<V> my(tile, cl, L, in.D);
-    const unsigned bytes = static_cast<unsigned>(my.c) * sizeof(T);
+    const Lane<V> my(work.tile, cl, L, in.D);
     const int len = length_at(in.lengths, b, in.N), begin = seg * r.plan.seg_len;
     const int stop = in.N - begin < r.plan.seg_len ? in.N : begin + r.plan.seg_len, end = stop < len ? stop : len;
     T* out = static_cast<T*>(r.out) + static_cast<int64_t>(b) * in.N * in.D;
@@ -47,25 +46,50 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
         carry[j] = seg == 0 && r.state ? r.state[static_cast<int64_t>(b) * in.D + my.c + j] : 0.0f;
         total[j] = 1.0f;
     }
-    if (!(MODE & kEnds)) {
-        const float* e = r.ends + (static_cast<int64_t>(b) * r.plan.segments * in.D + my.c) * 2;
-#pragma unroll 8
-        for (int s = 0; s < seg; ++s, e += 2 * static_cast<int64_t>(in.D)) {
-            const Pair made = *reinterpret_cast<const AnyPair*>(e);
-#pragma unroll
-            for (int j = 0; j < V; ++j) carry[j] = fmaf(made[2 * j], carry[j], made[2 * j + 1]);
-        }
-    }
     const bool last = w == W - 1 && sub == SUB - 1;
 
     if (begin < end) {
         Bit<T, V> xr[P], fr[P], gr[P], zr[P];
-        const auto fetch = [&](int first) {
-            take_rows<T, V, P, SUB>(fr, in.f, b, first, len, set, bytes);
-            take_rows<T, V, P, SUB>(gr, in.g, b, first, len, set, bytes);
-            take_rows<T, V, P, SUB>(xr, in.x, b, first, len, set, bytes);
-            if (GATED) take_rows<T, V, P, SUB>(zr, in.z, b, first, len, set, bytes);
+        const auto fetch = [&](int first, auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
+            unsigned bytes = static_cast<unsigned>(my.c) * sizeof(T);
+            asm volatile("" : "+v"(bytes));  // added by the loads themselves, not to every input's address ahead of the loop
+            take_rows<T, V, P, SUB, WHOLE>(fr, in.f, b, first, len, set, bytes);
+            take_rows<T, V, P, SUB, WHOLE>(gr, in.g, b, first, len, set, bytes);
+            take_rows<T, V, P, SUB, WHOLE>(xr, in.x, b, first, len, set, bytes);
+            if (GATED) take_rows<T, V, P, SUB, WHOLE>(zr, in.z, b, first, len, set, bytes);
         };
+        fetch(begin + w * kRows, std::false_type{});
+        if constexpr (!(MODE & kEnds) && W > 1) {
+            // the segments in front, a share of them a wave, on top of the first loads
+            if (seg > 0) {
+                const int share = (seg + W - 1) / W, from = w * share, to = seg < from + share ? seg : from + share;
+                const float* e = r.ends + ((static_cast<int64_t>(b) * r.plan.segments + from) * in.D + my.c) * 2;
+                Pair mine;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    mine[2 * j] = 1.0f;
+                    mine[2 * j + 1] = 0.0f;
+                }
+#pragma unroll 8
+                for (int s = from; s < to; ++s, e += 2 * static_cast<int64_t>(in.D)) {
+                    const Pair made = *reinterpret_cast<const AnyPair*>(e);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        mine[2 * j] = product(mine[2 * j], made[2 * j]);
+                        mine[2 * j + 1] = fmaf(made[2 * j], mine[2 * j + 1], made[2 * j + 1]);
+                    }
+                }
+                if (sub == 0) pairs[1][w][cl] = mine;  // (the other buffer than the first block's)
+                lds_sync();
+#pragma unroll
+                for (int k = 0; k < W; ++k) {
+                    const Pair made = pairs[1][k][cl];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) carry[j] = fmaf(made[2 * j], carry[j], made[2 * j + 1]);
+                }
+            }
+        }
         int buffer = 0;
         const auto leave = [&](int to) {
             Some s;
@@ -74,8 +98,9 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
             if (last) states[to][cl] = s;
         };
         if (W > 1) leave(0);
-        const auto run = [&](auto whole, int first) {  // whole: all positions lie before the end, all lanes have channels of their own
-            constexpr bool WHOLE = decltype(whole)::value;
+        // whole: all positions lie before the end; ahead: and so do the next block's; full: all lanes have V channels of their own
+        const auto run = [&](auto whole, auto ahead, auto full, int first) {
+            constexpr bool WHOLE = decltype(whole)::value, FULL = decltype(full)::value;
             const int l0 = first + set;
             float a[P][V], put[P][V];
             float(&h)[V] = carry;
@@ -95,7 +120,7 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
                     put[i][j] = on ? __builtin_amdgcn_sqrtf(d.rest) * open_gate(g[j], ch[j].g_bias) * x[j] : 0.0f;
                 }
             }
-            fetch(first + kBlock);
+            if (decltype(ahead)::value || first + kBlock < end) fetch(first + kBlock, ahead);
             if constexpr (W > 1) {
                 Pair mine;
                 float A[V], E[V];
@@ -132,7 +157,7 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
                 buffer ^= 1;
             }
             if ((MODE & kSave) && l0 % kRecurSave == 0 && l0 < end)
-                my.template give<WHOLE>(r.saved + (static_cast<int64_t>(b) * ((in.N + kRecurSave - 1) / kRecurSave) + l0 / kRecurSave) * in.D, h);
+                my.template give<FULL>(r.saved + (static_cast<int64_t>(b) * ((in.N + kRecurSave - 1) / kRecurSave) + l0 / kRecurSave) * in.D, h);
             if constexpr ((MODE & kOut) != 0 || W == 1) {
                 // a place for the whole wave and the lane's offset in it
                 T* to = out + static_cast<int64_t>(first) * in.D;
@@ -150,7 +175,7 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
                             o[j] = GATED ? h[j] * silu(zi[j]) : h[j];
                             o[j] = WHOLE || l0 + i < end ? o[j] : 0.0f;
                         }
-                        if (WHOLE || l0 + i < stop) my.template give<WHOLE>(to, o, SUB > 1 ? at : 0u);
+                        if (WHOLE || l0 + i < stop) my.template give<FULL>(to, o, SUB > 1 ? at : 0u);
                     }
                 }
             } else if (w == W - 1) {
@@ -161,11 +186,17 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
             }
             if (W > 1) leave(buffer);
         };
-        fetch(begin + w * kRows);
         int block = begin;
-        if (my.full)
-            for (; block + kBlock <= end; block += kBlock) run(std::true_type{}, block + w * kRows);
-        for (; block < end; block += kBlock) run(std::false_type{}, block + w * kRows);
+        const auto whole_blocks = [&](auto full) {
+            for (; block + 2 * kBlock <= end; block += kBlock) run(std::true_type{}, std::true_type{}, full, block + w * kRows);
+            if (block + kBlock <= end) {
+                run(std::true_type{}, std::false_type{}, full, block + w * kRows);
+                block += kBlock;
+            }
+        };
+        if (my.full || (MODE & kEnds)) whole_blocks(std::true_type{});  // (which gives nothing away here)
+        else whole_blocks(std::false_type{});
+        for (; block < end; block += kBlock) run(std::false_type{}, std::false_type{}, std::false_type{}, block + w * kRows);
     }
     if (MODE & kOut) {
         const float zero[V] = {};
@@ -249,8 +280,10 @@ constexpr int kPositions = 4, kWaves = 8, kFewWaves = 4;  // a lane's positions;
 
 int channels_a_lane(int D) { return D == 1 ? 1 : 2; }
 
-// Measured, us, wide tiles / narrow / segments (B x N x D, bfloat16, no gate but in the first): 64x512x2048 146 / 165 / 237, 16x1000x1024 64 / 58 / 68, 30x300x300
-// 27 / 22 / 24, 8x256x1024 20 / 16.5 / 19, 4x5000x1024 291 / 117 / 84, 2x10000x256 573 / 170 / 34, 4x16384x514 933 / 291 / 124.
+// Measured, us, wide tiles / narrow / segments (B x N x D, bfloat16, no gate but in the first): 64x512x2048 145 / 158 / 252, 16x1000x1024 51 / 47 / 54, 30x300x300
+// 21 / 18 / 21, 8x256x1024 16 / 14 / 19, 4x5000x1024 228 / 91 / 64, 2x10000x256 446 / 143 / 29, 4x16384x514 865 / 263 / 118.  The first is 4.65 TB/s (float 5.5), of
+// 5.14 that a copy has; segments are read twice: the last one's two passes take 56 us (3.6 TB/s) and 60 (4.5).
+static_assert(kWaves != kFewWaves, "workgroups of so few have segments");
 RecurPlan recur_plan(int B, int N, int D) { return recur_plan_of(B, N, D, 256, 256, 512); }
 
 template <typename T, int V, int W, int SUB, int MODE>
@@ -272,7 +305,7 @@ hipError_t recur_by(const RecurRun& r, hipStream_t st) {
     if (r.plan.segments > 1) return recur_of<T, V, kFewWaves, 1>(r, st);
     if (r.in.N <= kPositions) return recur_of<T, V, 1, 1>(r, st);
     if constexpr (V > 1) {
-        if (r.plan.sets > 1) return recur_of<T, V, kWaves, 4>(r, st);
+        if (r.plan.narrow) return recur_of<T, V, kWaves, 4>(r, st);
     }
     return recur_of<T, V, kWaves, 1>(r, st);
 }
@@ -288,7 +321,7 @@ size_t recur_workspace(int B, int N, int D) {
 
 hipError_t launch_recur(int dtype, const RecurIn& in, const float* state, void* out, float* final_state, float* saved, void* ws, hipStream_t st) {
     RecurRun r{in, state, out, final_state, saved, static_cast<float*>(ws), recur_plan(in.B, in.N, in.D)};
-    if (!near_rows(in.x) || !near_rows(in.f) || !near_rows(in.g) || !near_rows(in.z)) widen_tiles(r.plan, in.D);
+    if (in.N <= kPositions || !near_rows(in.x) || !near_rows(in.f) || !near_rows(in.g) || !near_rows(in.z)) widen_tiles(r.plan, in.D);
     if (!fits(recur_blocks(r.plan, in.B), 64 * kWaves)) return hipErrorInvalidValue;
     if (channels_a_lane(in.D) == 1) return dtype ? recur_by<uint16_t, 1>(r, st) : recur_by<float, 1>(r, st);
     return dtype ? recur_by<uint16_t, 2>(r, st) : recur_by<float, 2>(r, st);

@@ -14,7 +14,6 @@ namespace lccrf {
 namespace enc {
 namespace {
 
-
 struct GradRun {
     RecurIn in;
     AnyRows dout;
@@ -37,10 +36,9 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
     const RecurIn& in = r.in;
     const int lane = threadIdx.x & 63, cl = lane % L, sub = lane / L, set = sub * P, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const RecurWork work = recur_work(r.plan);
-    const int tile = work.tile, b = static_cast<int>(work.which / r.plan.segments), seg = static_cast<int>(work.which - static_cast<int64_t>(b) * r.plan.segments);
+    const int b = work.b, seg = work.seg;
     if (b >= in.B) return;
-    const Lane<V> my(tile, cl, L, in.D);
-    const unsigned bytes = static_cast<unsigned>(my.c) * sizeof(T);
+    const Lane<V> my(work.tile, cl, L, in.D);
     const int len = length_at(in.lengths, b, in.N), begin = seg * r.plan.seg_len;
     const int stop = in.N - begin < r.plan.seg_len ? in.N : begin + r.plan.seg_len, end = stop < len ? stop : len;
     const int64_t first_row = static_cast<int64_t>(b) * in.N;
@@ -55,13 +53,6 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
         total[j] = 1.0f;
     }
     if (!ENDS) {
-        const int64_t base = static_cast<int64_t>(b) * r.plan.segments;
-#pragma unroll 8
-        for (int s = r.plan.segments - 1; s > seg; --s) {
-            const Pair e = *reinterpret_cast<const AnyPair*>(r.ends + ((base + s) * in.D + my.c) * 2);
-#pragma unroll
-            for (int j = 0; j < V; ++j) c[j] = fmaf(e[2 * j], c[j], e[2 * j + 1]);
-        }
         const float zero[V] = {};
         for (int l = (begin < end ? end : begin) + w * SUB + sub; l < stop; l += W * SUB) {
             const int64_t at = (first_row + l) * in.D;
@@ -75,17 +66,50 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
     if (begin < end) {
         Bit<T, V> xr[P], fr[P], gr[P], zr[P], dr[P];
         Bit<float, V> sr;
-        const auto fetch = [&](int block) {
+        const auto fetch = [&](int block, auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
             const int first = block + w * kRows;
+            unsigned bytes = static_cast<unsigned>(my.c) * sizeof(T);
+            asm volatile("" : "+v"(bytes));  // added by the load itself, not to every row's address ahead of the loop
             if (!ENDS) take_bit<float, V>(sr, r.saved + (static_cast<int64_t>(b) * ((in.N + kRecurSave - 1) / kRecurSave) + block / kRecurSave) * in.D, 4u * my.c);
-            take_rows<T, V, P, SUB>(fr, in.f, b, first, len, set, bytes);
-            take_rows<T, V, P, SUB>(dr, r.dout, b, first, len, set, bytes);
-            if (GATED) take_rows<T, V, P, SUB>(zr, in.z, b, first, len, set, bytes);
+            take_rows<T, V, P, SUB, WHOLE>(fr, in.f, b, first, len, set, bytes);
+            take_rows<T, V, P, SUB, WHOLE>(dr, r.dout, b, first, len, set, bytes);
+            if (GATED) take_rows<T, V, P, SUB, WHOLE>(zr, in.z, b, first, len, set, bytes);
             if (!ENDS) {
-                take_rows<T, V, P, SUB>(gr, in.g, b, first, len, set, bytes);
-                take_rows<T, V, P, SUB>(xr, in.x, b, first, len, set, bytes);
+                take_rows<T, V, P, SUB, WHOLE>(gr, in.g, b, first, len, set, bytes);
+                take_rows<T, V, P, SUB, WHOLE>(xr, in.x, b, first, len, set, bytes);
             }
         };
+        int block = begin + (end - begin - 1) / kBlock * kBlock;
+        fetch(block, std::false_type{});
+        if (!ENDS && len > stop) {
+            // the segments behind that have positions, a share of them a wave, on top of the first loads
+            const int many = (len - stop - 1) / r.plan.seg_len + 1, share = (many + W - 1) / W, from = w * share, to = many < from + share ? many : from + share;
+            const float* e = r.ends + ((static_cast<int64_t>(b) * r.plan.segments + seg + to) * in.D + my.c) * 2;
+            float A[V], G[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                A[j] = 1.0f;
+                G[j] = 0.0f;
+            }
+#pragma unroll 8
+            for (int s = to; s > from; --s, e -= 2 * static_cast<int64_t>(in.D)) {
+                const Pair made_there = *reinterpret_cast<const AnyPair*>(e);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    A[j] = product(A[j], made_there[2 * j]);
+                    G[j] = fmaf(made_there[2 * j], G[j], made_there[2 * j + 1]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (sub == 0) made[1][w][j][cl] = Three{A[j], 0.0f, G[j], 0.0f};  // (the other buffer than the first block's)
+            lds_sync();
+#pragma unroll
+            for (int k = W - 1; k >= 0; --k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) c[j] = fmaf(made[1][k][j][cl][0], c[j], made[1][k][j][cl][2]);
+        }
         int buffer = 0;
         const auto leave = [&](int to) {
             if (front) {
@@ -94,10 +118,10 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
             }
         };
         leave(0);
-        const auto run = [&](auto whole, int block) {  // whole: all positions lie before the end, all lanes have channels of their own
-            constexpr bool WHOLE = decltype(whole)::value;
+        const auto run = [&](auto whole, auto full, int block) {  // whole: all positions lie before the end; full: all lanes have V channels of their own
+            constexpr bool WHOLE = decltype(whole)::value, FULL = decltype(full)::value;
             const int first = block + w * kRows, l0 = first + set;
-            float a[P][V], m[P][V], rest[P][V], open[P][V], in_gate[P][V], x[P][V], dy[P][V], h[V];
+            float a[P][V], m[P][V], inv[P][V], open[P][V], in_gate[P][V], x[P][V], dy[P][V], h[V];
             Bit<T, V> z[P], dout[P];
 #pragma unroll
             for (int i = 0; i < P; ++i) {
@@ -121,8 +145,9 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
                     dy[i][j] = on ? GATED ? di[j] * silu(zi[j]) : di[j] : 0.0f;
                     if (!ENDS) {
                         open[i][j] = d.open;
-                        rest[i][j] = d.rest;
-                        m[i][j] = __builtin_amdgcn_sqrtf(d.rest);
+                        // u / m is 0 where 1 - a^2 is (or is too small for its root)
+                        inv[i][j] = d.rest < 1.17549435e-38f ? 0.0f : __builtin_amdgcn_rsqf(d.rest);
+                        m[i][j] = d.rest * inv[i][j];
                         in_gate[i][j] = open_gate(g[j], ch[j].g_bias);
                         x[i][j] = on ? x[i][j] : 0.0f;
                     }
@@ -134,7 +159,7 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) h[j] = s[j];
             }
-            fetch(block > begin ? block - kBlock : begin);
+            fetch(block > begin ? block - kBlock : begin, whole);  // (whole: so are those in front)
             const auto put = [&](int i, int j) { return WHOLE || l0 + i < end ? m[i][j] * in_gate[i][j] * x[i][j] : 0.0f; };
             float before_a[V], before_e[V], behind_a[V], behind_g[V];
 #pragma unroll
@@ -215,11 +240,9 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
                         const float dh = dy[i][j] + c[j], u = kLn2f * (ch[j].c * open[i][j]), ai = a[i][j], gate_in = in_gate[i][j];
-                        // u / m: 0 where 1 - a^2 is (or is too small for its root)
-                        const float ratio = rest[i][j] < 1.17549435e-38f ? 0.0f : u * __builtin_amdgcn_rsqf(rest[i][j]);
                         dx[j] = dh * m[i][j] * gate_in;
                         dg[j] = dx[j] * x[i][j] * (1.0f - gate_in);
-                        const float dlog = dh * ai * (before[i][j] * u - gate_in * x[i][j] * ai * ratio);
+                        const float dlog = dh * ai * (before[i][j] * u - gate_in * x[i][j] * ai * (u * inv[i][j]));
                         df[j] = dlog * (1.0f - open[i][j]);
                         if (GATED) {
                             const float gate = sigmoid(zi[j]);
@@ -232,19 +255,24 @@ __global__ __launch_bounds__(64 * W) void recur_grad_kernel(GradRun r) {
                     }
                     if (on) {
                         const int64_t row = (first_row + first + i) * in.D;
-                        my.template give<WHOLE>(static_cast<T*>(r.g.dx) + row, dx, at);
-                        my.template give<WHOLE>(static_cast<T*>(r.g.df) + row, df, at);
-                        my.template give<WHOLE>(static_cast<T*>(r.g.dg) + row, dg, at);
-                        if (GATED) my.template give<WHOLE>(static_cast<T*>(r.g.dz) + row, dz, at);
+                        my.template give<FULL>(static_cast<T*>(r.g.dx) + row, dx, at);
+                        my.template give<FULL>(static_cast<T*>(r.g.df) + row, df, at);
+                        my.template give<FULL>(static_cast<T*>(r.g.dg) + row, dg, at);
+                        if (GATED) my.template give<FULL>(static_cast<T*>(r.g.dz) + row, dz, at);
                     }
                 }
             }
             leave(buffer);
         };
-        int block = begin + (end - begin - 1) / kBlock * kBlock;
-        fetch(block);
-        for (; block >= begin && !(my.full && block + kBlock <= end); block -= kBlock) run(std::false_type{}, block);
-        for (; block >= begin; block -= kBlock) run(std::true_type{}, block);
+        if (block + kBlock > end) {
+            run(std::false_type{}, std::false_type{}, block);
+            block -= kBlock;
+        }
+        if (my.full || ENDS) {  // (which give nothing away)
+            for (; block >= begin; block -= kBlock) run(std::true_type{}, std::true_type{}, block);
+        } else {
+            for (; block >= begin; block -= kBlock) run(std::true_type{}, std::false_type{}, block);
+        }
     }
     if constexpr (ENDS) {
 #pragma unroll
@@ -319,13 +347,13 @@ __global__ __launch_bounds__(1024) void recur_sums_kernel(const float* __restric
     to[ch] = sum;
 }
 
-constexpr int P = 2, W = 4;  // a lane's positions, a workgroup's waves: 142 registers, three waves a SIMD (four positions: 203, two; the whole training step of
-                             // B=128 N=256 D=1024, bfloat16, ragged, 198 us / 227)
+constexpr int P = 2, W = 4;  // a lane's positions, a workgroup's waves: 125 registers (bfloat16), four waves a SIMD, so that the 1024 workgroups of B=128 N=256
+                             // D=1024 run at once (whole training step, ragged, us: 188 - 194; at 142 registers 203 - 210; four positions, 203 registers, 227)
 static_assert(P * W % kRecurSave == 0, "a block begins where a state is saved");
 
-// Measured, us, forward and gradient, wide tiles / narrow / segments (B x N x D, bfloat16): 128x256x1024 ragged 203 / 218 / 258, 64x1024x514 353 / 308 / 277, 16x1000x1024
-// 246 / 173 / 165, 100x200x128 63 / 48 / 59, 30x300x300 102 / 68 / 68, 8x256x1024 72 / 46 / 51, 4x5000x1024 1176 / 646 / 419 (in all of them the
-// forward pass by wide tiles).
+// Measured, us, forward and gradient, wide tiles / narrow / segments (B x N x D, bfloat16): 128x256x1024 ragged 188 / 219 / 267, 64x1024x514 371 / 354 / 384 (forwards
+// wide, backwards segments: 355), 16x1000x1024 222 / 164 / 156 (forwards narrow: 151), 100x200x128 59 / 48 / 61, 30x300x300 89 / 61 / 61, 8x256x1024 69 / 51 / 61,
+// 4x5000x1024 1057 / 447 / 193.
 RecurPlan grad_plan(int B, int N, int D) { return recur_plan_of(B, N, D, 768, 1 << 30, 512); }
 
 template <typename T, int V, int SUB>
@@ -349,7 +377,7 @@ hipError_t grad_of(const GradRun& r, hipStream_t st) {
 template <typename T, int V>
 hipError_t grad_by(const GradRun& r, hipStream_t st) {
     if constexpr (V > 1) {
-        if (r.plan.sets > 1) return grad_of<T, V, 4>(r, st);
+        if (r.plan.narrow) return grad_of<T, V, 4>(r, st);
     }
     return grad_of<T, V, 1>(r, st);
 }
