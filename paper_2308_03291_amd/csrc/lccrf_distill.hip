@@ -419,6 +419,10 @@ __global__ __launch_bounds__(THREADS) void held_kernel(DistillIn in, const float
 
 constexpr int64_t kMostBlocks = 1 << 20;
 
+// Measured, us, bfloat16: up to 256 pieces by teams / by workgroups, 32768 rows of 500 classes 16 / 40, 1000 18 / 35, 2000 28 / 46 (4.7 TB/s), with the gradient 1000 30 / 56,
+// 2000 47 / 79 (5.6).  Loss and gradient of a row in registers / read twice: 8192 rows of 5003 39 / 47, 30000 195 / 215 (5.0), 4096 rows of 100003 389 / 468 (4.2; ragged
+// lengths 357).  Read twice or the loss alone, by 256 threads / by 512: 8192 rows of 10000 32 / 45 (5.1), 30000 87 / 83 (5.9).
+
 template <typename T, bool GRAD>
 hipError_t distill_of(const DistillIn& in, const float* dloss, const float* given, float* loss, float* lse, void* dlogits, hipStream_t st) {
     constexpr int W = Wide<T>::V;

@@ -347,10 +347,10 @@ __global__ __launch_bounds__(256) void wide_kernel(NormIn in, AnyRows dout, int 
 
 // ---- whole sequences in registers ------------------------------------------------------------------------------
 // Where a sequence's groups fit a workgroup's registers, they are read once: a workgroup has whole groups, `lx` pieces (a power of two) wide, of all positions, R
-// pieces a thread.  kRun tiles side by side run on one XCD, one after another: where a tile is half a cache line wide the line is then fetched from memory once.
-constexpr int kRun = 2;
+// pieces a thread.  `run` tiles side by side go to one XCD, one after another: where a tile is half a cache line wide the line is then fetched from memory once, and
+// neighbouring lines of a row soon after each other.
 struct Held {
-    int ppg, lx, groups, tiles, threads, pieces;  // pieces a group; across a workgroup; groups a workgroup, such tiles; its threads, pieces each
+    int ppg, lx, groups, tiles, threads, pieces, run;  // pieces a group; across a workgroup; groups a workgroup, such tiles; its threads, pieces each
 };
 
 // The sum of v over a group's pieces and all positions, for every thread of the group: first over the workgroup's positions, then over the pieces.
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(R > 4 ? 512 : 1024) void held_kernel(NormIn in, Any
                                                                   float* __restrict__ partial) {
     extern __shared__ float lds[];  // held_sum's; GRAD: [threads][W]
     const int tx = threadIdx.x & (p.lx - 1), ty = threadIdx.x / p.lx, ly = blockDim.x / p.lx, C = in.D / in.G;
-    const unsigned rest = blockIdx.x / 8, work = (rest / kRun * 8 + blockIdx.x % 8) * kRun + rest % kRun;
+    const unsigned run = p.run, rest = blockIdx.x / 8, work = (rest / run * 8 + blockIdx.x % 8) * run + rest % run;
     if (work >= static_cast<unsigned>(in.B) * p.tiles) return;
     const int b = work / p.tiles, tile = work - b * p.tiles, group = tx / p.ppg, g = tile * p.groups + group;
     const bool is = group < p.groups && g < in.G;
@@ -980,8 +980,9 @@ Span span_plan(int dtype, int B, int N, int D, int G) {
 }
 
 // Whether a sequence's groups fit registers.  At least 64 bytes of a row a workgroup, more where groups leave fewer lanes without a piece; as many threads as hold
-// the positions in R pieces.  (64 x 512 x 1024 in 32 groups, bf16: 28.7 - 30.7 us with 64 bytes and kRun 2, 30.8 with 128 and 1, 133 with 64 and 1.)  Over
-// kHeldBytes threads hold eight pieces in one go: fewer and larger workgroups.
+// the positions in R pieces.  Runs of sixteen tiles, of two where that would leave XCDs without one.  Measured, us, bfloat16, runs of 1 / 2 / 16 tiles of 64 bytes, of 16 of
+// 128: 64 x 512 x 1024 in 32 groups 133 / 28 / 29 / 31 (4.7 TB/s; two passes 40), with its gradient - / 116 / 109 / 112 (two passes 117), 256 x 512 x 1024 - / 149 / 123 / 117,
+// gradient of 20 x 500 x 2048 in 64 groups - / 72 / 73 / 79.  Over kHeldBytes threads hold eight pieces in one go: fewer and larger workgroups.
 constexpr int64_t kHeldBytes = int64_t{16} << 20;
 bool held_plan(int dtype, int B, int N, int D, int G, Held& p) {
     const bool large = static_cast<int64_t>(B) * N * D * (dtype ? 2 : 4) > kHeldBytes;
@@ -996,6 +997,7 @@ bool held_plan(int dtype, int B, int N, int D, int G, Held& p) {
         if (lx / 2 < pieces && lx / p.ppg * p.ppg * p.lx > p.lx / p.ppg * p.ppg * lx * 9 / 8) p.lx = lx;
     p.groups = p.lx / p.ppg;
     p.tiles = (G - 1) / p.groups + 1;
+    p.run = static_cast<int64_t>(B) * p.tiles >= 256 ? 16 : 2;
     for (const int most : {2, 4, 8})
         for (p.threads = 256; p.threads <= (most > 4 ? 512 : 1024); p.threads *= 2) {
             if (p.threads < p.lx || (N - 1) / (p.threads / p.lx) + 1 > most) continue;
@@ -1033,7 +1035,7 @@ hipError_t alone_of(const NormIn& in, AnyRows dout, const Alone& p, int pieces, 
 
 template <typename T, int W, bool GRAD>
 hipError_t held_of(const NormIn& in, AnyRows dout, const Held& p, const float* given, void* out, float* stats, float* partial, hipStream_t st) {
-    const int64_t blocks = (static_cast<int64_t>(in.B) * p.tiles + 8 * kRun - 1) / (8 * kRun) * (8 * kRun);
+    const int64_t round = 8 * p.run, blocks = (static_cast<int64_t>(in.B) * p.tiles + round - 1) / round * round;
     if (!fits(blocks, p.threads)) return hipErrorInvalidValue;
     const auto kernel = p.pieces == 2 ? held_kernel<T, W, 2, GRAD> : p.pieces == 4 ? held_kernel<T, W, 4, GRAD> : held_kernel<T, W, 8, GRAD>;
     const int entries = p.threads / 64 * (p.lx < 64 ? p.lx : 64);
