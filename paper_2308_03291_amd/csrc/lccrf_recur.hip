@@ -15,7 +15,7 @@ struct RecurRun {
     void* out;
     float* final_state;
     float* saved;  // [B][ceil(N / kRecurSave)][D]
-    float* ends;   // segments > 1: [B][segments][D][2]: what a segment makes of a state, the first one of the call's (kEnds: written)
+    float* ends;   // segments > 1: [B][segments][D][2]: what a segment makes of a state (kEnds: written); the first one: the call's state, and what it makes of it
     RecurPlan plan;
 };
 
@@ -38,13 +38,20 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
     const int stop = in.N - begin < r.plan.seg_len ? in.N : begin + r.plan.seg_len, end = stop < len ? stop : len;
     T* out = static_cast<T*>(r.out) + static_cast<int64_t>(b) * in.N * in.D;
 
+    // (where sequences are cut the second pass takes the call's state from `ends`: a later segment may have written the final one over it already)
+    const bool cut = !(MODE & kEnds) && r.plan.segments > 1;
     RecurChannel ch[V];
     float carry[V], total[V];  // the state in front of the first block, later (the last lanes': behind their positions) of the next one; kEnds: this lane's product of decays
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         ch[j] = recur_channel(in, my.c + j);
-        carry[j] = seg == 0 && r.state ? r.state[static_cast<int64_t>(b) * in.D + my.c + j] : 0.0f;
+        carry[j] = seg == 0 && r.state && !cut ? r.state[static_cast<int64_t>(b) * in.D + my.c + j] : 0.0f;
         total[j] = 1.0f;
+    }
+    if (cut && seg == 0 && r.state) {
+        const Pair made = *reinterpret_cast<const AnyPair*>(r.ends + (static_cast<int64_t>(b) * r.plan.segments * in.D + my.c) * 2);
+#pragma unroll
+        for (int j = 0; j < V; ++j) carry[j] = made[2 * j];
     }
     const bool last = w == W - 1 && sub == SUB - 1;
 
@@ -76,8 +83,9 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
                     const Pair made = *reinterpret_cast<const AnyPair*>(e);
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        mine[2 * j] = product(mine[2 * j], made[2 * j]);
-                        mine[2 * j + 1] = fmaf(made[2 * j], mine[2 * j + 1], made[2 * j + 1]);
+                        const float a = s > 0 ? made[2 * j] : 0.0f;
+                        mine[2 * j] = product(mine[2 * j], a);
+                        mine[2 * j + 1] = fmaf(a, mine[2 * j + 1], made[2 * j + 1]);
                     }
                 }
                 if (sub == 0) pairs[1][w][cl] = mine;  // (the other buffer than the first block's)
@@ -204,8 +212,7 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
         for (int l = done + w * SUB + sub; l < stop; l += W * SUB) my.give(out + static_cast<int64_t>(l) * in.D, zero);
     }
     if constexpr ((MODE & kEnds) != 0) {
-        // the product over all lanes of a channel, each with its positions of all blocks (in front of the first segment is the call's own state: nothing else
-        // is taken from there)
+        // the product over all lanes of a channel, each with its positions of all blocks
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
@@ -220,10 +227,10 @@ __global__ __launch_bounds__(64 * W) void recur_kernel(RecurRun r) {
         Pair made;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            float all = seg == 0 ? 0.0f : 1.0f;
+            float all = 1.0f;
 #pragma unroll
             for (int k = 0; k < W; ++k) all = product(all, pairs[0][k][cl][j]);
-            made[2 * j] = all;
+            made[2 * j] = seg > 0 ? all : r.state ? r.state[static_cast<int64_t>(b) * in.D + my.c + j] : 0.0f;
             made[2 * j + 1] = carry[j];
         }
         *reinterpret_cast<AnyPair*>(r.ends + ((static_cast<int64_t>(b) * r.plan.segments + seg) * in.D + my.c) * 2) = made;  // (a channel of two lanes: the same twice)

@@ -181,6 +181,18 @@ def test_recurrence_over_its_own_state(crf, final_is_state):
     check(final, want["final"], "final")
 
 
+@pytest.mark.parametrize("B,N,D", [(5, 9000, 40), (1, 20000, 130), (9, 700, 257), (3, 4000, 1)])
+def test_recurrence_in_place_and_apart(crf, B, N, D):
+    """The final state written over the call's by whichever segment ends a sequence: the same bits as into memory of its own."""
+    c, lengths, state, _ = recur_case(13, B, N, D, torch.float32, "ragged")
+    lengths[0] = 70  # (its last segment is among the first)
+    apart = crf.lccrf_recurrence(**c, lengths=lengths, state=state)
+    for _ in range(3):
+        carry = state.clone()
+        out, final = crf.lccrf_recurrence(**c, lengths=lengths, state=carry, final=carry)
+        assert torch.equal(out, apart[0]) and torch.equal(final, apart[1])
+
+
 @pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("B,D", [(1, 1), (3, 5), (64, 256), (5, 1023), (700, 12)])
 def test_recurrence_step(crf, t, B, D):
