@@ -111,6 +111,9 @@ __global__ __launch_bounds__(256) void team_kernel(DistillIn in, const float* __
     constexpr int W = Wide<T>::V;
     const int lane = threadIdx.x & 63, t = lane % L, pieces = in.V / W, left = in.V - pieces * W;
     const float per_t = 1.0f / in.temperature, k2 = kLog2e * per_t;
+    // which entry names a class: V is less than a piece more than all lanes'
+    __shared__ uint8_t named[GRAD ? 256 / L : 1][GRAD ? (L * R + 1) * W : 1];
+    [[maybe_unused]] uint8_t* mine = named[GRAD ? threadIdx.x / L : 0];
     const int64_t teams = static_cast<int64_t>(gridDim.x) * (256 / L);
     const int64_t rounds = (in.n + teams - 1) / teams;
     int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / L) + threadIdx.x / L;
@@ -157,7 +160,19 @@ __global__ __launch_bounds__(256) void team_kernel(DistillIn in, const float* __
         if (!GRAD && there && t == 0) lse[row] = some ? fmaf(M, per_t, log_s) : 0.0f;
         if constexpr (GRAD) {
             const float scale = there ? dloss[row] * in.temperature : 0.0f, share = 1.0f / s;
-            top.gather_twice(in.K);
+            // A class that is named once is that entry's own: of a class's entries one stays in the table, the others see it.  Comparing all with all, which costs K steps
+            // a row, is for waves that have a class twice.
+            bool twice = false;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (top.id[e] >= 0) mine[top.id[e]] = static_cast<uint8_t>(t + e * L);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int e = 0; e < E; ++e) twice = twice || (top.id[e] >= 0 && mine[top.id[e]] != t + e * L);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            if (__ballot(twice)) top.gather_twice(in.K);
             if (there) {
                 T* o = dlogits + row * in.V;
 #pragma unroll
