@@ -105,7 +105,8 @@ template <typename T, int L, int E> struct Entries {
 };
 
 // ---- few classes: a team of L lanes a position -----------------------------------------------------------------
-// R pieces of W classes a lane, and one more class with the first lanes where V is no multiple of W.
+// R pieces of W classes a lane, and one more class with the first lanes where V is no multiple of W.  Looking for classes named twice by the table instead of comparing
+// all entries with all: 46408 rows of 110 classes with 86 entries 31 us / 187, 32768 of 2000 with 64 50 / 72.
 template <typename T, int L, int R, int E, bool GRAD>
 __global__ __launch_bounds__(256) void team_kernel(DistillIn in, const float* __restrict__ dloss, float* __restrict__ loss, float* __restrict__ lse, T* dlogits) {
     constexpr int W = Wide<T>::V;

@@ -63,7 +63,8 @@ template <int W> __device__ __forceinline__ void weights_of(const NormIn& in, in
 
 // ---- every position by itself ---------------------------------------------------------------------------------
 // A team of `team` lanes has a group of a position, R pieces a lane, all of it in registers.  A wave's teams have `groups` groups of so many
-// positions; a workgroup keeps to its groups, so that the gradient's sums over positions stay in registers.
+// positions; a workgroup keeps to its groups, so that the gradient's sums over positions stay in registers.  Forwards 64 x 512 x 1024 in 16 groups, bfloat16, 34 us
+// (3.9 TB/s); with its gradient 128 x 128 x 1024 in eight, float, 77 us (3.5 TB/s), in seven of 1001, ragged, 89 - 93 (rows begin anywhere in a line).
 struct Alone {
     int ppg, team, groups, tiles;  // pieces a group, lanes a team, groups a wave, such tiles of groups in all
     int64_t blocks;                // workgroups a tile
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(256) void alone_kernel(NormIn in, AnyRows dout, Alo
         if (!ALL) return sum_across(v, p.team);
         v = sum_across(v, 64);
         if (lane == 0) sums[which * 4 + wave] = v;
-        lds_sync();  // (a place is written again after three other such sums)
+        lds_sync();  // (a place is written again behind the wait of another such sum: all have read it)
         return sums[which * 4] + sums[which * 4 + 1] + sums[which * 4 + 2] + sums[which * 4 + 3];
     };
     const bool is = g < in.G;
@@ -553,7 +554,8 @@ __global__ __launch_bounds__(R > 4 ? 512 : 1024) void held_kernel(NormIn in, Any
 // ---- whole sequences ------------------------------------------------------------------------------------------
 // Two passes: sums of every chunk of positions, then the results; the second finds most of what it reads in the memory-side cache.  Workgroups are lx pieces wide
 // (whole groups, or one of the `parts` of a group that is wider), ly = 256 / lx positions high and go over a chunk of a sequence's positions.  What a group's
-// chunks come to is joined by every workgroup of the second pass for its own groups, all in the same order: no launch between the two.
+// chunks come to is joined by every workgroup of the second pass for its own groups, all in the same order: no launch between the two.  4 x 16384 x 512 in eight
+// groups, bfloat16, lengths from 9000 on: 9 us and 22, of which 23 are the bytes' at the rate of a copy.
 struct Span {
     int ppg, lx, groups, parts, tiles;  // pieces a group; across a workgroup; groups a workgroup or workgroups a group; tiles a row
     int chunk, chunks;                  // positions a workgroup, workgroups a sequence
