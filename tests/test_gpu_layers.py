@@ -372,6 +372,27 @@ def test_distill(crf, t, kind, n, V, K):
         check(also, given["loss"], "loss of lse")
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("V,K", [(40, 6), (64, 12), (200, 30), (500, 60), (110, 86), (1000, 200), (3000, 20)])
+def test_distill_beside_a_class_named_twice(crf, t, V, K):
+    """Entries that name a class twice change their own position alone, whoever shares its wave: the others keep their bits."""
+    g = generator(V + K)
+    logits, dloss = normal(g, 301, V, dtype=t), normal(g, 301)
+    ids, teacher = top_of(g, logits, K, "top")
+    before = crf.lccrf_distill_grad(dloss, logits, ids, teacher)
+    twice = [7, 150, 299]  # (positions that have entries)
+    assert bool((ids[twice] >= 0).all())
+    moved = ids[twice, 1].long()
+    ids[twice, 1] = ids[twice, 0]
+    after = crf.lccrf_distill_grad(dloss, logits, ids, teacher)
+    others = torch.ones(301, dtype=torch.bool, device=DEV)
+    others[twice] = False
+    assert torch.equal(after[others], before[others])
+    for row, was in zip(twice, moved.tolist()):
+        changed = (after[row] != before[row]).nonzero().flatten().tolist()
+        assert sorted(changed) == sorted({int(ids[row, 0]), was}), row
+
+
 @pytest.mark.parametrize("V", (40, 3001, 30000))
 def test_distill_of_masked_classes(crf, V):
     """Classes masked with -inf or the type's lowest value have probability 0; where the teacher names one, the loss is infinite and the gradient
