@@ -400,6 +400,12 @@ __global__ __launch_bounds__(THREADS) void held_kernel(DistillIn in, const float
         tops[wave] = wave_top;
         sums[wave] = s;
     }
+    // dlogits may be the logits: what the loss reads of the named classes has come before any of the workgroup's stores goes out.  (The barrier orders LDS alone, and
+    // a slot whose entries all name classes again has left nothing there.)
+    if (wave == 0) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) asm volatile("" : "+v"(top.x[e]));
+    }
     lds_sync();
     float M = tops[0];
 #pragma unroll
