@@ -6,6 +6,7 @@
 // Means and sums of squares are taken in two passes over values in registers and joined pairwise with their counts,
 //     n = n1 + n2,  d = mean2 - mean1,  mean = mean1 + d n2 / n,  M = M1 + M2 + d^2 n1 n2 / n,
 // always in the same order: no difference of large numbers, however far the mean is from 0.
+#include "lccrf_ahead.h"
 #include "lccrf_layers.h"
 
 namespace lccrf {
@@ -617,6 +618,7 @@ template <typename V, typename Of, typename F> __device__ __forceinline__ int jo
 
 // Moments of every group's part over a chunk: [B][G][chunks][parts][2] (mean, M; the count follows from the lengths).
 constexpr int kBatch = 4;  // positions in flight
+static_assert(kMaxPositions - 1 + kBatch * 256 < int64_t{1} << 31, "where a thread's next turn begins fits 32 bits");
 template <typename T, int W>
 __global__ __launch_bounds__(256) void moments_kernel(NormIn in, Span p, float* __restrict__ made) {
     __shared__ Moments lds[256];
@@ -628,7 +630,7 @@ __global__ __launch_bounds__(256) void moments_kernel(NormIn in, Span p, float* 
     Part<T, W> v[kBatch];
     const auto fetch = [&](int l) {
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) v[u].load(line<T>(in.x, my.b, l + u * my.ly < stop ? l + u * my.ly : stop - 1) + at.c, W);
+        for (int u = 0; u < kBatch; ++u) v[u].load(line<T>(in.x, my.b, or_last(l, u * my.ly, stop)) + at.c, W);
     };
     int l = begin + my.ty;
     fetch(l);
@@ -757,7 +759,7 @@ __global__ __launch_bounds__(256) void apply_kernel(NormIn in, AnyRows dout, Spa
     const auto fetch = [&](int l) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int at_l = l + u * my.ly < end ? l + u * my.ly : end - 1;
+            const int at_l = or_last(l, u * my.ly, end);
             v[u].load(line<T>(in.x, my.b, at_l) + at.c, W);
             if (GRAD) d[u].load(line<T>(dout, my.b, at_l) + at.c, W);
         }
@@ -837,8 +839,8 @@ __global__ __launch_bounds__(256) void columns_kernel(NormIn in, AnyRows dout, S
     const auto fetch = [&](int l) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            on[u] = my.is && l + u * my.ly < stop;
-            const int pos = l + u * my.ly < stop ? l + u * my.ly : stop - 1, b = ALONE ? pos / in.N : my.b, row = ALONE ? pos - b * in.N : pos;
+            on[u] = my.is && before(l, u * my.ly, stop);
+            const int pos = or_last(l, u * my.ly, stop), b = ALONE ? pos / in.N : my.b, row = ALONE ? pos - b * in.N : pos;
             if (ALONE) {
                 on[u] = on[u] && row < length_at(in.lengths, b, in.N);
                 means[u] = given[(static_cast<int64_t>(pos) * in.G + at.group) * 2];

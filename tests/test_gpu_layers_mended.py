@@ -1,4 +1,5 @@
-"""Calls of the layers of include/lccrf_layers.h at the edges of what their header allows: repeated entries over the logits themselves."""
+"""Calls of the layers of include/lccrf_layers.h at the edges of what their header allows: the longest sequences, repeated entries over the logits
+themselves."""
 import pytest
 import torch
 
@@ -6,6 +7,31 @@ import layers_reference as ref
 from test_gpu_layers import DEV, TYPES, U, _dirty_memory, check, crf, generator, normal  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+MOST = 2 ** 31 - 1024  # positions of a call
+
+
+# ---- group norm -----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("N", (MOST, MOST - 700))
+def test_group_norm_of_the_longest_sequence(crf, N):
+    """One channel, so that a workgroup's threads are 256 positions high and what they load ahead would reach past 2^31.  x is 1 and -1 in turn: the mean is 0 and
+    the deviation 1 / sqrt(1 + eps), which is 1 in bfloat16."""
+    x = torch.ones(1, N, 1, dtype=torch.bfloat16, device=DEV)
+    x[:, 1::2] = -1.0
+    stats = crf.group_norm_stats(x, 1)
+    out = crf.lccrf_group_norm(x, groups=1, silu=False, stats=stats)
+    assert torch.equal(out, x)
+    del out
+    # a thread joins 512 chunks one after another, some 60 additions and joinings besides
+    off = (512 + 60) * U
+    assert abs(float(stats[0, 0, 0])) <= 2 * off and abs(float(stats[0, 0, 1]) - (1 + 1e-5) ** -0.5) <= 2 * off
+    w, bias = torch.full((1,), 2.0, device=DEV), torch.zeros(1, device=DEV)
+    g = crf.lccrf_group_norm_grad(x, x, w, bias, groups=1, silu=False, stats=stats)
+    # dx = rstd (2 x - hat mean(2 x hat)) = 2 x rstd (1 - rstd^2), 2e-5 of x; the mean of 2 is off by as many additions, rstd as above
+    assert float(g.dx.abs().max()) <= 2e-5 + 8 * off
+    # 8192 chunks' sums one after another
+    assert abs(float(g.dweight) / N - (1 + 1e-5) ** -0.5) <= (8192 + 60) * U + 2 * off and abs(float(g.dbias)) <= (8192 + 60) * U * N
 
 
 # ---- distillation ---------------------------------------------------------------------------------------------
