@@ -93,7 +93,8 @@ int lccrf_group_norm_grad(const lccrf_rows* dout, const lccrf_rows* x, lccrf_dty
  *     lse  = log sum_v exp(logits[v] / t)
  *     loss = t^2 * sum_k q_k * (log q_k - (logits[ids_k] / t - lse))
  *   logits [n][V], rows logits_row elements apart; loss and lse float [n].  A position without an entry (padding) has loss 0 and lse 0, and
- *   its logits are not read.  t is positive and finite, K at most LCCRF_MAX_TOP, V at most 2^30; n = 0 is allowed, n at most 2^31 - 1.
+ *   its logits are not read.  t is finite and at least 2^-126, K at most LCCRF_MAX_TOP, V at most 2^30; n = 0 is allowed, n at most 2^31 - 1.
+ *   (The loss is a difference of logarithms: what their rounding leaves in it grows as t^2.)
  */
 #define LCCRF_MAX_TOP 256
 int lccrf_distill(const void* logits, int64_t logits_row, lccrf_dtype dtype, const int32_t* ids, const float* teacher, int64_t n, int V,

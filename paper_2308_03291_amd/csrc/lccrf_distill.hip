@@ -1,7 +1,7 @@
 // Distillation from a teacher's top logits, and its gradient.
 //
 // With M the largest logit, s = sum exp((x - M) / t), Mt and st the teacher's: log q_k = (v_k - Mt) / t - log st, log p = (x - M) / t - log s, so
-//     loss = t^2 sum_k q_k (((v_k - Mt) - (x[id_k] - M)) / t - log(st / s)),   lse = M / t + log s,   dlogits = dloss t (exp((x - M) / t) / s - q).
+//     loss = t sum_k q_k ((v_k - Mt) - (x[id_k] - M) + t log(s / st)),   lse = M / t + log s,   dlogits = dloss t (exp((x - M) / t) / s - q).
 // The logits read (and their gradient written) are what bounds it.  Few classes: a team of lanes has a position in registers, and reads it
 // once.  Many: a workgroup a position.  A row is taken in whole pieces of 16 bytes, what is left over one class a thread: no two
 // threads have the same class, so the gradient may be written over the logits.
@@ -66,12 +66,13 @@ template <typename T, int L, int E> struct Entries {
         for (int e = 0; e < E; ++e) v[e] = id[e] >= 0 ? v[e] * r : 0.0f;
         return kLn2f * __builtin_amdgcn_logf(sum);
     }
-    // sum of q (log q - log p), M and log_s the student's
-    __device__ __forceinline__ float divergence(float per_t, float log_st, float M, float log_s) const {
+    // The loss, M and log_s the student's.  One t is taken into the sum: differences of logits divided by a small t could pass the largest float where what is
+    // left of them times t^2 does not.
+    __device__ __forceinline__ float loss(float t, float log_st, float M, float log_s) const {
         float sum = 0.0f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum += v[e] == 0.0f ? 0.0f : v[e] * fmaf(lead[e] - (x[e] - M), per_t, log_s - log_st);
-        return team_sum<L>(sum);
+        for (int e = 0; e < E; ++e) sum += v[e] == 0.0f ? 0.0f : v[e] * fmaf(log_s - log_st, t, lead[e] - (x[e] - M));
+        return t * team_sum<L>(sum);
     }
     // q of every class that is named, with its first entry; that entry alone keeps its id.
     __device__ __forceinline__ void gather_twice(int K) {
@@ -155,8 +156,8 @@ __global__ __launch_bounds__(256) void team_kernel(DistillIn in, const float* __
         s = team_sum<L>(s + last);
         const float log_s = kLn2f * __builtin_amdgcn_logf(s), log_st = top.settle(k2);
         if (loss) {
-            const float d = top.divergence(per_t, log_st, M, log_s);
-            if (there && t == 0) loss[row] = some ? in.temperature * in.temperature * d : 0.0f;
+            const float d = top.loss(in.temperature, log_st, M, log_s);
+            if (there && t == 0) loss[row] = some ? d : 0.0f;
         }
         if (!GRAD && there && t == 0) lse[row] = some ? fmaf(M, per_t, log_s) : 0.0f;
         if constexpr (GRAD) {
@@ -273,8 +274,8 @@ __global__ __launch_bounds__(THREADS) void row_kernel(DistillIn in, const float*
         if (wave == 0) {
             const float log_st = top.settle(k2);
             if (loss) {
-                const float d = top.divergence(per_t, log_st, M, log_s);
-                if (lane == 0) loss[row] = in.temperature * in.temperature * d;
+                const float d = top.loss(in.temperature, log_st, M, log_s);
+                if (lane == 0) loss[row] = d;
             }
             if (!GRAD && lane == 0) lse[row] = fmaf(M, per_t, log_s);
             if (GRAD) top.gather_twice(in.K);
@@ -415,8 +416,8 @@ __global__ __launch_bounds__(THREADS) void held_kernel(DistillIn in, const float
     for (int v = 0; v < kWaves; ++v) s += sums[v] * exp2_fast((tops[v] - M) * k2);
     const float scale = dloss[row] * in.temperature, share = scale / s;
     if (wave == 0 && loss) {
-        const float d = top.divergence(per_t, log_st, M, kLn2f * __builtin_amdgcn_logf(s));
-        if (lane == 0) loss[row] = in.temperature * in.temperature * d;
+        const float d = top.loss(in.temperature, log_st, M, kLn2f * __builtin_amdgcn_logf(s));
+        if (lane == 0) loss[row] = d;
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {

@@ -11,10 +11,12 @@ inline size_t size_of(int dt) { return dt == LCCRF_F32 ? 4 : 2; }
 inline bool lies(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline AnyRows rows(const lccrf_rows& r) { return {r.data, r.batch, r.row}; }
 inline bool positive(float v) { return v > 0.0f && v <= 3.402823466e38f; }
+// A scalar that kernels divide by: below the least normal float its inverse is none.
+inline bool normal(float v) { return positive(v) && v >= 1.17549435e-38f; }
 inline bool sizes_ok(int B, int N, int D) { return B >= 1 && N >= 1 && D >= 1 && D <= 1 << 22 && static_cast<int64_t>(B) * N <= kMaxPositions; }
 inline bool norm_ok(int dt, int B, int N, int D, int G) { return type_ok(dt) && sizes_ok(B, N, D) && G >= 1 && G <= D && D % G == 0; }
 inline bool distill_ok(int dt, int64_t n, int V, int K, float t) {
-    return type_ok(dt) && n >= 0 && n < (int64_t{1} << 31) && V >= 1 && V <= 1 << 30 && K >= 1 && K <= LCCRF_MAX_TOP && positive(t);
+    return type_ok(dt) && n >= 0 && n < (int64_t{1} << 31) && V >= 1 && V <= 1 << 30 && K >= 1 && K <= LCCRF_MAX_TOP && normal(t);
 }
 
 inline int status(hipError_t e) { return e == hipSuccess ? LCCRF_OK : e == hipErrorInvalidValue ? LCCRF_EINVAL : LCCRF_ELAUNCH; }

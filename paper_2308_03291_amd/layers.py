@@ -273,8 +273,8 @@ def lccrf_distill(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor
 
         loss = t^2 sum_k q_k (log q_k - log p[ids_k]),  q = softmax(teacher / t),  p = softmax(logits / t),  lse = log sum exp(logits / t).
 
-    An entry whose id is outside [0, V) or whose logit is -inf is not there; a class may be named twice; a position without an entry (padding) has
-    loss and lse 0."""
+    t is finite and at least 2^-126.  An entry whose id is outside [0, V) or whose logit is -inf is not there; a class may be named twice; a position without
+    an entry (padding) has loss and lse 0."""
     code, _, dev, lead, n, V, K, row, pids, pteacher = _distill_args(logits, ids, teacher)
     loss = _result(loss, "loss", lead, torch.float32, logits.device, dev)
     lse = _result(lse, "lse", lead, torch.float32, logits.device, dev)

@@ -1,5 +1,5 @@
-"""Calls of the layers of include/lccrf_layers.h at the edges of what their header allows: the longest sequences, repeated entries over the logits
-themselves."""
+"""Calls of the layers of include/lccrf_layers.h at the edges of what their header allows: the longest sequences, temperatures far from 1,
+repeated entries over the logits themselves."""
 import pytest
 import torch
 
@@ -54,3 +54,52 @@ def test_distill_over_the_logits_with_entries_that_only_repeat(crf, t, V, K):
         over = logits.clone()
         assert torch.equal(crf.lccrf_distill_grad(dloss, over, ids, teacher, temperature=2.0, loss=over_loss, out=over), apart)
         assert torch.equal(over_loss, apart_loss)
+
+
+@pytest.mark.parametrize("t", (2.0 ** -120, 1e-30, 1e-10, 3e-3, 1e4, 2.0 ** 60))
+@pytest.mark.parametrize("V,K", [(37, 9), (3001, 70), (9001, 64), (200003, 20)])
+def test_distill_at_temperatures_far_from_one(crf, t, V, K):
+    """Losses of the size of t differences of logits, and of t^2."""
+    g = generator(V)
+    logits, dloss = normal(g, 7, V, scale=2.0), normal(g, 7)
+    teacher, ids = torch.topk(logits + normal(g, 7, V), K, -1)
+    ids = ids.to(torch.int32)
+    t = float(torch.tensor(t))
+    want, given = (ref.distill(logits, ids, teacher, t, dloss, from_lse=k) for k in (False, True))
+    loss, lse = crf.lccrf_distill(logits, ids, teacher, temperature=t)
+    check(loss, want["loss"], "loss")
+    check(lse, want["lse"], "lse")
+    assert t > 1 or float(want["loss"][0].abs().max()) > 0.1 * t
+    check(crf.lccrf_distill_grad(dloss, logits, ids, teacher, temperature=t, loss=loss), want["dlogits"], "dlogits")
+    check(loss, want["loss"], "loss with the gradient")
+    if t > 1e-3:
+        check(crf.lccrf_distill_grad(dloss, logits, ids, teacher, temperature=t, lse=lse), given["dlogits"], "dlogits of lse")
+
+
+@pytest.mark.parametrize("t", (2.0 ** -126, 1e30, 3e38))
+@pytest.mark.parametrize("V,K", [(9, 9), (3001, 70), (30000, 5)])
+def test_distill_at_the_ends_of_the_temperatures(crf, t, V, K):
+    """Gradients of t (p - q) where t^2 or 1 / t is no normal float; the loss there is 0, or past every float, and no NaN."""
+    g = generator(V)
+    logits, dloss = normal(g, 5, V, scale=2.0), normal(g, 5, scale=1e-2)
+    teacher, ids = torch.topk(logits + normal(g, 5, V), K, -1)
+    ids, loss = ids.to(torch.int32), torch.empty(5, device=DEV)
+    t = float(torch.tensor(t))
+    check(crf.lccrf_distill_grad(dloss, logits, ids, teacher, temperature=t, loss=loss), ref.distill(logits, ids, teacher, t, dloss)["dlogits"], "dlogits")
+    assert not bool(loss.isnan().any()) and (t < 1 or K == V or bool(torch.isposinf(loss).all())) and (t > 1 or bool((loss.abs() < 1e-36).all()))
+
+
+@pytest.mark.parametrize("V", (40, 3001, 30000))
+def test_distill_of_a_named_class_at_the_lowest_logit(crf, V):
+    """t^2 times its distance by t passes no float where the distance divided by t does."""
+    g = generator(V)
+    logits = normal(g, 6, V)
+    logits[:, 3] = torch.finfo(torch.float32).min
+    ids = torch.tensor([[3, 7, 11, 20]], dtype=torch.int32, device=DEV).repeat(6, 1)
+    teacher = normal(g, 6, 4)
+    want = ref.distill(logits, ids, teacher, 0.25, torch.ones(6))
+    assert 1e30 < float(want["loss"][0].min()) < float(want["loss"][0].max()) < 1e38
+    loss = torch.empty(6, device=DEV)
+    crf.lccrf_distill_grad(torch.ones(6, device=DEV), logits, ids, teacher, temperature=0.25, loss=loss)
+    check(loss, want["loss"], "loss with the gradient")
+    check(crf.lccrf_distill(logits, ids, teacher, temperature=0.25)[0], want["loss"], "loss")
