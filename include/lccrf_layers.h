@@ -68,7 +68,7 @@ int lccrf_recurrence_step(const lccrf_recurrence_inputs* in, lccrf_dtype dtype, 
  * all positions of a sequence (per_position 0) or at one position (per_position 1: what streams can run), of n values in all:
  *     mean = sum x / n,   var = sum (x - mean)^2 / n,   rstd = 1 / sqrt(var + eps)
  *     y    = (x - mean) * rstd * weight + bias,         out = y * s(y)   (silu 0: y)
- *   x [B][N][D] rows, weight [D] or NULL (= 1), bias [D] or NULL (= 0), out [B][N][D]; eps is positive and finite.
+ *   x [B][N][D] rows, weight [D] or NULL (= 1), bias [D] or NULL (= 0), out [B][N][D]; eps is finite and at least 2^-126.
  * stats: NULL, or [B][G][2] ([B][N][G][2] per position) floats that take (mean, rstd), 0 where there is nothing to normalise:
  * what the gradient would otherwise compute again.
  */

@@ -11,7 +11,7 @@ inline size_t size_of(int dt) { return dt == LCCRF_F32 ? 4 : 2; }
 inline bool lies(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline AnyRows rows(const lccrf_rows& r) { return {r.data, r.batch, r.row}; }
 inline bool positive(float v) { return v > 0.0f && v <= 3.402823466e38f; }
-// A scalar that kernels divide by: below the least normal float its inverse is none.
+// A scalar that kernels divide by, or take a root's inverse of: below the least normal float that is none.
 inline bool normal(float v) { return positive(v) && v >= 1.17549435e-38f; }
 inline bool sizes_ok(int B, int N, int D) { return B >= 1 && N >= 1 && D >= 1 && D <= 1 << 22 && static_cast<int64_t>(B) * N <= kMaxPositions; }
 inline bool norm_ok(int dt, int B, int N, int D, int G) { return type_ok(dt) && sizes_ok(B, N, D) && G >= 1 && G <= D && D % G == 0; }
@@ -94,7 +94,7 @@ size_t lccrf_group_norm_grad_workspace_bytes(lccrf_dtype dtype, int B, int N, in
 
 int lccrf_group_norm(const lccrf_rows* x, lccrf_dtype dtype, const float* weight, const float* bias, const int32_t* lengths, int B, int N, int D, int G, int per_position,
                      float eps, int silu, void* out, float* stats, void* workspace, size_t workspace_bytes, void* stream) {
-    if (!norm_ok(dtype, B, N, D, G) || !positive(eps)) return LCCRF_EINVAL;
+    if (!norm_ok(dtype, B, N, D, G) || !normal(eps)) return LCCRF_EINVAL;
     if (!x || !x->data || !out) return LCCRF_ENULL;
     if (!room(workspace, workspace_bytes, norm_workspace(dtype, B, N, D, G, per_position != 0))) return LCCRF_EWORKSPACE;
     const size_t e = size_of(dtype);
@@ -106,7 +106,7 @@ int lccrf_group_norm(const lccrf_rows* x, lccrf_dtype dtype, const float* weight
 int lccrf_group_norm_grad(const lccrf_rows* dout, const lccrf_rows* x, lccrf_dtype dtype, const float* weight, const float* bias, const int32_t* lengths, int B, int N,
                           int D, int G, int per_position, float eps, int silu, const float* stats, void* dx, float* dweight, float* dbias, void* workspace,
                           size_t workspace_bytes, void* stream) {
-    if (!norm_ok(dtype, B, N, D, G) || !positive(eps)) return LCCRF_EINVAL;
+    if (!norm_ok(dtype, B, N, D, G) || !normal(eps)) return LCCRF_EINVAL;
     if (!dout || !dout->data || !x || !x->data || !dx) return LCCRF_ENULL;
     if (!room(workspace, workspace_bytes, norm_grad_workspace(dtype, B, N, D, G, per_position != 0))) return LCCRF_EWORKSPACE;
     const size_t e = size_of(dtype);

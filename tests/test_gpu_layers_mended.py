@@ -34,6 +34,15 @@ def test_group_norm_of_the_longest_sequence(crf, N):
     assert abs(float(g.dweight) / N - (1 + 1e-5) ** -0.5) <= (8192 + 60) * U + 2 * off and abs(float(g.dbias)) <= (8192 + 60) * U * N
 
 
+@pytest.mark.parametrize("alone", (False, True))
+@pytest.mark.parametrize("N", (9, 3000))
+def test_group_norm_of_equal_values_with_the_least_eps(crf, alone, N):
+    """No spread and an eps of 2^-126: 0 times 2^63, and the bias."""
+    bias = normal(generator(1), 8)
+    out = crf.lccrf_group_norm(torch.full((2, N, 8), 3.0, device=DEV), None, bias, groups=2, eps=2.0 ** -126, silu=False, per_position=alone)
+    assert torch.equal(out, bias.expand(2, N, 8))
+
+
 # ---- distillation ---------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("t", TYPES)
