@@ -182,13 +182,16 @@ class Student(Tagger):
 
     def loss_and_gradients(self, ids, tags, lengths=None, *, teacher=None, share: float = 0.5, temperature: float = 2.0):
         """(the loss, its gradient by every parameter).  ``teacher``: (tags, emissions) of ``top_emissions``; then ``share`` of the loss is the mean distance a
-        sequence of the student's emissions from those, summed over its positions, the rest the tags' negative log-likelihood."""
+        sequence of the student's emissions from those, summed over its positions within the lengths (whether the teacher's tags are masked past them or
+        not), the rest the tags' negative log-likelihood."""
         p, D = self.params, self.D
         a = self.forward(ids, lengths, train=True)
         loss, demit, dtrans = self._through_chain(a["emit"], tags, lengths)
         grads = {"trans": dtrans}
         if teacher is not None:
             weights = torch.full(ids.shape, share / ids.shape[0], device=ids.device)
+            if lengths is not None:
+                weights.masked_fill_(torch.arange(ids.shape[1], device=ids.device)[None] >= lengths[:, None], 0.0)
             far = torch.empty_like(weights)
             dfar = crf.lccrf_distill_grad(weights, a["emit"], *teacher, temperature=temperature, loss=far)
             loss = (1 - share) * loss + (weights * far).sum()
