@@ -444,7 +444,9 @@ constexpr int64_t kMostBlocks = 1 << 20;
 
 // Measured, us, bfloat16: up to 256 pieces by teams / by workgroups, 32768 rows of 500 classes 16 / 40, 1000 18 / 35, 2000 28 / 46 (4.7 TB/s), with the gradient 1000 30 / 56,
 // 2000 47 / 79 (5.6).  Loss and gradient of a row in registers / read twice: 8192 rows of 5003 39 / 47, 30000 195 / 215 (5.0), 4096 rows of 100003 389 / 468 (4.2; ragged
-// lengths 357).  Read twice or the loss alone, by 256 threads / by 512: 8192 rows of 10000 32 / 45 (5.1), 30000 87 / 83 (5.9).
+// lengths 357).  25 pieces a thread take 128 registers, the last that leave room for two workgroups a CU, 32 take 156: 2048 rows of 100003 196 / 229, of 70001 133 / 155; with
+// more than 64 entries there is room for one either way (270 / 270), and 32 serve them all.  Read twice or the loss alone, by 256 threads / by 512: 8192 rows of
+// 10000 32 / 45 (5.1), 30000 87 / 83 (5.9).
 
 template <typename T, bool GRAD>
 hipError_t distill_of(const DistillIn& in, const float* dloss, const float* given, float* loss, float* lse, void* dlogits, hipStream_t st) {
@@ -475,7 +477,7 @@ hipError_t distill_of(const DistillIn& in, const float* dloss, const float* give
             if (pieces <= 2048) return go(many ? held_kernel<T, 256, 8, kEntries> : held_kernel<T, 256, 8, 1>, 256);
             if (pieces <= 4096) return go(many ? held_kernel<T, 512, 8, kEntries> : held_kernel<T, 512, 8, 1>, 512);
             if (pieces <= 8192) return go(many ? held_kernel<T, 512, 16, kEntries> : held_kernel<T, 512, 16, 1>, 512);
-            if (pieces <= 12800) return go(many ? held_kernel<T, 512, 25, kEntries> : held_kernel<T, 512, 25, 1>, 512);
+            if (pieces <= 12800 && !many) return go(held_kernel<T, 512, 25, 1>, 512);
             return go(many ? held_kernel<T, 512, 32, kEntries> : held_kernel<T, 512, 32, 1>, 512);
         }
     }
