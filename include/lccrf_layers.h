@@ -28,7 +28,8 @@ extern "C" {
  *     h[l]   = exp(u[l]) * h[l-1] + sqrt(1 - exp(2 u[l])) * s(g[l] + g_bias) * x[l],     h[-1] = state or 0
  *     out[l] = h[l] * z[l] * s(z[l])                                                     (z.data NULL: h[l])
  *   x, f, g, z [B][N][D] rows; decay [D], f_bias and g_bias [D] or NULL (= 0); state and final [B][D] float (state NULL: 0;
- *   final NULL: not wanted; final may be state itself).  rate is positive and finite, D at most 2^22.
+ *   final NULL: not wanted; final may be state itself).  rate is positive and finite, and so has to be its product
+ *   with log(1 + exp(decay)) in float; D at most 2^22.
  * saved: NULL, or lccrf_recurrence_saved_bytes of device memory that takes what the gradient would otherwise compute again (the
  * states in front of every eighth position; its layout is the library's own).
  */
@@ -102,8 +103,10 @@ int lccrf_distill(const void* logits, int64_t logits_row, lccrf_dtype dtype, con
 
 /*
  * Its gradient: dlogits[v] = dloss * t * (p[v] - sum of q_k with ids_k = v), [n][V] dense, 0 for positions without an entry; dloss
- * float [n].  lse: of lccrf_distill, or NULL (computed again).  loss: NULL, or [n] that takes the loss as well: where dloss is known ahead (weights
- * of positions), this one call is all of a training step's loss.  dlogits may be logits itself (logits_row = V then).
+ * float [n].  lse: of lccrf_distill, or NULL (computed again, with exponentials of differences from the largest logit).  A given lse is looked
+ * at in rows past 256 pieces of 16 bytes, where p is exp(logits / t - lse): what both have lost at their own size, some
+ * 2^-22 (|lse| + |logits| / t), is in p as a relative error.  loss: NULL, or [n] that takes the loss as well: where dloss is known ahead
+ * (weights of positions), this one call is all of a training step's loss.  dlogits may be logits itself (logits_row = V then).
  */
 int lccrf_distill_grad(const float* dloss, const void* logits, int64_t logits_row, lccrf_dtype dtype, const int32_t* ids,
                        const float* teacher, int64_t n, int V, int K, float temperature, const float* lse, float* loss, void* dlogits,

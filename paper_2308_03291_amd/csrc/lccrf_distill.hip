@@ -74,7 +74,8 @@ template <typename T, int L, int E> struct Entries {
         for (int e = 0; e < E; ++e) sum += v[e] == 0.0f ? 0.0f : v[e] * fmaf(log_s - log_st, t, lead[e] - (x[e] - M));
         return t * team_sum<L>(sum);
     }
-    // q of every class that is named, with its first entry; that entry alone keeps its id.
+    // q of every class that is named, with its first entry; that entry alone keeps its id.  K steps of one wave: rows of few classes take them only where a class is named twice
+    // (team_kernel's table), rows by workgroups always, where the other waves read on meanwhile or wait.
     __device__ __forceinline__ void gather_twice(int K) {
         float all[E];
         bool first[E];

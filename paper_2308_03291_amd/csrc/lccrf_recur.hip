@@ -288,8 +288,8 @@ constexpr int kPositions = 4, kWaves = 8, kFewWaves = 4;  // a lane's positions;
 int channels_a_lane(int D) { return D == 1 ? 1 : 2; }
 
 // Measured, us, wide tiles / narrow / segments (B x N x D, bfloat16, no gate but in the first): 64x512x2048 145 / 158 / 252, 16x1000x1024 51 / 47 / 54, 30x300x300
-// 21 / 18 / 21, 8x256x1024 16 / 14 / 19, 4x5000x1024 228 / 91 / 64, 2x10000x256 446 / 143 / 29, 4x16384x514 865 / 263 / 118.  The first is 4.65 TB/s (float 5.5), of
-// 5.14 that a copy has; segments are read twice: the last one's two passes take 56 us (3.6 TB/s) and 60 (4.5).
+// 21 / 18 / 21, 8x256x1024 16 / 14 / 19, 4x5000x1024 228 / 91 / 64, 2x10000x256 446 / 143 / 29, 4x16384x514 865 / 263 / 118.  The first is 4.65 TB/s (float 5.5;
+// a copy, which writes as much as it reads, 5.14); segments are read twice: the last one's two passes take 56 us (3.6 TB/s) and 60 (4.5).
 static_assert(kWaves != kFewWaves, "workgroups of so few have segments");
 RecurPlan recur_plan(int B, int N, int D) { return recur_plan_of(B, N, D, 256, 256, 512); }
 

@@ -285,8 +285,8 @@ def lccrf_distill(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor
 def lccrf_distill_grad(dloss: torch.Tensor, logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, *, temperature: float = 1.0,
                        lse: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of ``lccrf_distill`` by its logits, dloss t (p - q) [..., V], given dloss (float32, the positions' shape).  ``lse``: of the forward
-    call; computed again without it.  ``loss`` takes the loss as well: where dloss is known ahead, this one call is all of a training step's loss.
-    ``out`` may be ``logits`` itself."""
+    call; computed again without it (more closely in rows of many classes where |lse| or |logits| / t is large: p is exp(logits / t - lse) of
+    rounded numbers).  ``loss`` takes the loss as well: where dloss is known ahead, this one call is all of a training step's loss.  ``out`` may be ``logits`` itself."""
     code, dtype, dev, lead, n, V, K, row, pids, pteacher = _distill_args(logits, ids, teacher)
     f32 = torch.float32
     pd, ps, pl = _dense(dloss, "dloss", lead, f32, dev), _dense(lse, "lse", lead, f32, dev, True), _dense(loss, "loss", lead, f32, dev, True)
